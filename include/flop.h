@@ -66,7 +66,8 @@ typedef enum {
   FLOP_OP_L0 = 2,          /* flop_expected_l0_lagrangian (T = gates n, r = n_seg) */
   FLOP_OP_COMPACT = 3,     /* flop_compact_ranks                       */
   FLOP_OP_COMPACT_FWD = 4, /* flop_compact_fwd (r = k)                 */
-  FLOP_OP_EMBEDDING_BWD = 5 /* flop_gated_embedding_bwd (r = d_i)       */
+  FLOP_OP_EMBEDDING_BWD = 5, /* flop_gated_embedding_bwd (r = d_i)      */
+  FLOP_OP_COMPACT_FWD_I8 = 6 /* flop_compact_fwd_i8 (r = k)             */
 } flop_op_t;
 
 const char* flop_status_string(int status);
@@ -431,6 +432,66 @@ int flop_compact_fwd(const void* X, int64_t ldx, const void* Qc, int64_t ldqc, c
 int flop_chain_fwd(const void* X, int64_t ldx, const void* Q, int64_t ldq, const void* P, int64_t ldp,
                    const float* z, void* Y, int64_t ldy, int64_t T, int64_t d_in, int64_t d_out, int64_t r,
                    int dt, void* stream);
+
+/* Compact factors in 8 bits (no counterpart in the paper, which stops at pruning; a deployed model keeps its factors in
+ * 8-bit integers with a scale per output channel and quantises its tokens as they come).  8-bit matrices are row-major
+ * like all others; their leading dimensions are multiples of 16 and their base pointers 16-byte aligned
+ * (FLOP_ERR_UNSUPPORTED otherwise), and the header's rule on columns behind a row's end holds for them.
+ *
+ * flop_quantize_rows: X[rows, cols] (type dt) to 8 bits with a scale per row:
+ *     scale[i] = max_j |X[i, j]| / 127,   Xq[i, j] = 127 X[i, j] / max_j |X[i, j]|  rounded half to even
+ * The rounding is that of the exact quotient.  A row of zeros has scale 0 and zeros.  A row that holds an infinity or a NaN has
+ * scale NaN and zeros, so that what is computed from it is NaN.  Rows are tokens (X[T, d_in]) or output channels
+ * (Qc[k, d_in], Pc[d_out, k]).  Columns of Xq from cols on are left untouched.  Xq may not overlap X. */
+int flop_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dt, int8_t* Xq, int64_t ldxq,
+                       float* scale, void* stream);
+
+/* The product of 8-bit operands, the sums scaled back:
+ *     Y[m, n] = (sum_k A[m, k] B[n, k]) * a_scale[m] * b_scale[n]
+ * with exact 32-bit sums (K <= 131071, FLOP_ERR_UNSUPPORTED beyond), scaled in fp32 and stored in dt (dt is the type of Y here).
+ * Any 8-bit values, -128 among them.  At most 4,000,000 rows of A and of B. */
+int flop_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb,
+                 const float* b_scale, void* Y, int64_t ldy, int64_t M, int64_t N, int64_t K, int dt, void* stream);
+
+/* flop_compact_fwd with both products in 8 bits: Y = (X Qc^T) Pc^T, where Qc and Pc are given as 8-bit rows with a scale each
+ * (flop_quantize_rows of the factors flop_compact_ranks wrote) and dt is the type of X and Y.  Tokens are quantised as
+ * flop_quantize_rows does it; with acc the 32-bit sums of the first product,
+ *     h[t, j] = acc[t, j] q_scale[j],   hq[t, j] = 127 h[t, j] / max_j |h[t, j]|  rounded half to even (as fp64 has it),
+ *     h_scale[t] = x_scale[t] max_j |h[t, j]| / 127,   Y[t, n] = (sum_j hq[t, j] Pq[n, j]) * h_scale[t] * p_scale[n]
+ * The integers do not depend on the number of tokens in the call or on the kernels that serve it, and a token's result only on that token.
+ * ws: flop_workspace_bytes(FLOP_OP_COMPACT_FWD_I8, T, d_in, d_out, k, dt). */
+int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ldqq, const float* q_scale,
+                        const int8_t* Pq, int64_t ldpq, const float* p_scale, void* Y, int64_t ldy, int64_t T,
+                        int64_t d_in, int64_t d_out, int64_t k, int dt, void* ws, size_t ws_bytes, void* stream);
+
+/* Distillation of a dense teacher into the pruned model (no counterpart in the paper): the loss of the student's logits
+ * S[T, V] (type dt) against the teacher's K largest logits per token, t_logits[T, K] f32 (ld ldt) and their words
+ * t_idx[T, K] int32 (ld ldi).  Slots whose index is outside [0, V) are empty, of equal indices in a row the first slot
+ * counts; L is the set of words listed.  With tau = temperature (positive, finite) and p = softmax(S / tau):
+ *   t_lse NULL:  q = softmax over L of t / tau                              loss = sum_L q (log q - log p)
+ *   t_lse[T]:    q = exp(t / tau - t_lse), t_lse the teacher's log sum of exp(t / tau) over ALL words, r = max(0, 1 - sum_L q)
+ *                (0 if L is the whole vocabulary)          loss = sum_L q (log q - log p) + r (log r - log p_rest)
+ *   p_rest = sum of p outside L: the rest of the vocabulary is one more bucket.
+ *   dS[t, v] = g (p_v - q_v) on L, g (p_v - r p_v / p_rest) outside; g = weight[t] / tau (times dloss[t] in _bwd)
+ * weight[T] (nullable: 1) multiplies loss and gradient.  Tokens with g = 0 (loss: weight = 0) and tokens whose list is empty have
+ * loss 0 and gradient 0, whatever their logits hold.  A NaN or +infinity among the other tokens' logits makes the
+ * loss NaN; -infinity (a word that is masked out) has probability 0.
+ *   _fwd       loss[T]; stats[T * 4] f32 (nullable) keeps what _bwd needs
+ *   _bwd       dS[T, V] from the same arguments and stats; dloss[T] (nullable: 1) is the gradient arriving at loss
+ *   _fwd_bwd   both in one pass over the logits, for a caller that knows the weight of every token beforehand
+ * dS may be S (same ld), no other overlap.  Columns from V on are left untouched.  V <= 1,048,576, K <= 1024.  Sums are fp32 in a fixed
+ * order: results are reproducible.  Needs no workspace. */
+int flop_distill_topk_fwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt,
+                          const int32_t* t_idx, int64_t ldi, int64_t K, const float* t_lse, const float* weight,
+                          float temperature, float* loss, float* stats, void* stream);
+int flop_distill_topk_bwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt,
+                          const int32_t* t_idx, int64_t ldi, int64_t K, const float* t_lse, const float* weight,
+                          float temperature, const float* stats, const float* dloss, void* dS, int64_t ldds,
+                          void* stream);
+int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits,
+                              int64_t ldt, const int32_t* t_idx, int64_t ldi, int64_t K, const float* t_lse,
+                              const float* weight, float temperature, float* loss, void* dS, int64_t ldds,
+                              void* stream);
 
 #ifdef __cplusplus
 }

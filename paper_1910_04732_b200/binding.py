@@ -24,7 +24,7 @@ LIB_PATH = os.path.join(_HERE, "libflop_b200.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 F32, BF16 = 0, 1
-OP_FWD, OP_BWD, OP_L0, OP_COMPACT, OP_COMPACT_FWD, OP_EMBEDDING_BWD = range(6)
+OP_FWD, OP_BWD, OP_L0, OP_COMPACT, OP_COMPACT_FWD, OP_EMBEDDING_BWD, OP_COMPACT_FWD_I8 = range(7)
 
 EXPORTS = ("flop_status_string", "flop_last_async_status", "flop_device_status", "flop_sync_bytes",
            "flop_gated_lowrank_fwd_chained", "flop_gated_lowrank_bwd_chained", "flop_selftest_wait_timeout", "flop_launch_count", "flop_plan_tile_schedule", "flop_plan_chain_queue", "flop_scale_rows_grouped", "flop_dlog_alpha_finish_grouped", "flop_gemm_timing_begin",
@@ -34,7 +34,8 @@ EXPORTS = ("flop_status_string", "flop_last_async_status", "flop_device_status",
            "flop_expected_l0_lagrangian",
            "flop_expected_l0_lagrangian_noalloc", "flop_agp_gates", "flop_gated_embedding_fwd",
            "flop_gated_embedding_bwd",
-           "flop_compact_ranks", "flop_compact_fwd", "flop_chain_fwd")
+           "flop_compact_ranks", "flop_compact_fwd", "flop_chain_fwd", "flop_quantize_rows", "flop_gemm_i8", "flop_compact_fwd_i8",
+           "flop_distill_topk_fwd", "flop_distill_topk_bwd", "flop_distill_topk_fwd_bwd")
 
 
 class HcParams(ctypes.Structure):
@@ -149,6 +150,13 @@ def load_library() -> ctypes.CDLL:
     lib.flop_compact_ranks.argtypes = [vp, ci, HcParams, i64, vp, i64, vp, i64, i64, i64, ci,
                                        vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     lib.flop_compact_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, i64, ci, vp, sz, vp]
+    lib.flop_quantize_rows.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, vp]
+    lib.flop_gemm_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, i64, ci, vp]
+    lib.flop_compact_fwd_i8.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, i64, i64, ci, vp, sz, vp]
+    student = [vp, i64, i64, i64, ci, vp, i64, vp, i64, i64, vp, vp, ctypes.c_float]
+    lib.flop_distill_topk_fwd.argtypes = student + [vp, vp, vp]
+    lib.flop_distill_topk_bwd.argtypes = student + [vp, vp, vp, i64, vp]
+    lib.flop_distill_topk_fwd_bwd.argtypes = student + [vp, vp, i64, vp]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ci
     lib.flop_launch_count.restype = ctypes.c_ulonglong
@@ -478,3 +486,32 @@ def compact_ranks(log_alpha_or_z, mode: int, hc, idx, k_dev, z_det=None, P=None,
 
 def compact_fwd(X, Qc, Pc, Y, k: int, ws) -> None:
     _check(_native().compact_fwd(X, Qc, Pc, Y, k, ws), "flop_compact_fwd")
+
+
+def quantize_rows(X, Xq, scale) -> None:
+    """flop_quantize_rows: Xq (int8, 16-byte rows: `padded(..., torch.int8, multiple=16)`) and scale[rows] f32 from X."""
+    _check(_native()._operators.quantize_rows(X, Xq, scale), "flop_quantize_rows")
+
+
+def gemm_i8(A, B, a_scale, b_scale, Y) -> None:
+    """flop_gemm_i8: Y[M,N] (bf16 or f32) = (A[M,K] B[N,K]^T) * a_scale[M] * b_scale[N], A and B int8."""
+    _check(_native()._operators.gemm_i8(A, B, a_scale, b_scale, Y), "flop_gemm_i8")
+
+
+def compact_fwd_i8(X, Qq, q_scale, Pq, p_scale, Y, k: int, ws) -> None:
+    """flop_compact_fwd_i8: compact_fwd on factors in 8 bits (workspace: OP_COMPACT_FWD_I8)."""
+    _check(_native()._operators.compact_fwd_i8(X, Qq, q_scale, Pq, p_scale, Y, k, ws), "flop_compact_fwd_i8")
+
+
+def distill_topk_fwd(S, t_logits, t_idx, t_lse, weight, temperature: float, loss, stats=None) -> None:
+    """flop_distill_topk_fwd: loss[T] f32 of the logits S[T, V] against the teacher's top logits; stats[T, 4] f32 for the backward call."""
+    _check(_native()._operators.distill_topk_fwd(S, t_logits, t_idx, t_lse, weight, temperature, loss, stats), "flop_distill_topk_fwd")
+
+
+def distill_topk_bwd(S, t_logits, t_idx, t_lse, weight, temperature: float, stats, dloss, dS) -> None:
+    _check(_native()._operators.distill_topk_bwd(S, t_logits, t_idx, t_lse, weight, temperature, stats, dloss, dS), "flop_distill_topk_bwd")
+
+
+def distill_topk_fwd_bwd(S, t_logits, t_idx, t_lse, weight, temperature: float, loss, dS) -> None:
+    """flop_distill_topk_fwd_bwd: loss and gradient in one pass over the logits (dS may be S)."""
+    _check(_native()._operators.distill_topk_fwd_bwd(S, t_logits, t_idx, t_lse, weight, temperature, loss, dS), "flop_distill_topk_fwd_bwd")

@@ -204,12 +204,143 @@ FLOP_METHOD(compact_fwd, 6) {   // X, Qc, Pc, Y, k, ws
   return call([&] { return flop_compact_fwd(X.p, X.ld, Qc.p, Qc.ld, Pc.p, Pc.ld, Y.p, Y.ld, X.rows, X.cols, Pc.rows, k, dt, ws, wb, st); });
 }
 
+// ---- the 8-bit products and the distillation loss (module _operators)
+float number(PyObject* o) {   // float(o)
+  PyObject* v = PyNumber_Float(o);
+  if (!v) throw Stop{};
+  const double d = PyFloat_AS_DOUBLE(v);
+  Py_DECREF(v);
+  return (float)d;
+}
+// A tensor of another type than the call reads would be read as that type: refused here, the library sees addresses only.
+void need(PyObject* o, at::ScalarType type, int64_t count, const char* what) {
+  const at::Tensor* t = tensor(o);
+  if (!t) return;
+  if (t->scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s: expected %s, got %s", what, at::toString(type), at::toString(t->scalar_type()));
+    throw Stop{};
+  }
+  if (count >= 0 && (!t->is_contiguous() || t->numel() < count)) {
+    PyErr_Format(PyExc_AssertionError, "%s: expected %lld contiguous values", what, (long long)count);
+    throw Stop{};
+  }
+}
+void same(int64_t a, int64_t b, const char* what) {
+  if (a == b) return;
+  PyErr_Format(PyExc_AssertionError, "%s: %lld against %lld", what, (long long)a, (long long)b);
+  throw Stop{};
+}
+
+FLOP_METHOD(quantize_rows, 3) {   // X, Xq, scale
+  const Mat X = matrix(a[0]), Xq = matrix(a[1]);
+  const int dt = storage(required(a[0]));
+  need(a[1], at::kChar, -1, "Xq"); need(a[2], at::kFloat, X.rows, "scale");
+  same(X.rows, Xq.rows, "rows of X and Xq"); same(X.cols, Xq.cols, "columns of X and Xq");
+  float* scale = ptr<float>(a[2]);
+  void* st = stream();
+  return call([&] { return flop_quantize_rows(X.p, X.ld, X.rows, X.cols, dt, (int8_t*)Xq.p, Xq.ld, scale, st); });
+}
+
+FLOP_METHOD(gemm_i8, 5) {   // A, B, a_scale, b_scale, Y
+  const Mat A = matrix(a[0]), B = matrix(a[1]), Y = matrix(a[4]);
+  const int dt = storage(required(a[4]));
+  need(a[0], at::kChar, -1, "A"); need(a[1], at::kChar, -1, "B");
+  need(a[2], at::kFloat, A.rows, "a_scale"); need(a[3], at::kFloat, B.rows, "b_scale");
+  same(A.cols, B.cols, "columns of A and B"); same(Y.rows, A.rows, "rows of Y and A"); same(Y.cols, B.rows, "columns of Y and rows of B");
+  const float *sa = ptr<float>(a[2]), *sb = ptr<float>(a[3]);
+  void* st = stream();
+  return call([&] { return flop_gemm_i8((const int8_t*)A.p, A.ld, sa, (const int8_t*)B.p, B.ld, sb, Y.p, Y.ld, A.rows, B.rows, A.cols, dt, st); });
+}
+
+FLOP_METHOD(compact_fwd_i8, 8) {   // X, Qq, q_scale, Pq, p_scale, Y, k, ws
+  const Mat X = matrix(a[0]), Q = matrix(a[1]), P = matrix(a[3]), Y = matrix(a[5]);
+  const int dt = storage(required(a[0]));
+  const int64_t k = integer(a[6]);
+  need(a[1], at::kChar, -1, "Qq"); need(a[3], at::kChar, -1, "Pq");
+  need(a[2], at::kFloat, k, "q_scale"); need(a[4], at::kFloat, P.rows, "p_scale");
+  same(storage(required(a[5])), dt, "types of Y and X"); same(Y.rows, X.rows, "rows of Y and X"); same(Y.cols, P.rows, "columns of Y and rows of Pq");
+  same(Q.cols, X.cols, "columns of Qq and X");
+  same(Q.rows >= k && P.cols >= k, 1, "k fits Qq and Pq");
+  const float *qs = ptr<float>(a[2]), *ps = ptr<float>(a[4]);
+  void* ws = ptr(a[7]); const size_t wb = numel(a[7]);
+  void* st = stream();
+  return call([&] {
+    return flop_compact_fwd_i8(X.p, X.ld, (const int8_t*)Q.p, Q.ld, qs, (const int8_t*)P.p, P.ld, ps, Y.p, Y.ld, X.rows, X.cols, P.rows, k, dt, ws, wb, st);
+  });
+}
+
+struct Distill { Mat S, t, idx; int dt; const float *lse, *weight; float tau; };
+Distill distill(PyObject* const* a) {   // S, t_logits, t_idx, t_lse, weight, temperature
+  Distill d;
+  d.S = matrix(a[0]); d.t = matrix(a[1]); d.idx = matrix(a[2]);
+  d.dt = storage(required(a[0]));
+  need(a[1], at::kFloat, -1, "t_logits"); need(a[2], at::kInt, -1, "t_idx");
+  need(a[3], at::kFloat, d.S.rows, "t_lse"); need(a[4], at::kFloat, d.S.rows, "weight");
+  same(d.t.rows, d.S.rows, "rows of t_logits and S"); same(d.idx.rows, d.S.rows, "rows of t_idx and S"); same(d.idx.cols, d.t.cols, "columns of t_idx and t_logits");
+  d.lse = ptr<float>(a[3]); d.weight = ptr<float>(a[4]);
+  d.tau = number(a[5]);
+  return d;
+}
+Mat gradient(PyObject* o, const Distill& d) {
+  const Mat g = matrix(o);
+  same(storage(required(o)), d.dt, "types of dS and S"); same(g.rows, d.S.rows, "rows of dS and S"); same(g.cols, d.S.cols, "columns of dS and S");
+  return g;
+}
+
+FLOP_METHOD(distill_topk_fwd, 8) {   // S, t_logits, t_idx, t_lse, weight, temperature, loss, stats
+  const Distill d = distill(a);
+  need(a[6], at::kFloat, d.S.rows, "loss"); need(a[7], at::kFloat, 4 * d.S.rows, "stats");
+  float *loss = ptr<float>(a[6]), *stats = ptr<float>(a[7]);
+  void* st = stream();
+  return call([&] {
+    return flop_distill_topk_fwd(d.S.p, d.S.ld, d.S.rows, d.S.cols, d.dt, (const float*)d.t.p, d.t.ld, (const int32_t*)d.idx.p, d.idx.ld, d.t.cols, d.lse, d.weight,
+                                 d.tau, loss, stats, st);
+  });
+}
+
+FLOP_METHOD(distill_topk_bwd, 9) {   // S, t_logits, t_idx, t_lse, weight, temperature, stats, dloss, dS
+  const Distill d = distill(a);
+  const Mat dS = gradient(a[8], d);
+  need(a[6], at::kFloat, 4 * d.S.rows, "stats"); need(a[7], at::kFloat, d.S.rows, "dloss");
+  const float *stats = ptr<float>(a[6]), *dloss = ptr<float>(a[7]);
+  void* st = stream();
+  return call([&] {
+    return flop_distill_topk_bwd(d.S.p, d.S.ld, d.S.rows, d.S.cols, d.dt, (const float*)d.t.p, d.t.ld, (const int32_t*)d.idx.p, d.idx.ld, d.t.cols, d.lse, d.weight,
+                                 d.tau, stats, dloss, dS.p, dS.ld, st);
+  });
+}
+
+FLOP_METHOD(distill_topk_fwd_bwd, 8) {   // S, t_logits, t_idx, t_lse, weight, temperature, loss, dS
+  const Distill d = distill(a);
+  const Mat dS = gradient(a[7], d);
+  need(a[6], at::kFloat, d.S.rows, "loss");
+  float* loss = ptr<float>(a[6]);
+  void* st = stream();
+  return call([&] {
+    return flop_distill_topk_fwd_bwd(d.S.p, d.S.ld, d.S.rows, d.S.cols, d.dt, (const float*)d.t.p, d.t.ld, (const int32_t*)d.idx.p, d.idx.ld, d.t.cols, d.lse,
+                                     d.weight, d.tau, loss, dS.p, dS.ld, st);
+  });
+}
+
 #define FLOP_ENTRY(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FLOP_ENTRY(gate_sample), FLOP_ENTRY(gated_lowrank_fwd), FLOP_ENTRY(gated_lowrank_bwd), FLOP_ENTRY(expected_l0_lagrangian),
                          FLOP_ENTRY(gated_embedding_fwd), FLOP_ENTRY(gated_embedding_bwd), FLOP_ENTRY(compact_ranks), FLOP_ENTRY(compact_fwd),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyMethodDef operator_methods[] = {FLOP_ENTRY(quantize_rows), FLOP_ENTRY(gemm_i8), FLOP_ENTRY(compact_fwd_i8), FLOP_ENTRY(distill_topk_fwd),
+                                  FLOP_ENTRY(distill_topk_bwd), FLOP_ENTRY(distill_topk_fwd_bwd), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef operators = {PyModuleDef_HEAD_INIT, "_operators", nullptr, -1, operator_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__binding_native(void) { return PyModule_Create(&module); }
+// The calls beside the layer's own path are a module of their own inside this one.
+PyMODINIT_FUNC PyInit__binding_native(void) {
+  PyObject* m = PyModule_Create(&module);
+  PyObject* o = m ? PyModule_Create(&operators) : nullptr;
+  if (!o || PyModule_AddObject(m, "_operators", o) < 0) {
+    Py_XDECREF(o);
+    Py_XDECREF(m);
+    return nullptr;
+  }
+  return m;
+}

@@ -33,6 +33,8 @@
 #include "gemm_few.cuh"
 #include "agp.cuh"
 #include "embedding.cuh"
+#include "distill.cuh"
+#include "quantized.cuh"
 
 using namespace flop;
 typedef __nv_bfloat16 bf16;
@@ -1206,6 +1208,87 @@ static int launch_l0_small(const float* log_alpha, int64_t n, const int64_t* seg
   return FLOP_OK;
 }
 
+namespace {
+
+// ---- 8-bit integers with a scale per row
+bool i8_ok(const void* p, int64_t ld) { return aligned16(p) && (ld % 16) == 0; }
+constexpr int64_t kMaxI8K = 131071;      // products of two 8-bit values that a 32-bit sum holds whatever they are
+constexpr int64_t kMaxI8Rows = 4000000;  // tiles of 64 rows in one grid dimension
+
+struct I8Ws {
+  int8_t* Xq; int64_t ldxq; float* x_scale;     // the tokens
+  int* acc; int64_t ldacc;                      // sums of the first product
+  int8_t* Hq; int64_t ldhq; float* h_scale;     // the intermediate
+  size_t bytes;
+};
+I8Ws plan_i8_ws(Arena& ar, int64_t T, int64_t d_in, int64_t k) {
+  I8Ws w{};
+  w.ldxq = round_up(std::max<int64_t>(d_in, 1), 16);
+  w.ldhq = w.ldacc = round_up(std::max<int64_t>(k, 1), 16);
+  w.Xq = (int8_t*)ar.take((size_t)T * w.ldxq);
+  w.x_scale = (float*)ar.take((size_t)T * 4);
+  w.acc = (int*)ar.take((size_t)T * w.ldacc * 4);
+  w.Hq = (int8_t*)ar.take((size_t)T * w.ldhq);
+  w.h_scale = (float*)ar.take((size_t)T * 4);
+  w.bytes = ar.used;
+  return w;
+}
+
+int launch_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dt, int8_t* Xq, int64_t ldxq, float* scale, cudaStream_t st) {
+  if (dt == FLOP_BF16) launch_k(i8::quantize_rows_kernel<bf16>, dim3((unsigned)rows), dim3(i8::kRowThreads), (size_t)0, st, (const bf16*)X, ldx, (int)cols, Xq, ldxq, scale);
+  else launch_k(i8::quantize_rows_kernel<float>, dim3((unsigned)rows), dim3(i8::kRowThreads), (size_t)0, st, (const float*)X, ldx, (int)cols, Xq, ldxq, scale);
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
+}
+// out: bf16, fp32 (scaled sums) or int (the sums)
+template <typename T>
+int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, T* Y, int64_t ldy, int64_t M,
+                   int64_t N, int64_t K, cudaStream_t st) {
+  launch_k(i8::gemm_simple_kernel<T>, dim3((unsigned)((M + 63) / 64), (unsigned)((N + 63) / 64)), dim3(256), (size_t)0, st, A, lda, B, ldb, a_scale, b_scale, Y,
+           ldy, (int)M, (int)N, (int)K);
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
+}
+
+// ---- distillation from top logits
+template <typename T, int MODE>
+int launch_distill_inst(const distill::Args& a, int64_t rows, cudaStream_t st) {
+  static OncePerDevice configured;
+  auto kern = distill::row_kernel<T, MODE>;
+  FLOP_TRY(allow_smem(configured, distill::kMaxVocab / 8 + 12 * distill::kMaxSlots, kern));
+  const size_t smem = (size_t)(a.V + 31) / 32 * 4 + (size_t)12 * a.K;
+  launch_k(kern, dim3((unsigned)rows), dim3(distill::kThreads), smem, st, a);
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
+}
+template <int MODE>
+int distill_impl(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi, int64_t K,
+                 const float* t_lse, const float* weight, float temperature, float* loss, float* stats, const float* stats_in, const float* dloss, void* dS,
+                 int64_t ldds, cudaStream_t st) {
+  if (T < 0 || V < 0 || K < 0 || !valid_dt(dt) || !(temperature > 0.f) || !(temperature < INFINITY)) return FLOP_ERR_INVALID_ARG;
+  if (T == 0) return FLOP_OK;
+  if ((MODE & distill::FWD) && !loss) return FLOP_ERR_INVALID_ARG;
+  if (MODE == distill::BWD && !stats_in) return FLOP_ERR_INVALID_ARG;
+  if (V > 0 && !check_mat(S, lds, V)) return FLOP_ERR_INVALID_ARG;
+  if (V > 0 && (MODE & distill::BWD) && !check_mat(dS, ldds, V)) return FLOP_ERR_INVALID_ARG;
+  if (K > 0 && (!check_mat(t_logits, ldt, K) || !check_mat(t_idx, ldi, K))) return FLOP_ERR_INVALID_ARG;
+  if (V > distill::kMaxVocab || K > distill::kMaxSlots || T > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  if (V > 0 && dt == FLOP_BF16 && (!bf16_ok(S, lds) || ((MODE & distill::BWD) && !bf16_ok(dS, ldds)))) return FLOP_ERR_UNSUPPORTED;
+  // every row is read whole before it is written, so the gradient may take the logits' place; half of it may not
+  if ((MODE & distill::BWD) && !(dS == S && ldds == lds) && Span(S, T, V, lds, elt(dt)).meets(Span(dS, T, V, ldds, elt(dt)))) return FLOP_ERR_INVALID_ARG;
+  distill::Args a{};
+  a.S = S; a.lds = lds; a.V = (int)V; a.t_logits = t_logits; a.ldt = ldt; a.t_idx = t_idx; a.ldi = ldi; a.K = (int)K; a.t_lse = t_lse; a.weight = weight;
+  a.inv_tau = (float)(1.0 / (double)temperature); a.c = (float)(1.4426950408889634 / (double)temperature);
+  a.loss = loss; a.stats = stats; a.stats_in = stats_in; a.dloss = dloss; a.dS = dS; a.ldds = ldds;
+  if (dt == FLOP_BF16) return launch_distill_inst<bf16, MODE>(a, T, st);
+  return launch_distill_inst<float, MODE>(a, T, st);
+}
+
+}  // namespace
+
 // ====================================================================== C ABI
 extern "C" {
 
@@ -1402,6 +1485,7 @@ int flop_workspace_bytes(int op, int64_t T, int64_t d_in, int64_t d_out, int64_t
     case FLOP_OP_L0: ar.used = l0_ws_bytes(T, r); break;
     case FLOP_OP_COMPACT: ar.used = 0; break;
     case FLOP_OP_EMBEDDING_BWD: ar.used = embedding_ws_bytes(T, r); break;
+    case FLOP_OP_COMPACT_FWD_I8: plan_i8_ws(ar, T, d_in, r); break;
     default: return FLOP_ERR_INVALID_ARG;
   }
   *out_bytes = align_up(ar.used, 256);
@@ -2484,6 +2568,72 @@ int flop_compact_ranks(const float* log_alpha_or_z, int mode, flop_hc_params_t h
     FLOP_CUDA(cudaGetLastError());
   }
   return FLOP_OK;
+}
+
+int flop_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dt, int8_t* Xq, int64_t ldxq, float* scale, void* stream) {
+  if (rows < 0 || cols < 0 || !valid_dt(dt)) return FLOP_ERR_INVALID_ARG;
+  if (rows == 0) return FLOP_OK;
+  if (!scale || (cols > 0 && (!check_mat(X, ldx, cols) || !check_mat(Xq, ldxq, cols)))) return FLOP_ERR_INVALID_ARG;
+  if (cols > 0 && ((dt == FLOP_BF16 && !bf16_ok(X, ldx)) || !i8_ok(Xq, ldxq))) return FLOP_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX || cols > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  if (Span(X, rows, cols, ldx, elt(dt)).meets(Span(Xq, rows, cols, ldxq, 1))) return FLOP_ERR_INVALID_ARG;
+  return launch_quantize_rows(X, ldx, rows, cols, dt, Xq, ldxq, scale, (cudaStream_t)stream);
+}
+
+int flop_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, void* Y, int64_t ldy, int64_t M,
+                 int64_t N, int64_t K, int dt, void* stream) {
+  if (M < 0 || N < 0 || K < 0 || !valid_dt(dt)) return FLOP_ERR_INVALID_ARG;
+  if (M == 0 || N == 0) return FLOP_OK;
+  if (!check_mat(Y, ldy, N)) return FLOP_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dt == FLOP_BF16 && !bf16_ok(Y, ldy)) return FLOP_ERR_UNSUPPORTED;
+  if (K == 0) return dt == FLOP_BF16 ? zero_2d<bf16>(Y, ldy, M, N, st) : zero_2d<float>(Y, ldy, M, N, st);
+  if (!check_mat(A, lda, K) || !check_mat(B, ldb, K) || !a_scale || !b_scale) return FLOP_ERR_INVALID_ARG;
+  if (!i8_ok(A, lda) || !i8_ok(B, ldb) || K > kMaxI8K || M > kMaxI8Rows || N > kMaxI8Rows) return FLOP_ERR_UNSUPPORTED;
+  if (dt == FLOP_BF16) return launch_gemm_i8<bf16>(A, lda, a_scale, B, ldb, b_scale, (bf16*)Y, ldy, M, N, K, st);
+  return launch_gemm_i8<float>(A, lda, a_scale, B, ldb, b_scale, (float*)Y, ldy, M, N, K, st);
+}
+
+int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ldqq, const float* q_scale, const int8_t* Pq, int64_t ldpq, const float* p_scale,
+                        void* Y, int64_t ldy, int64_t T, int64_t d_in, int64_t d_out, int64_t k, int dt, void* ws, size_t ws_bytes, void* stream) {
+  if (T < 0 || d_in < 0 || d_out < 0 || k < 0 || !valid_dt(dt)) return FLOP_ERR_INVALID_ARG;
+  if (T == 0 || d_out == 0) return FLOP_OK;
+  if (!check_mat(Y, ldy, d_out)) return FLOP_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dt == FLOP_BF16 && !bf16_ok(Y, ldy)) return FLOP_ERR_UNSUPPORTED;
+  if (k == 0 || d_in == 0) return dt == FLOP_BF16 ? zero_2d<bf16>(Y, ldy, T, d_out, st) : zero_2d<float>(Y, ldy, T, d_out, st);
+  if (!check_mat(X, ldx, d_in) || !check_mat(Qq, ldqq, d_in) || !check_mat(Pq, ldpq, k) || !q_scale || !p_scale) return FLOP_ERR_INVALID_ARG;
+  if ((dt == FLOP_BF16 && !bf16_ok(X, ldx)) || !i8_ok(Qq, ldqq) || !i8_ok(Pq, ldpq)) return FLOP_ERR_UNSUPPORTED;
+  if (d_in > kMaxI8K || k > kMaxI8K || T > kMaxI8Rows || d_out > kMaxI8Rows) return FLOP_ERR_UNSUPPORTED;
+  Arena probe{nullptr, 0, 0};
+  FLOP_TRY(check_ws(ws, ws_bytes, plan_i8_ws(probe, T, d_in, k).bytes));
+  Arena ar{(unsigned char*)ws, ws_bytes, 0};
+  const I8Ws w = plan_i8_ws(ar, T, d_in, k);
+  FLOP_TRY(launch_quantize_rows(X, ldx, T, d_in, dt, w.Xq, w.ldxq, w.x_scale, st));
+  FLOP_TRY(launch_gemm_i8<int>(w.Xq, w.ldxq, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, T, k, d_in, st));
+  launch_k(i8::requantize_rows_kernel, dim3((unsigned)T), dim3(i8::kRowThreads), (size_t)0, st, (const int*)w.acc, w.ldacc, (int)k, q_scale, (const float*)w.x_scale,
+           w.Hq, w.ldhq, w.h_scale);
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  if (dt == FLOP_BF16) return launch_gemm_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
+  return launch_gemm_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
+}
+
+int flop_distill_topk_fwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi,
+                          int64_t K, const float* t_lse, const float* weight, float temperature, float* loss, float* stats, void* stream) {
+  return distill_impl<distill::FWD>(S, lds, T, V, dt, t_logits, ldt, t_idx, ldi, K, t_lse, weight, temperature, loss, stats, nullptr, nullptr, nullptr, 0,
+                                    (cudaStream_t)stream);
+}
+int flop_distill_topk_bwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi,
+                          int64_t K, const float* t_lse, const float* weight, float temperature, const float* stats, const float* dloss, void* dS, int64_t ldds,
+                          void* stream) {
+  return distill_impl<distill::BWD>(S, lds, T, V, dt, t_logits, ldt, t_idx, ldi, K, t_lse, weight, temperature, nullptr, nullptr, stats, dloss, dS, ldds,
+                                    (cudaStream_t)stream);
+}
+int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi,
+                              int64_t K, const float* t_lse, const float* weight, float temperature, float* loss, void* dS, int64_t ldds, void* stream) {
+  return distill_impl<distill::BOTH>(S, lds, T, V, dt, t_logits, ldt, t_idx, ldi, K, t_lse, weight, temperature, loss, nullptr, nullptr, nullptr, dS, ldds,
+                                     (cudaStream_t)stream);
 }
 
 }  // extern "C"

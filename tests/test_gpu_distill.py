@@ -1,0 +1,320 @@
+"""The distillation loss against the fp64 oracle: every form, type, width and list where it can go wrong.
+
+Bound.  A probability 2^(x c - m): c and the product are rounded (2^-24 |x c| each, in units of log 2), the exponential is good to 2^-22, a sum of
+V terms of which a thread adds at most V / 32 in turn to (V / 32 + 64) 2^-24.  `e` below is that for one probability, p or q; a loss term has two logarithms
+and one q, a gradient p - q (outside the list p - r p / p_rest, where r = 1 - sum q has the absolute error of q), rounded to its type.  That error of r is there
+however small r is: r may be 0 in the oracle and e in fp32.  It moves the gradient by e p / p_rest and the loss by e (1 + |log r| + |log p_rest|), so
+both are counted wherever the rest is a bucket."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as O
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+STORE = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_1910_04732_b200 import build, binding
+    build.build()
+    binding.load_library()
+    return binding
+
+
+def rows_of(rows, cols, dtype, fill, extra=0):
+    per = 16 // torch.empty((), dtype=dtype).element_size()
+    ld = (cols + per - 1) // per * per + extra * per
+    return torch.full((rows, max(ld, per)), fill, dtype=dtype, device="cuda")[:, :cols]
+
+
+def behind(t):
+    return t.as_strided((t.shape[0], t.stride(0) - t.shape[1]), (t.stride(0), 1), t.storage_offset() + t.shape[1])
+
+
+class Case:
+    def __init__(self, T, V, K, dtype=BF, tau=1.0, rest=True, weighted=True, seed=0, extra=0, spread=1.0):
+        g = np.random.default_rng([seed, T, V, K])
+        n = min(K, V)
+        teacher = (g.standard_normal((T, V)) + 10 * g.random((T, V)) ** max(1.0, V / 20)) * spread
+        student = 0.8 * teacher + 0.7 * g.standard_normal((T, V)) * spread
+        top = np.argsort(-teacher, axis=1)[:, :n]
+        self.idx = np.full((T, K), -1, np.int32)
+        self.t = np.full((T, K), np.nan, np.float32)
+        self.idx[:, :n], self.t[:, :n] = top, np.take_along_axis(teacher, top, 1)
+        self.lse = np.array([math.log(math.fsum(np.exp(r / tau - r.max() / tau))) + r.max() / tau for r in teacher]).astype(np.float32) if rest else None
+        self.weight = g.uniform(0.1, 2.0, T).astype(np.float32) if weighted else None
+        self.tau, self.dtype, self.T, self.V, self.K = tau, dtype, T, V, K
+        self.S = rows_of(T, V, dtype, float("nan"), extra)
+        self.S.copy_(torch.from_numpy(student.astype(np.float32)))
+        self.dloss = None
+        self.extra = extra
+
+    def device(self):
+        d = lambda a: None if a is None else torch.from_numpy(a).cuda()  # noqa: E731
+        return d(self.t), d(self.idx), d(self.lse), d(self.weight), self.tau
+
+    def run(self, b, form, in_place=False):
+        """(loss, gradient or None)"""
+        a = self.device()
+        loss, S = torch.full((self.T,), -3.0, device="cuda"), self.S
+        if form == "fwd":
+            b.distill_topk_fwd(S, *a, loss)
+            return loss, None
+        if in_place:
+            S = self.S.as_strided(self.S.shape, self.S.stride()).clone(memory_format=torch.preserve_format)
+            S = rows_of(self.T, self.V, self.dtype, float("nan"), self.extra)
+            S.copy_(self.S)
+        dS = S if in_place else rows_of(self.T, self.V, self.dtype, -7.0, self.extra)
+        if form == "both":
+            b.distill_topk_fwd_bwd(S, *a, loss, dS)
+        else:
+            stats = torch.full((self.T, 4), -5.0, device="cuda")
+            b.distill_topk_fwd(S, *a, loss, stats)
+            b.distill_topk_bwd(S, *a, stats, None if self.dloss is None else torch.from_numpy(self.dloss).cuda(), dS)
+        if not in_place:
+            assert torch.all(behind(dS) == -7.0)
+        return loss, dS
+
+    def check(self, b, form, in_place=False):
+        loss, dS = self.run(b, form, in_place)
+        S = self.S.cpu().double().numpy()
+        want, grad, facts = O.distill_topk(S, self.t, self.idx, self.lse, self.weight, self.tau)
+        got = loss.cpu().double().numpy()
+        w = np.ones(self.T) if self.weight is None else self.weight.astype(np.float64)
+        up = w / self.tau * (1.0 if self.dloss is None or form != "bwd" else self.dloss)
+        for i, f in enumerate(facts):
+            if f is None:
+                assert got[i] == 0 and (dS is None or not torch.any(dS[i])), i
+                continue
+            log2 = lambda a: (np.abs(a[np.isfinite(a)]).max(initial=0.0) if a is not None else 0.0) / self.tau / math.log(2)  # noqa: E731
+            size = log2(S[i]) + log2(self.t[i][self.idx[i] >= 0].astype(np.float64)) + (0 if self.lse is None else abs(float(self.lse[i])) / math.log(2))
+            e = (self.V / 32 + 64) * U + 8 * U + 2 * U * size
+            bound = abs(w[i]) * (2 * e * (1 + f["terms"]) + (e * (1 + f["log_r"]) * 2 if self.lse is not None else 0)) + abs(want[i]) * 2 * U
+            assert abs(got[i] - want[i]) <= bound, (i, got[i], want[i], bound)
+            if dS is None:
+                continue
+            g = grad[i] if self.dloss is None or form != "bwd" else grad[i] * self.dloss[i]
+            allowed = abs(up[i]) * (2 * e * (f["p"] + f["q"]) + 2 * (e + e * f["r"]) * f["pull"]) + np.abs(g) * (STORE[self.dtype] + 3 * U) + 1e-38
+            off = np.abs(dS[i].cpu().double().numpy() - g)
+            assert np.all(off <= allowed), (i, int(np.argmax(off / allowed)), float(np.max(off / allowed)))
+        assert b.device_status() == b.OK
+        return loss, dS
+
+
+FORMS = ["fwd", "bwd", "both"]
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("T,V,K,extra", [(1, 1, 1, 0), (3, 2, 1, 0), (5, 7, 3, 1), (2, 8, 8, 0), (3, 31, 40, 0), (4, 33, 5, 2), (70, 205, 16, 0), (9, 256, 1, 0), (3, 1000, 100, 0), (5, 2047, 31, 1),
+                                         (2, 2049, 33, 0), (3, 4099, 300, 0), (2, 8200, 64, 0), (3, 16400, 20, 0), (2, 33000, 1024, 0), (1, 50001, 100, 1), (2, 66000, 7, 0)])
+def test_sizes(b, form, dtype, rest, T, V, K, extra):
+    Case(T, V, K, dtype, 1.0, rest, extra=extra).check(b, form)
+
+
+@pytest.mark.parametrize("form", ["fwd", "both"])
+@pytest.mark.parametrize("V", [131071, 131088, 200003, 262145, 530000, 1048576])
+def test_wide_vocabularies(b, form, V):
+    for dtype in (BF, F):
+        Case(2, V, 50, dtype, 2.0, True).check(b, form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("tau", [0.3, 2.0, 3.5, 20.0])
+@pytest.mark.parametrize("rest", [True, False])
+def test_temperatures(b, form, tau, rest):
+    for dtype in (BF, F):
+        Case(4, 3001, 40, dtype, tau, rest, weighted=False).check(b, form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("V", [205, 5000, 40000])
+def test_lists(b, form, rest, V):
+    """Shorter lists, empty ones, repeated and foreign words; rows of weight 0 that hold anything."""
+    for dtype in (BF, F):
+        c = Case(12, V, 20, dtype, 1.5, rest)
+        c.idx[1, 7:] = -1
+        c.idx[2] = -1                                       # an empty list
+        c.idx[3, 1::2] = V                                  # words of another vocabulary
+        c.idx[4, 10:] = c.idx[4, :10]                       # every word twice: the first slot counts
+        c.idx[5] = c.idx[5, 0]                              # one word twenty times
+        c.idx[6, 3] = 2 ** 31 - 1
+        c.idx[7, 3] = -2 ** 31
+        c.idx[8, :2] = [0, V - 1]
+        c.weight[9] = 0
+        c.S[9, 3], c.S[9, 4], c.t[9, 0] = float("nan"), float("inf"), float("nan")
+        if rest:
+            c.lse[9] = np.nan
+        c.weight[10] = -0.5
+        c.t[11, 0] = -np.inf                                # a word that the teacher rules out
+        c.t[c.idx < 0] = np.nan
+        c.S[2, 1] = float("nan")                            # not looked at either
+        c.check(b, form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("rest", [True, False])
+def test_masked_words(b, form, rest):
+    """-inf in the student's logits: outside the list (also all of it), and on it where the teacher gives nothing."""
+    for dtype in (BF, F):
+        c = Case(4, 700, 12, dtype, 1.0, rest)
+        c.S[0, torch.from_numpy(np.setdiff1d(np.arange(0, 700, 3), c.idx[0])).cuda()] = float("-inf")
+        c.S[1, int(c.idx[1, 2])] = float("-inf")
+        c.t[1, 2] = -np.inf
+        if not rest:
+            out = np.setdiff1d(np.arange(700), c.idx[2])
+            c.S[2, torch.from_numpy(out).cuda()] = float("-inf")
+        c.check(b, form)
+
+
+def test_infinite_and_undefined_losses(b):
+    for dtype in (BF, F):
+        for V in (300, 9000):
+            c = Case(6, V, 10, dtype, 1.0, True)
+            out = torch.from_numpy(np.setdiff1d(np.arange(V), c.idx[0])).cuda()
+            c.S[0, out] = float("-inf")                     # the teacher gives the rest something, the student nothing
+            c.S[1, int(c.idx[1, 0])] = float("-inf")        # the same on the list
+            c.S[2, V // 2], c.S[3, V - 1] = float("nan"), float("inf")
+            c.S[4] = float("-inf")
+            for form in FORMS:
+                loss, dS = c.run(b, form)
+                assert torch.isinf(loss[:2]).all() and torch.isnan(loss[2:5]).all() and torch.isfinite(loss[5])
+                if dS is not None:
+                    assert torch.isfinite(dS[0]).all() and torch.isfinite(dS[5]).all() and torch.isnan(dS[2]).all()
+
+
+@pytest.mark.parametrize("form", ["bwd", "both"])
+def test_gradient_in_place(b, form):
+    for dtype in (BF, F):
+        for T, V, K in ((30, 205, 16), (5, 6001, 40), (3, 40000, 20), (2, 140000, 30)):
+            c = Case(T, V, K, dtype, 2.0, True)
+            _, want = c.run(b, form)
+            _, got = c.check(b, form, in_place=True)
+            assert torch.equal(got, want) and torch.isnan(behind(got)).all()
+
+
+def test_forward_and_backward_are_the_call_that_does_both(b):
+    for dtype in (BF, F):
+        for V in (205, 3000, 50000):
+            c = Case(9, V, 30, dtype, 2.0, True)
+            c.dloss = np.random.default_rng(V).uniform(-1, 1, 9).astype(np.float32)
+            c.dloss[4] = 0
+            c.check(b, "bwd")
+            loss, dS = c.run(b, "both")
+            c.dloss = None
+            alone, dS2 = c.run(b, "bwd")
+            only, _ = c.run(b, "fwd")
+            assert torch.equal(loss, alone) and torch.equal(loss, only)
+            err = (dS.double() - dS2.double()).norm() / dS.double().norm()
+            assert err < 2 * STORE[dtype] + 1e-6
+
+
+def test_gradient_is_the_difference_of_the_library_s_losses(b):
+    """Central differences of the loss call itself; h = 2^-4 makes the fp32 rounding of the losses (about 2^-21 each) 2^-18 and the third derivative
+    (below 2 for tau = 1) h^2 / 3 = 1.3e-3."""
+    V, K = 40, 8
+    for rest in (True, False):
+        c = Case(1, V, K, F, 1.0, rest, weighted=False)
+        _, dS = c.run(b, "both")
+        h, many = 2.0 ** -4, Case(2 * V, V, K, F, 1.0, rest, weighted=False)
+        many.t[:], many.idx[:] = c.t[0], c.idx[0]
+        if rest:
+            many.lse[:] = c.lse[0]
+        many.S.copy_(c.S.expand(2 * V, V))
+        many.S[:V] += h * torch.eye(V, device="cuda")
+        many.S[V:] -= h * torch.eye(V, device="cuda")
+        loss, _ = many.run(b, "fwd")
+        diff = (loss[:V] - loss[V:]) / (2 * h)
+        assert torch.all((diff - dS[0]).abs() < 1.3e-3 + 2.0 ** -17)
+
+
+def test_far_apart_logits(b):
+    """Logits of hundreds: the rest of the vocabulary lies far below the list, or far above it."""
+    for dtype in (BF, F):
+        for rest in (True, False):
+            c = Case(4, 900, 10, dtype, 1.0, rest, spread=30.0)
+            c.S[1, torch.from_numpy(c.idx[1].astype(np.int64)).cuda()] = 400.0
+            c.S[2, torch.from_numpy(c.idx[2].astype(np.int64)).cuda()] = -400.0
+            for form in FORMS:
+                c.check(b, form)
+
+
+def test_fp32_rows_at_any_address(b):
+    for T, V, off, ld in ((5, 205, 1, 207), (3, 5001, 3, 5001), (3, 40001, 2, 40006)):
+        c = Case(T, V, 12, F, 1.0, True)
+        base = torch.full((off + T * ld + 8,), float("nan"), device="cuda")
+        S = base.as_strided((T, V), (ld, 1), off)
+        S.copy_(c.S)
+        c.S = S
+        out = torch.full((off + T * ld + 8,), -7.0, device="cuda")
+        dS = out.as_strided((T, V), (ld, 1), off)
+        loss = torch.zeros(T, device="cuda")
+        b.distill_topk_fwd_bwd(S, *c.device(), loss, dS)
+        c.S = rows_of(T, V, F, 0.0)
+        c.S.copy_(S)
+        loss2, dS2 = c.check(b, "both")
+        assert torch.allclose(loss, loss2, rtol=1e-5) and torch.allclose(dS, dS2, rtol=1e-4, atol=1e-9)
+        assert torch.all(out[:off] == -7) and torch.all(out[off + (T - 1) * ld + V:] == -7)
+
+
+def test_strided_teacher(b):
+    c = Case(6, 500, 9, BF, 1.0, True)
+    _, want = c.run(b, "both")
+    t, idx, lse, w, tau = c.device()
+    wide_t, wide_i = torch.full((6, 30), float("nan"), device="cuda"), torch.full((6, 30), 3, dtype=torch.int32, device="cuda")
+    wide_t[:, 5:14], wide_i[:, 7:16] = t, idx
+    loss, dS = torch.zeros(6, device="cuda"), rows_of(6, 500, BF, 0.0)
+    b.distill_topk_fwd_bwd(c.S, wide_t[:, 5:14], wide_i[:, 7:16], lse, w, tau, loss, dS)
+    assert torch.equal(dS, want)
+
+
+def test_nothing_to_do(b):
+    S, none = rows_of(4, 100, BF, 1.0), torch.zeros(4, 0, device="cuda")
+    loss, dS = torch.full((4,), -3.0, device="cuda"), rows_of(4, 100, BF, -7.0)
+    b.distill_topk_fwd_bwd(S, none, none.int(), None, None, 1.0, loss, dS)                 # K = 0
+    assert not torch.any(loss) and not torch.any(dS) and torch.all(behind(dS) == -7)
+    loss.fill_(-3.0)
+    b.distill_topk_fwd(torch.zeros(4, 0, dtype=BF, device="cuda"), torch.zeros(4, 3, device="cuda"), torch.zeros(4, 3, dtype=torch.int32, device="cuda"), None, None, 1.0, loss)
+    assert not torch.any(loss)                                                               # V = 0
+
+
+def test_offsets_beyond_32_bits(b):
+    T, V, K = 17000, 128000, 8                       # 2.2e9 logits, 4.4 GB
+    small = Case(2, V, K, BF, 1.0, True)
+    S = torch.zeros(T, V, dtype=BF, device="cuda")
+    S[-2:] = small.S
+    a = list(small.device())
+    for i in range(4):
+        a[i] = torch.cat([torch.zeros(T - 2, *a[i].shape[1:], dtype=a[i].dtype, device="cuda"), a[i]])
+    loss, loss2 = torch.full((T,), -3.0, device="cuda"), torch.zeros(2, device="cuda")
+    b.distill_topk_fwd_bwd(S, *a, loss, S)
+    dS2 = rows_of(2, V, BF, 0.0)
+    b.distill_topk_fwd_bwd(small.S, *small.device(), loss2, dS2)
+    assert torch.equal(S[-2:], dS2) and torch.equal(loss[-2:], loss2) and not torch.any(S[:-2]) and not torch.any(loss[:-2])
+
+
+def test_replays_and_streams(b):
+    cases = [Case(40, 205, 16, BF, 1.0, True), Case(6, 40000, 20, BF, 1.0, False)]
+    want = [c.run(b, "both") for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    graphs, outs = [], []
+    for c, s in zip(cases, streams):
+        a, loss, dS, graph = c.device(), torch.zeros(c.T, device="cuda"), rows_of(c.T, c.V, BF, 0.0), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            b.distill_topk_fwd_bwd(c.S, *a, loss, dS)
+        graphs.append(graph), outs.append((loss, dS, a))
+    for _ in range(10):
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (loss, dS, _), (l, d) in zip(outs, want):
+        assert torch.equal(loss, l) and torch.equal(dS, d)

@@ -8,9 +8,15 @@
 // where p_rest is the student's mass outside L.  Gradient: c (p_v - q_v) on L and c (p_v - r p_v / p_rest) outside it.
 //
 // The sums outside L are taken over the words outside L, not as one minus the rest: a student that agrees with its teacher leaves a
-// tail of 1e-3 there, which a difference of sums near one holds to four digits.  A bit per word says which are listed; a repeated
-// index shows as a bit that is already set.  Everything is held in units of log 2, relative to the largest value of its own set, so
-// nothing overflows and a tail far below the list keeps its digits.  Sums in fp32, in a fixed order.
+// tail of 1e-3 there, which a difference of sums near one holds to four digits.  A bit per word says which are listed (a repeated
+// index shows as a bit that is already set); listed words become -inf where the row is held, so that the two passes over
+// it know nothing of the list, and the K entries of the gradient are written over the zeros they leave.  Exponentials are powers of two
+// relative to the largest value of their own set: nothing overflows, and a tail far below the list keeps its digits.  Sums of
+// the vocabulary in fp32, of the slots in fp64 (1 - sum q cancels, and so do the two logarithms of a term), all in a fixed order.
+//
+// Bound: HBM.  Loss and gradient need one read and one write of the logits, so a row is read once and held in registers, 16-byte pieces
+// dealt out over the G threads of a part: a warp per row for small vocabularies, a block, or a cluster of up to eight blocks that
+// exchange the maximum and sum of their parts through distributed shared memory.  Rows too wide for eight blocks are read twice.
 #pragma once
 #include "common.cuh"
 
@@ -19,65 +25,460 @@ namespace distill {
 
 constexpr int kMaxSlots = 1024;
 constexpr int kMaxVocab = 1 << 20;        // a bit per word in shared memory: 128 KB
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr double kLn2d = 0.6931471805599453;
 
 enum { FWD = 1, BWD = 2, BOTH = 3 };
 
 struct Args {
-  const void* S; int64_t lds; int V;
+  const void* S; int64_t lds; int T, V;
   const float* t_logits; int64_t ldt; const int32_t* t_idx; int64_t ldi; int K;
   const float* t_lse; const float* weight;       // nullable
-  float inv_tau, c;                              // 1 / temperature, log2(e) / temperature
+  float inv_tau, c; double inv_tau_d;            // 1 / temperature, log2(e) / temperature
   float* loss; float* stats;                     // FWD, BOTH (stats nullable)
   const float* stats_in; const float* dloss;     // BWD (dloss nullable)
   void* dS; int64_t ldds;                        // BWD, BOTH
   int vec;                                       // rows of S and dS start on 16 bytes
+  int parts, part_pieces;                        // blocks per row (a cluster, but for BWD), pieces of each
 };
 
-constexpr int kThreads = 256;
+__host__ __device__ constexpr int warps_of(int g) { return g / 32; }
+// shared memory of one part: a bit per word in whole 16 bytes, three values per slot
+__host__ __device__ inline size_t part_smem(int V, int K) { return (size_t)((V + 127) / 128) * 16 + (size_t)((3 * K + 3) / 4) * 16; }
 
-// Value over the block, the warps' results joined in warp order; every thread gets it.  `red`: 32 floats.
-template <typename F>
-__device__ __forceinline__ float block_reduce(float v, float* red, F f) {
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// e^x to the last bit or two of fp32, for the few values whose error would be seen in the loss
+__device__ __forceinline__ float exp_of(double x) {
+  const float hi = (float)x, e = expf(hi);
+  return fabsf(hi) < 200.f ? e * (1.f + (float)(x - (double)hi)) : e;       // (no correction where it is infinite)
+}
+__device__ __forceinline__ float pow2_of(float x) { return exp_of((double)x * kLn2d); }
+// log2 with the error of the fraction's logarithm: the exponent is added in fp64
+__device__ __forceinline__ double log2_of(float x) {
+  int e;
+  const float f = frexpf(x, &e);
+  return (double)log2f(f) + (double)e;
+}
+// log r, r = 1 - a
+__device__ __forceinline__ double log_left(double a, float r) { return a < 0.5 ? (double)log1pf(-(float)a) : (double)logf(r); }
+// log of the student's mass outside the list: the sum s there (relative to 2^m_rest) against the sum `top` on it (relative to 2^mc), l2a the log2 of both.
+// Near zero as log1p: a difference of two logarithms of sums would be off by 1e-7 where the loss is 0.01.
+__device__ __forceinline__ double log_share(float s, float m_rest, float mc, float top, double l2a) {
+  const float rest = s * pow2_of(m_rest - mc);
+  if (rest > 1e-30f && top < 1e30f) return rest >= top ? -(double)log1pf(top / rest) : (double)logf(rest / (rest + top));
+  return ((double)m_rest - (double)mc + log2_of(s) - l2a) * kLn2d;
+}
+__device__ __forceinline__ float nan_max(float a, float b) { return a != a || a > b ? a : b; }
+template <typename V, typename F>
+__device__ __forceinline__ V warp_all(V v, F f) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-  for (int w = 1; w < (int)blockDim.x / 32; ++w) v = f(v, red[w]);
   return v;
 }
-__device__ __forceinline__ float fadd(float a, float b) { return a + b; }
-__device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float nan_max(float a, float b) { return a != a || a > b ? a : b; }
+template <typename V> __device__ __forceinline__ V add(V a, V b) { return a + b; }
+__device__ __forceinline__ float max2(float a, float b) { return fmaxf(a, b); }
 
-template <typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) row_kernel(const Args a) {
+// ---- pieces of a row: 16 bytes, -inf where the row has ended
+template <typename T> constexpr int kPer = 16 / (int)sizeof(T);
+template <typename T> __device__ __forceinline__ uint32_t neg_inf_word();
+template <> __device__ __forceinline__ uint32_t neg_inf_word<float>() { return 0xff800000u; }
+template <> __device__ __forceinline__ uint32_t neg_inf_word<__nv_bfloat16>() { return 0xff80ff80u; }
+
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T* row, int piece, int V, int vec) {
+  const int at = piece * kPer<T>;
+  if (vec && at + kPer<T> <= V) return __ldcs(reinterpret_cast<const uint4*>(row + at));
+  uint4 v = make_uint4(neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>());
+  T* h = reinterpret_cast<T*>(&v);
+#pragma unroll
+  for (int e = 0; e < kPer<T>; ++e)
+    if (at + e < V) h[e] = row[at + e];
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* row, int piece, int V, int vec, uint4 v) {
+  const int at = piece * kPer<T>;
+  if (vec && at + kPer<T> <= V) { __stcs(reinterpret_cast<uint4*>(row + at), v); return; }
+  const T* h = reinterpret_cast<const T*>(&v);
+#pragma unroll
+  for (int e = 0; e < kPer<T>; ++e)
+    if (at + e < V) row[at + e] = h[e];
+}
+// which elements of a piece are listed
+template <typename T>
+__device__ __forceinline__ uint32_t listed_of(const uint32_t* bits, int piece) {
+  const uint8_t* bytes = reinterpret_cast<const uint8_t*>(bits);
+  if (kPer<T> == 8) return bytes[piece];
+  return (bytes[piece >> 1] >> (4 * (piece & 1))) & 15u;
+}
+template <typename T>
+__device__ __forceinline__ void hide(uint4& v, uint32_t listed) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) {
+      if (listed >> i & 1u) w[i] = 0xff800000u;
+    } else {
+      if (listed >> (2 * i) & 1u) w[i] = (w[i] & 0xffff0000u) | 0xff80u;
+      if (listed >> (2 * i + 1) & 1u) w[i] = (w[i] & 0xffffu) | 0xff800000u;
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ float piece_max(uint4 v) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+  if (sizeof(T) == 4) return fmaxf(fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])), fmaxf(__uint_as_float(w[2]), __uint_as_float(w[3])));
+  auto h = [&](int i) { return *reinterpret_cast<const __nv_bfloat162*>(&w[i]); };
+  const __nv_bfloat162 m = __hmax2(__hmax2(h(0), h(1)), __hmax2(h(2), h(3)));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+// element e (compile-time after unrolling) in fp32
+template <typename T>
+__device__ __forceinline__ float elem(const uint4& v, int e) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+  if (sizeof(T) == 4) return __uint_as_float(w[e]);
+  return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+}
+template <typename T>
+__device__ __forceinline__ float piece_sum(const uint4& v, float c, float m) {
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < kPer<T>; ++e) s += ex2(fmaf(elem<T>(v, e), c, -m));
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ uint4 piece_grad(const uint4& v, float c, float m, float scale) {
+  uint4 o;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) {
+      w[i] = __float_as_uint(scale * ex2(fmaf(elem<T>(v, i), c, -m)));
+    } else {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(scale * ex2(fmaf(elem<T>(v, 2 * i), c, -m)), scale * ex2(fmaf(elem<T>(v, 2 * i + 1), c, -m)));
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  return o;
+}
+
+// ---- cluster
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void store_peer(const void* local, uint32_t rank, float a, float b) {
+  uint32_t addr = (uint32_t)__cvta_generic_to_shared(local), peer;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(addr), "r"(rank));
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(peer), "f"(a), "f"(b) : "memory");
+}
+
+// One part of one row, held in registers: G threads, P pieces of 16 bytes each.
+template <typename T, int MODE, int G, int P>
+__global__ void __launch_bounds__(G == 32 ? 256 : G) part_kernel(const Args a) {
+  constexpr int NW = warps_of(G), kGroups = G == 32 ? 8 : 1;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float red[32];
-  __shared__ int s_dup;
-  const int words = (a.V + 31) / 32;
-  uint32_t* bits = reinterpret_cast<uint32_t*>(smem);
-  int* slot_idx = reinterpret_cast<int*>(bits + words);
-  float* slot_t = reinterpret_cast<float*>(slot_idx + a.K);      // teacher's logit, then q
-  float* slot_x = slot_t + a.K;                                  // student's logit
-  const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x;
+  struct First { float t, n, x, m, s; };                // largest t, number of listed words, largest listed logit; maximum and sum outside the list
+  struct Second { double a, kl; float top; };           // sum of the teacher's exponentials, of the terms, of the student's on the list
+  __shared__ First first[NW];
+  __shared__ Second second[NW];
+  __shared__ float2 peer[8];
+  __shared__ int s_dup[kGroups];
+  const int group = G == 32 ? threadIdx.x >> 5 : 0, tid = G == 32 ? threadIdx.x & 31 : threadIdx.x;
+  const int lane = threadIdx.x & 31, warp = G == 32 ? 0 : threadIdx.x >> 5;
+  const int64_t row = G == 32 ? (int64_t)blockIdx.x * kGroups + group : blockIdx.x / a.parts;
+  const int part = G == 32 ? 0 : (int)(blockIdx.x % a.parts);
+  const bool cluster = (MODE & FWD) && G != 32 && a.parts > 1;
+  if (cluster) cluster_arrive();                        // completed before the first store to a peer: all of them run
+  auto sync = [&] { if (G == 32) __syncwarp(); else __syncthreads(); };
+  const int words4 = (a.V + 127) / 128;
+  unsigned char* mine = smem + (size_t)group * part_smem(a.V, a.K);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(mine);
+  int* slot_idx = reinterpret_cast<int*>(mine + (size_t)words4 * 16);
+  float* slot_t = reinterpret_cast<float*>(slot_idx + a.K);
+  float* slot_x = slot_t + a.K;
+  for (int i = tid; i < words4; i += G) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) s_dup[group] = 0;
+  sync();
   pdl_wait();
   pdl_launch_dependents();
+  if (G == 32 && row >= a.T) return;
   const T* S = reinterpret_cast<const T*>(a.S) + row * a.lds;
   T* dS = MODE == FWD ? nullptr : reinterpret_cast<T*>(a.dS) + row * a.ldds;
+  const int all_pieces = (a.V + kPer<T> - 1) / kPer<T>;
+  const int lo = part * a.part_pieces, hi = min(lo + a.part_pieces, all_pieces);
   const float w = a.weight ? a.weight[row] : 1.f;
   float g = w * a.inv_tau;
   if (MODE == BWD && a.dloss) g = a.dloss[row] * g;
   bool off = MODE == BWD ? g == 0.f : w == 0.f;
-  for (int i = tid; i < words; i += kThreads) bits[i] = 0;
+  uint4 d[P];
+  auto load = [&] {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = lo + i * G + tid;
+      d[i] = p < hi ? load_piece<T>(S, p, a.V, a.vec) : make_uint4(neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>());
+    }
+  };
+  auto hide_listed = [&] {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = lo + i * G + tid;
+      const uint32_t listed = p < hi ? listed_of<T>(bits, p) : 0u;
+      if (listed) hide<T>(d[i], listed);
+    }
+  };
+  First f{-INFINITY, 0.f, -INFINITY, -INFINITY, 0.f};
+  if (!off) {
+    load();                                             // in flight while the list is read
+    for (int j = tid; j < a.K; j += G) {
+      int idx = a.t_idx[row * a.ldi + j];
+      if (idx < 0 || idx >= a.V) idx = -1;
+      slot_idx[j] = idx;
+      if (idx < 0) continue;
+      if (atomicOr(&bits[idx >> 5], 1u << (idx & 31)) >> (idx & 31) & 1u) s_dup[group] = 1;
+      slot_t[j] = a.t_logits[row * a.ldt + j];
+      // the backward call's parts are not ordered against one another: in place, another one's words may be gone already
+      const int at = idx / kPer<T>;
+      if (MODE != BWD || (at >= lo && at < hi)) slot_x[j] = to_f32(S[idx]);
+    }
+    sync();
+    if (s_dup[group]) {                                 // rare: the first of equal indices stays
+      uint32_t drop = 0;
+      for (int j = tid, n = 0; j < a.K; j += G, ++n)
+        if (slot_idx[j] >= 0)
+          for (int i = 0; i < j; ++i)
+            if (slot_idx[i] == slot_idx[j]) { drop |= 1u << n; break; }
+      sync();
+      for (int j = tid, n = 0; j < a.K; j += G, ++n)
+        if (drop >> n & 1u) slot_idx[j] = -1;
+      sync();
+    }
+    for (int j = tid; j < a.K; j += G)
+      if (slot_idx[j] >= 0) {
+        f.t = nan_max(f.t, slot_t[j]);
+        f.n += 1.f;
+        if (MODE & FWD) f.x = fmaxf(f.x, slot_x[j]);
+      }
+    f.t = warp_all(f.t, nan_max);
+    f.n = warp_all(f.n, add<float>);
+    if (MODE & FWD) {
+      f.x = warp_all(f.x, max2);
+      hide_listed();
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < P; ++i) m = fmaxf(m, piece_max<T>(d[i]));
+      f.m = warp_all(m, max2);
+      const float ref = f.m == -INFINITY ? 0.f : __fmul_rn(f.m, a.c);
+#pragma unroll
+      for (int i = 0; i < P; ++i) f.s += piece_sum<T>(d[i], a.c, ref);
+      f.s = warp_all(f.s, add<float>);
+    } else {
+      hide_listed();
+    }
+    if (NW > 1) {
+      if (lane == 0) first[warp] = f;
+      sync();
+      First o = lane < NW ? first[lane] : First{-INFINITY, 0.f, -INFINITY, -INFINITY, 0.f};
+      f.t = warp_all(o.t, nan_max);
+      f.n = warp_all(o.n, add<float>);
+      f.x = warp_all(o.x, max2);
+      f.m = warp_all(o.m, max2);
+      f.s = warp_all(o.m == -INFINITY ? o.s : o.s * pow2_of(__fmul_rn(o.m, a.c) - __fmul_rn(f.m, a.c)), add<float>);
+    }
+    if (cluster) {
+      cluster_wait();
+      if (threadIdx.x < a.parts) store_peer(&peer[part], threadIdx.x, f.m, f.s);
+      __syncwarp();
+      cluster_arrive();
+      cluster_wait();
+      float2 o = lane < a.parts ? peer[lane] : make_float2(-INFINITY, 0.f);
+      f.m = warp_all(o.x, max2);
+      f.s = warp_all(o.x == -INFINITY ? o.y : o.y * pow2_of(__fmul_rn(o.x, a.c) - __fmul_rn(f.m, a.c)), add<float>);
+    }
+    off = f.n == 0.f || (!a.t_lse && f.t == -INFINITY);  // an empty list, or one that gives every word nothing
+  } else if (cluster) {
+    cluster_wait();
+  }
+  if (off) {
+    if ((MODE & FWD) && part == 0 && tid == 0) {
+      a.loss[row] = 0.f;
+      if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
+    }
+    if (MODE & BWD)
+      for (int p = lo + tid; p < hi; p += G) store_piece<T>(dS, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
+    return;
+  }
+  // the student's references in units of log 2: largest logit of all, largest outside the list
+  float mc, l2all = 0.f, m_rest, l2rest;
+  if (MODE & FWD) {
+    m_rest = f.m == -INFINITY ? 0.f : __fmul_rn(f.m, a.c);
+    mc = __fmul_rn(fmaxf(f.m, f.x), a.c);
+    l2rest = log2f(f.s);
+  } else {
+    const float* o = a.stats_in + 4 * row;
+    mc = o[0]; l2all = o[1]; m_rest = o[2]; l2rest = o[3];
+  }
+  // the slots: log q (up to the list's own normaliser without t_lse), q, and what they add to the sums
+  const double t_ref = a.t_lse ? (double)a.t_lse[row] : (double)f.t * a.inv_tau_d;
+  Second h{0.0, 0.0, 0.f};
+  for (int j = tid; j < a.K; j += G) {
+    if (slot_idx[j] < 0) continue;
+    const double lq = (double)slot_t[j] * a.inv_tau_d - t_ref;
+    const float q = exp_of(lq);
+    slot_t[j] = q;
+    h.a += (double)q;
+    if (MODE & FWD) {
+      // relative to the rounded reference that the sums are relative to
+      const double lx = ((double)slot_x[j] * (double)a.c - (double)mc) * kLn2d;
+      h.top += exp_of(lx);
+      if (!(q <= 0.f)) h.kl += (double)q * (lq - lx);
+    }
+  }
+  h.a = warp_all(h.a, add<double>);
+  if (MODE & FWD) { h.kl = warp_all(h.kl, add<double>); h.top = warp_all(h.top, add<float>); }
+  if (NW > 1) {
+    if (lane == 0) second[warp] = h;
+    sync();
+    Second o = lane < NW ? second[lane] : Second{0.0, 0.0, 0.f};
+    h.a = warp_all(o.a, add<double>);
+    if (MODE & FWD) { h.kl = warp_all(o.kl, add<double>); h.top = warp_all(o.top, add<float>); }
+  }
+  const float r = a.t_lse && f.n < (float)a.V ? (float)fmax(0.0, 1.0 - h.a) : 0.f;
+  const float q_norm = a.t_lse ? 1.f : (float)(1.0 / h.a);
+  if (MODE & FWD) {
+    const double l2a = log2_of(h.top + (f.s > 0.f ? f.s * pow2_of(m_rest - mc) : f.s));
+    l2all = (float)l2a;
+    if (part == 0 && tid == 0) {
+      double kl = h.kl + (a.t_lse ? h.a : 0.0) * l2a * kLn2d;
+      if (!a.t_lse) kl = h.kl / h.a - log2_of((float)h.a) * kLn2d + l2a * kLn2d;
+      if (r > 0.f) kl += (double)r * (log_left(h.a, r) - log_share(f.s, m_rest, mc, h.top, l2a));
+      a.loss[row] = w * (float)kl;
+      if (a.stats) { float* o = a.stats + 4 * row; o[0] = mc; o[1] = l2all; o[2] = m_rest; o[3] = l2rest; }
+    }
+  }
+  if (MODE & BWD) {
+    // outside the list: 2^(x - m_rest) times what is common to the row
+    const float pull = l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - mc - l2all) - r * ex2(-l2rest));
+    // keeps the compiler from holding the row unpacked across the reductions (123 registers instead of 80)
+#pragma unroll
+    for (int i = 0; i < P; ++i) asm volatile("" : "+r"(d[i].x), "+r"(d[i].y), "+r"(d[i].z), "+r"(d[i].w));
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = lo + i * G + tid;
+      if (p < hi) store_piece<T>(dS, p, a.V, a.vec, piece_grad<T>(d[i], a.c, m_rest, pull));
+    }
+    sync();                                             // the zeros of the listed words are written
+    for (int j = tid; j < a.K; j += G) {
+      const int idx = slot_idx[j], at = idx / kPer<T>;
+      if (idx >= 0 && at >= lo && at < hi) dS[idx] = from_f32<T>(g * (ex2(fmaf(slot_x[j], a.c, -mc) - l2all) - slot_t[j] * q_norm));
+    }
+  }
+}
+
+// ---- rows that one block of G threads walks, persistent over the rows.  Every thread copies its own 16-byte pieces to its own places in
+// shared memory, N pieces ahead, and waits for nobody to read them: the copies run on through the reductions and across rows.
+// RES (loss and gradient): the row fits the N places of every thread; the second pass finds it there, and as each place is read for the last
+// time the next row's piece is asked for.  Otherwise the places are a ring of batches, and a row that needs two passes is read twice, the
+// second time from L2.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <typename T>
+__device__ __forceinline__ void copy_piece(uint32_t dst, const T* row, int piece, int V, int vec) {
+  const int at = piece * kPer<T>, left = (V - at) * (int)sizeof(T);
+  if (vec) { copy16(dst, row + at, min(left, 16)); return; }      // (what lies behind the row is hidden with the listed words)
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (4 * e < left) copy4(dst + 4 * e, reinterpret_cast<const float*>(row) + at + e);
+}
+
+constexpr int kPlaces = 12, kBatch = 4;
+__host__ __device__ inline size_t row_smem(int g, int V, int K) { return (size_t)kPlaces * g * 16 + part_smem(V + 8, K); }
+
+template <typename T, int MODE, int G, bool RES>
+__global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
+  constexpr int NW = warps_of(G), N = kPlaces;
+  static_assert(!RES || MODE == BOTH, "one pass keeps nothing");
+  extern __shared__ __align__(16) unsigned char smem[];
+  struct First { float t, n, x, m, s; };
+  struct Second { double a, kl; float top; };
+  __shared__ First first[NW];
+  __shared__ Second second[NW];
+  __shared__ int s_dup;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint4* tile = reinterpret_cast<uint4*>(smem) + tid;                    // place i of this thread: tile[i * G]
+  const uint32_t tile_addr = (uint32_t)__cvta_generic_to_shared(tile);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(smem + (size_t)N * G * 16);
+  const int words4 = (a.V + 8 + 127) / 128, pieces = (a.V + kPer<T> - 1) / kPer<T>;
+  int* slot_idx = reinterpret_cast<int*>(bits + 4 * words4);
+  float* slot_t = reinterpret_cast<float*>(slot_idx + a.K);
+  float* slot_x = slot_t + a.K;
+  for (int i = tid; i < words4; i += G) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
   if (tid == 0) s_dup = 0;
   __syncthreads();
-  float mt = -INFINITY, n_listed = 0.f;
-  if (!off) {
-    for (int j = tid; j < a.K; j += kThreads) {
+  if (tid < 8 && a.V + tid < pieces * kPer<T>) atomicOr(&bits[(a.V + tid) >> 5], 1u << ((a.V + tid) & 31));
+  pdl_wait();
+  pdl_launch_dependents();
+  const T* S0 = reinterpret_cast<const T*>(a.S);
+  T* dS0 = reinterpret_cast<T*>(a.dS);
+  auto factor = [&](int64_t row) {                                       // what decides whether a row is looked at
+    float g = a.weight ? a.weight[row] : 1.f;
+    if (MODE == BWD && a.dloss) g *= a.dloss[row];
+    return g;
+  };
+  auto nothing = [&](int64_t row) {
+    if ((MODE & FWD) && tid == 0) {
+      a.loss[row] = 0.f;
+      if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
+    }
+    if (MODE & BWD)
+      for (int p = tid; p < pieces; p += G) store_piece<T>(dS0 + row * a.ldds, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
+  };
+  auto active_from = [&](int64_t row, bool write) {                      // the next row of this block that is looked at
+    while (row < a.T && factor(row) == 0.f) { if (write) nothing(row); row += gridDim.x; }
+    return row;
+  };
+  const int batches = (pieces + G * kBatch - 1) / (G * kBatch), passes = MODE == BOTH && !RES ? 2 : 1;
+  // the copies' own position: row, pass, batch (ring) -- one commit per batch or place, whether it copies or not
+  int64_t row = active_from(blockIdx.x, true), ahead = row;
+  int ahead_batch = 0, ring_in = 0, ring_out = 0;
+  auto copy_batch = [&]() {
+    if (ahead < a.T) {
+      const T* S = S0 + ahead * a.lds;
+      const int b = ahead_batch >= batches ? ahead_batch - batches : ahead_batch;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int p = (b * kBatch + i) * G + tid;
+        if (p < pieces) copy_piece<T>(tile_addr + (uint32_t)((ring_in * kBatch + i) * G * 16), S, p, a.V, a.vec);
+      }
+      if (++ahead_batch == passes * batches) { ahead_batch = 0; ahead = active_from(ahead + gridDim.x, false); }
+    }
+    if (++ring_in == N / kBatch) ring_in = 0;
+    copies_commit();
+  };
+  auto copy_place = [&](int i, int64_t r) {
+    const int p = i * G + tid;
+    if (r < a.T && p < pieces) copy_piece<T>(tile_addr + (uint32_t)(i * G * 16), S0 + r * a.lds, p, a.V, a.vec);
+    copies_commit();
+  };
+  if (RES) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) copy_place(i, row);
+  } else {
+    for (int i = 0; i < N / kBatch; ++i) copy_batch();
+  }
+  while (row < a.T) {
+    const T* S = S0 + row * a.lds;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    float g = w * a.inv_tau;
+    if (MODE == BWD && a.dloss) g = a.dloss[row] * g;
+    __syncthreads();                                                     // the bits of the row before are clear
+    for (int j = tid; j < a.K; j += G) {
       int idx = a.t_idx[row * a.ldi + j];
       if (idx < 0 || idx >= a.V) idx = -1;
       slot_idx[j] = idx;
@@ -87,102 +488,182 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const Args a) {
       slot_x[j] = to_f32(S[idx]);
     }
     __syncthreads();
-    if (s_dup) {            // rare: the first of equal indices stays
+    if (s_dup) {                                                         // rare: the first of equal indices stays
       uint32_t drop = 0;
-      for (int j = tid, n = 0; j < a.K; j += kThreads, ++n)
-        for (int i = 0; i < j; ++i)
-          if (slot_idx[i] == slot_idx[j]) { drop |= 1u << n; break; }
+      for (int j = tid, n = 0; j < a.K; j += G, ++n)
+        if (slot_idx[j] >= 0)
+          for (int i = 0; i < j; ++i)
+            if (slot_idx[i] == slot_idx[j]) { drop |= 1u << n; break; }
       __syncthreads();
-      for (int j = tid, n = 0; j < a.K; j += kThreads, ++n)
+      for (int j = tid, n = 0; j < a.K; j += G, ++n)
         if (drop >> n & 1u) slot_idx[j] = -1;
+      if (tid == 0) s_dup = 0;
       __syncthreads();
     }
-    for (int j = tid; j < a.K; j += kThreads)
-      if (slot_idx[j] >= 0) { mt = nan_max(mt, slot_t[j]); n_listed += 1.f; }
-    mt = block_reduce(mt, red, nan_max);
-    n_listed = block_reduce(n_listed, red, fadd);
-    off = n_listed == 0.f || (!a.t_lse && mt == -INFINITY);      // an empty list, or one that gives every word nothing
-  }
-  if (off) {
-    if (MODE & FWD) {
-      if (tid == 0) {
-        a.loss[row] = 0.f;
-        if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
+    First f{-INFINITY, 0.f, -INFINITY, -INFINITY, 0.f};
+    for (int j = tid; j < a.K; j += G)
+      if (slot_idx[j] >= 0) {
+        f.t = nan_max(f.t, slot_t[j]);
+        f.n += 1.f;
+        if (MODE & FWD) f.x = fmaxf(f.x, slot_x[j]);
+      }
+    // ---- first pass: maximum and sum outside the list, kept relative to the maximum so far
+    float m = -INFINITY, ref = 0.f, s = 0.f;
+    auto take = [&](const uint4& v) {
+      const float mv = piece_max<T>(v);
+      if (mv > m) {
+        const float to = __fmul_rn(mv, a.c);
+        s *= ex2(m == -INFINITY ? -INFINITY : ref - to);
+        m = mv; ref = to;
+      }
+      s += piece_sum<T>(v, a.c, ref);
+    };
+    if (RES) {
+      auto place = [&](int i) {
+        const int p = i * G + tid;
+        if (p < pieces) {
+          uint4 v = tile[i * G];
+          const uint32_t listed = listed_of<T>(bits, p);
+          if (listed) { hide<T>(v, listed); tile[i * G] = v; }
+          take(v);
+        }
+      };
+      copies_wait<N - 4>();
+      place(0); place(1); place(2); place(3);
+      copies_wait<N - 8>();
+      place(4); place(5); place(6); place(7);
+      copies_wait<0>();
+      place(8); place(9); place(10); place(11);
+    } else if (MODE & FWD) {
+      for (int b = 0; b < batches; ++b) {
+        copies_wait<N / kBatch - 1>();
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int p = (b * kBatch + i) * G + tid;
+          if (p < pieces) {
+            uint4 v = tile[(ring_out * kBatch + i) * G];
+            const uint32_t listed = listed_of<T>(bits, p);
+            if (listed) hide<T>(v, listed);
+            take(v);
+          }
+        }
+        if (++ring_out == N / kBatch) ring_out = 0;
+        copy_batch();
       }
     }
-    if (MODE & BWD)
-      for (int v = tid; v < a.V; v += kThreads) dS[v] = from_f32<T>(0.f);
-    return;
-  }
-  // the teacher: log2 q and q of every slot
-  float lt = 0.f;
-  if (!a.t_lse) {
-    float s = 0.f;
-    for (int j = tid; j < a.K; j += kThreads)
-      if (slot_idx[j] >= 0) s += exp2f((slot_t[j] - mt) * a.c);
-    lt = log2f(block_reduce(s, red, fadd));
-  } else {
-    const float lse = a.t_lse[row];
-    mt = 0.f;
-    for (int j = tid; j < a.K; j += kThreads)
-      if (slot_idx[j] >= 0) slot_t[j] = fmaf(slot_t[j], a.inv_tau, -lse);
-  }
-  auto log2q = [&](int j) { return a.t_lse ? slot_t[j] * kLog2e : fmaf(slot_t[j] - mt, a.c, -lt); };
-  float Q = 0.f;
-  for (int j = tid; j < a.K; j += kThreads)
-    if (slot_idx[j] >= 0) Q += exp2f(log2q(j));
-  Q = block_reduce(Q, red, fadd);
-  const float r = a.t_lse && n_listed < (float)a.V ? fmaxf(0.f, 1.f - Q) : 0.f;
-  // the student: largest value and sum of exponentials outside the list and over all words
-  float mc, l2all, m_rest, l2rest;
-  if (MODE & FWD) {
-    float m = -INFINITY, mx = -INFINITY;
-    for (int v = tid; v < a.V; v += kThreads)
-      if (!(bits[v >> 5] >> (v & 31) & 1u)) m = fmaxf(m, to_f32(S[v]));
-    m = block_reduce(m, red, fmax2);
-    m_rest = m == -INFINITY ? 0.f : m * a.c;
-    float s = 0.f;
-    for (int v = tid; v < a.V; v += kThreads)
-      if (!(bits[v >> 5] >> (v & 31) & 1u)) s += exp2f(fmaf(to_f32(S[v]), a.c, -m_rest));
-    s = block_reduce(s, red, fadd);
-    for (int j = tid; j < a.K; j += kThreads)
-      if (slot_idx[j] >= 0) mx = fmaxf(mx, slot_x[j]);
-    mx = fmaxf(m, block_reduce(mx, red, fmax2));
-    mc = mx * a.c;
-    float st = 0.f;
-    for (int j = tid; j < a.K; j += kThreads)
-      if (slot_idx[j] >= 0) st += exp2f(fmaf(slot_x[j], a.c, -mc));
-    st = block_reduce(st, red, fadd);
-    l2rest = log2f(s);
-    l2all = log2f(st + (s > 0.f ? s * exp2f(m_rest - mc) : s));
-    float kl = 0.f;
-    for (int j = tid; j < a.K; j += kThreads) {
+    f.m = m; f.s = s;
+    // ---- over the block
+    f.t = warp_all(f.t, nan_max);
+    f.n = warp_all(f.n, add<float>);
+    if (MODE & FWD) {
+      f.x = warp_all(f.x, max2);
+      f.m = warp_all(m, max2);
+      f.s = warp_all(m == -INFINITY ? s : s * ex2(ref - __fmul_rn(f.m, a.c)), add<float>);
+    }
+    if (lane == 0) first[warp] = f;
+    __syncthreads();
+    {
+      const First o = lane < NW ? first[lane] : First{-INFINITY, 0.f, -INFINITY, -INFINITY, 0.f};
+      f.t = warp_all(o.t, nan_max);
+      f.n = warp_all(o.n, add<float>);
+      if (MODE & FWD) {
+        f.x = warp_all(o.x, max2);
+        f.m = warp_all(o.m, max2);
+        f.s = warp_all(o.m == -INFINITY ? o.s : o.s * pow2_of(__fmul_rn(o.m, a.c) - __fmul_rn(f.m, a.c)), add<float>);
+      }
+    }
+    const bool empty = f.n == 0.f || (!a.t_lse && f.t == -INFINITY);     // an empty list, or one that gives every word nothing
+    float mc, l2all = 0.f, m_rest, l2rest;
+    if (MODE & FWD) {
+      m_rest = f.m == -INFINITY ? 0.f : __fmul_rn(f.m, a.c);
+      mc = __fmul_rn(fmaxf(f.m, f.x), a.c);
+      l2rest = log2f(f.s);
+    } else {
+      const float* o = a.stats_in + 4 * row;
+      mc = o[0]; l2all = o[1]; m_rest = o[2]; l2rest = o[3];
+    }
+    const double t_ref = a.t_lse ? (double)a.t_lse[row] : (double)f.t * a.inv_tau_d;
+    Second h{0.0, 0.0, 0.f};
+    for (int j = tid; j < a.K; j += G) {
       if (slot_idx[j] < 0) continue;
-      const float lq = log2q(j), q = exp2f(lq);
-      if (!(q <= 0.f)) kl += q * (lq - (fmaf(slot_x[j], a.c, -mc) - l2all));
+      const double lq = (double)slot_t[j] * a.inv_tau_d - t_ref;
+      const float q = exp_of(lq);
+      slot_t[j] = q;
+      h.a += (double)q;
+      if (MODE & FWD) {
+        const double lx = ((double)slot_x[j] * (double)a.c - (double)mc) * kLn2d;
+        h.top += exp_of(lx);
+        if (!(q <= 0.f)) h.kl += (double)q * (lq - lx);
+      }
     }
-    kl = block_reduce(kl, red, fadd);
-    if (r > 0.f) kl += r * (log2f(r) - (m_rest - mc + l2rest - l2all));
-    if (tid == 0) {
-      a.loss[row] = w * (kl * kLn2);
-      if (a.stats) { float* o = a.stats + 4 * row; o[0] = mc; o[1] = l2all; o[2] = m_rest; o[3] = l2rest; }
+    if (a.K > 32 * warp) {                                               // (the other warps have no slot)
+      h.a = warp_all(h.a, add<double>);
+      if (MODE & FWD) { h.kl = warp_all(h.kl, add<double>); h.top = warp_all(h.top, add<float>); }
     }
-  } else {
-    const float* o = a.stats_in + 4 * row;
-    mc = o[0]; l2all = o[1]; m_rest = o[2]; l2rest = o[3];
+    if (lane == 0) second[warp] = h;
+    __syncthreads();
+    {
+      const Second o = lane < NW ? second[lane] : Second{0.0, 0.0, 0.f};
+      h.a = warp_all(o.a, add<double>);
+      if (MODE & FWD) { h.kl = warp_all(o.kl, add<double>); h.top = warp_all(o.top, add<float>); }
+    }
+    const float r = a.t_lse && f.n < (float)a.V ? (float)fmax(0.0, 1.0 - h.a) : 0.f;
+    const float q_norm = a.t_lse ? 1.f : (float)(1.0 / h.a);
+    if (MODE & FWD) {
+      const double l2a = log2_of(h.top + (f.s > 0.f ? f.s * pow2_of(m_rest - mc) : f.s));
+      l2all = (float)l2a;
+      if (tid == 0) {
+        double kl = h.kl + (a.t_lse ? h.a : 0.0) * l2a * kLn2d;
+        if (!a.t_lse) kl = h.kl / h.a - log2_of((float)h.a) * kLn2d + l2a * kLn2d;
+        if (r > 0.f) kl += (double)r * (log_left(h.a, r) - log_share(f.s, m_rest, mc, h.top, l2a));
+        a.loss[row] = empty ? 0.f : w * (float)kl;
+        if (a.stats) { float* o = a.stats + 4 * row; o[0] = mc; o[1] = l2all; o[2] = m_rest; o[3] = l2rest; }
+      }
+    }
+    // ---- second pass: the gradient
+    const int64_t next = RES ? active_from(row + gridDim.x, true) : 0;
+    if (MODE & BWD) {
+      T* dS = dS0 + row * a.ldds;
+      const float pull = l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - mc - l2all) - r * ex2(-l2rest));
+      if (RES) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int p = i * G + tid;
+          if (p < pieces) {
+            uint4 o = piece_grad<T>(tile[i * G], a.c, m_rest, pull);
+            if (empty) o = make_uint4(0, 0, 0, 0);
+            store_piece<T>(dS, p, a.V, a.vec, o);
+          }
+          copy_place(i, next);
+        }
+      } else {
+        for (int b = 0; b < batches; ++b) {
+          copies_wait<N / kBatch - 1>();
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int p = (b * kBatch + i) * G + tid;
+            if (p < pieces) {
+              uint4 v = tile[(ring_out * kBatch + i) * G];
+              const uint32_t listed = listed_of<T>(bits, p);
+              if (listed) hide<T>(v, listed);
+              v = piece_grad<T>(v, a.c, m_rest, pull);
+              if (empty) v = make_uint4(0, 0, 0, 0);
+              store_piece<T>(dS, p, a.V, a.vec, v);
+            }
+          }
+          if (++ring_out == N / kBatch) ring_out = 0;
+          copy_batch();
+        }
+      }
+      __syncthreads();                                                   // the zeros of the listed words are written
+      for (int j = tid; j < a.K; j += G)
+        if (slot_idx[j] >= 0 && !empty) dS[slot_idx[j]] = from_f32<T>(g * (ex2(fmaf(slot_x[j], a.c, -mc) - l2all) - slot_t[j] * q_norm));
+    }
+    for (int j = tid; j < a.K; j += G)
+      if (slot_idx[j] >= 0) atomicAnd(&bits[slot_idx[j] >> 5], ~(1u << (slot_idx[j] & 31)));
+    row = RES ? next : active_from(row + gridDim.x, true);
   }
-  if (MODE & BWD) {
-    // outside the list: 2^(x - m_rest) times what is common to the row
-    const float pull = l2rest == -INFINITY ? 0.f : g * (exp2f(m_rest - mc - l2all) - r * exp2f(-l2rest));
-    for (int v = tid; v < a.V; v += kThreads) {
-      if (bits[v >> 5] >> (v & 31) & 1u) continue;
-      dS[v] = from_f32<T>(pull * exp2f(fmaf(to_f32(S[v]), a.c, -m_rest)));
-    }
-    for (int j = tid; j < a.K; j += kThreads) {
-      if (slot_idx[j] < 0) continue;
-      dS[slot_idx[j]] = from_f32<T>(g * (exp2f(fmaf(slot_x[j], a.c, -mc) - l2all) - exp2f(log2q(j))));
-    }
-  }
+  copies_wait<0>();
 }
 
 }  // namespace distill

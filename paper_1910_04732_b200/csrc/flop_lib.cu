@@ -1253,16 +1253,68 @@ int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int
 }
 
 // ---- distillation from top logits
-template <typename T, int MODE>
-int launch_distill_inst(const distill::Args& a, int64_t rows, cudaStream_t st) {
+template <typename T, int MODE, int G, int P>
+int launch_distill_part(const distill::Args& a, int parts, cudaStream_t st) {
   static OncePerDevice configured;
-  auto kern = distill::row_kernel<T, MODE>;
-  FLOP_TRY(allow_smem(configured, distill::kMaxVocab / 8 + 12 * distill::kMaxSlots, kern));
-  const size_t smem = (size_t)(a.V + 31) / 32 * 4 + (size_t)12 * a.K;
-  launch_k(kern, dim3((unsigned)rows), dim3(distill::kThreads), smem, st, a);
+  constexpr int rows_per_block = G == 32 ? 8 : 1;
+  auto kern = distill::part_kernel<T, MODE, G, P>;
+  const size_t smem = rows_per_block * distill::part_smem(a.V, a.K);
+  FLOP_TRY(allow_smem(configured, G == 32 ? 8 * distill::part_smem(2048, distill::kMaxSlots) : distill::part_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
+  distill::Args b = a;
+  const int pieces = (a.V + distill::kPer<T> - 1) / distill::kPer<T>;
+  b.parts = parts;
+  b.part_pieces = (pieces + parts - 1) / parts;
+  cudaLaunchConfig_t cfg{};
+  const int64_t blocks = G == 32 ? ((int64_t)a.T + rows_per_block - 1) / rows_per_block : (int64_t)a.T * parts;
+  if (blocks > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(G == 32 ? 256 : G); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = pdl_on() ? 1 : 0;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)parts; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = (MODE & distill::FWD) && G != 32 && parts > 1 ? 2 : 1;
+  cudaLaunchKernelEx(&cfg, kern, b);
   count_launch();
   FLOP_CUDA(cudaGetLastError());
   return FLOP_OK;
+}
+template <typename T, int MODE, int G, bool RES>
+int launch_distill_row(const distill::Args& a, cudaStream_t st) {
+  static OncePerDevice configured;
+  auto kern = distill::row_kernel<T, MODE, G, RES>;
+  FLOP_TRY(allow_smem(configured, kSmemBudget, kern));
+  const size_t smem = distill::row_smem(G, a.V, a.K);
+  const int resident = (int)std::min<size_t>(1024 / G, (size_t)(228 * 1024) / (smem + 2048));
+  launch_k(kern, dim3((unsigned)std::min<int64_t>(a.T, (int64_t)num_sms() * std::max(resident, 1))), dim3(G), smem, st, a);
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
+}
+template <typename T, int MODE>
+int launch_distill_inst(const distill::Args& a, cudaStream_t st) {
+  const int64_t pieces = (a.V + distill::kPer<T> - 1) / distill::kPer<T>;
+  if (pieces <= 32) return launch_distill_part<T, MODE, 32, 1>(a, 1, st);
+  if (pieces <= 64) return launch_distill_part<T, MODE, 32, 2>(a, 1, st);
+  if (pieces <= 128) return launch_distill_part<T, MODE, 32, 4>(a, 1, st);
+  if (pieces <= 256) return launch_distill_part<T, MODE, 32, 8>(a, 1, st);
+  if (a.T <= num_sms() / 2 && pieces <= 32768) {
+    int parts = 1;
+    while (parts < 8 && (pieces > (int64_t)parts * 2048 || (int64_t)a.T * parts * 2 <= num_sms())) parts *= 2;
+    if (pieces <= (int64_t)parts * 1024) return launch_distill_part<T, MODE, 256, 4>(a, parts, st);
+    if (pieces <= (int64_t)parts * 2048) return launch_distill_part<T, MODE, 256, 8>(a, parts, st);
+    return launch_distill_part<T, MODE, 512, 8>(a, parts, st);
+  }
+  if constexpr (MODE == distill::BOTH) {
+    if (pieces <= distill::kPlaces * 128) return launch_distill_row<T, MODE, 128, true>(a, st);
+    if (pieces <= distill::kPlaces * 256) return launch_distill_row<T, MODE, 256, true>(a, st);
+    if (pieces <= distill::kPlaces * 512) return launch_distill_row<T, MODE, 512, true>(a, st);
+  } else if (pieces <= 1024) {
+    return launch_distill_row<T, MODE, 128, false>(a, st);
+  }
+  if (pieces <= 4096 || a.V > distill::kMaxVocab / 2) return launch_distill_row<T, MODE, 256, false>(a, st);
+  return launch_distill_row<T, MODE, 512, false>(a, st);
 }
 template <int MODE>
 int distill_impl(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi, int64_t K,
@@ -1280,11 +1332,13 @@ int distill_impl(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const
   // every row is read whole before it is written, so the gradient may take the logits' place; half of it may not
   if ((MODE & distill::BWD) && !(dS == S && ldds == lds) && Span(S, T, V, lds, elt(dt)).meets(Span(dS, T, V, ldds, elt(dt)))) return FLOP_ERR_INVALID_ARG;
   distill::Args a{};
-  a.S = S; a.lds = lds; a.V = (int)V; a.t_logits = t_logits; a.ldt = ldt; a.t_idx = t_idx; a.ldi = ldi; a.K = (int)K; a.t_lse = t_lse; a.weight = weight;
+  a.S = S; a.lds = lds; a.T = (int)T; a.V = (int)V; a.t_logits = t_logits; a.ldt = ldt; a.t_idx = t_idx; a.ldi = ldi; a.K = (int)K; a.t_lse = t_lse; a.weight = weight;
   a.inv_tau = (float)(1.0 / (double)temperature); a.c = (float)(1.4426950408889634 / (double)temperature);
+  a.inv_tau_d = 1.0 / (double)temperature;
+  a.vec = dt == FLOP_BF16 || (aligned16(S) && lds % 4 == 0 && (!(MODE & distill::BWD) || (aligned16(dS) && ldds % 4 == 0)));
   a.loss = loss; a.stats = stats; a.stats_in = stats_in; a.dloss = dloss; a.dS = dS; a.ldds = ldds;
-  if (dt == FLOP_BF16) return launch_distill_inst<bf16, MODE>(a, T, st);
-  return launch_distill_inst<float, MODE>(a, T, st);
+  if (dt == FLOP_BF16) return launch_distill_inst<bf16, MODE>(a, st);
+  return launch_distill_inst<float, MODE>(a, st);
 }
 
 }  // namespace

@@ -43,7 +43,8 @@ class Case:
         n = min(K, V)
         teacher = (g.standard_normal((T, V)) + 10 * g.random((T, V)) ** max(1.0, V / 20)) * spread
         student = 0.8 * teacher + 0.7 * g.standard_normal((T, V)) * spread
-        top = np.argsort(-teacher, axis=1)[:, :n]
+        top = np.argpartition(-teacher, n - 1, axis=1)[:, :n]
+        top = np.take_along_axis(top, np.argsort(np.take_along_axis(-teacher, top, 1), axis=1), 1)
         self.idx = np.full((T, K), -1, np.int32)
         self.t = np.full((T, K), np.nan, np.float32)
         self.idx[:, :n], self.t[:, :n] = top, np.take_along_axis(teacher, top, 1)
@@ -81,14 +82,19 @@ class Case:
             assert torch.all(behind(dS) == -7.0)
         return loss, dS
 
-    def check(self, b, form, in_place=False):
+    def check(self, b, form, in_place=False, rows=None):
         loss, dS = self.run(b, form, in_place)
-        S = self.S.cpu().double().numpy()
-        want, grad, facts = O.distill_topk(S, self.t, self.idx, self.lse, self.weight, self.tau)
+        rows = np.arange(self.T) if rows is None else np.asarray(rows)
+        S = np.zeros((self.T, self.V))
+        S[rows] = self.S[torch.from_numpy(rows).cuda()].cpu().double().numpy()
+        want, grad, facts = np.zeros(self.T), {}, {}
+        for i in rows:
+            want[i], grad[i], facts[i] = O.distill_row(S[i], self.t[i], self.idx[i], None if self.lse is None else float(self.lse[i]),
+                                                       1.0 if self.weight is None else float(self.weight[i]), self.tau)
         got = loss.cpu().double().numpy()
         w = np.ones(self.T) if self.weight is None else self.weight.astype(np.float64)
         up = w / self.tau * (1.0 if self.dloss is None or form != "bwd" else self.dloss)
-        for i, f in enumerate(facts):
+        for i, f in facts.items():
             if f is None:
                 assert got[i] == 0 and (dS is None or not torch.any(dS[i])), i
                 continue
@@ -117,6 +123,28 @@ FORMS = ["fwd", "bwd", "both"]
                                          (2, 2049, 33, 0), (3, 4099, 300, 0), (2, 8200, 64, 0), (3, 16400, 20, 0), (2, 33000, 1024, 0), (1, 50001, 100, 1), (2, 66000, 7, 0)])
 def test_sizes(b, form, dtype, rest, T, V, K, extra):
     Case(T, V, K, dtype, 1.0, rest, extra=extra).check(b, form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("T,V,K", [(100, 2049, 20), (2500, 2300, 30), (1300, 4097, 9), (100, 6200, 40), (700, 12289, 33), (640, 16400, 500), (100, 24577, 20), (330, 30001, 1024), (310, 49153, 16),
+                                   (100, 66001, 64)])
+def test_many_rows(b, form, dtype, T, V, K):
+    """More rows than blocks, with lists of every length, repeated words, and rows that are passed over, next to one another."""
+    g = np.random.default_rng(T)
+    c = Case(T, V, K, dtype, 1.5, T % 20 == 0)
+    c.idx[np.arange(K)[None] >= g.integers(0, K + 1, (T, 1))] = -1
+    again = np.nonzero(g.random(T) < 0.3)[0]
+    c.idx[again, -1] = c.idx[again, 0]
+    c.weight[g.random(T) < 0.2] = 0
+    c.S[torch.from_numpy(c.weight == 0).cuda()] = float("nan")
+    pick = np.unique(np.r_[:4, T - 4:T, g.integers(0, T, 16)])
+    loss, dS = c.check(b, form, rows=pick)
+    assert torch.isfinite(loss).all() and (dS is None or torch.isfinite(dS).all())
+    assert not torch.any(loss[torch.from_numpy((c.weight == 0) | (c.idx < 0).all(1)).cuda()])
+    if form != "fwd":
+        _, same = c.run(b, form, in_place=True)
+        assert torch.equal(same, dS)
 
 
 @pytest.mark.parametrize("form", ["fwd", "both"])
@@ -298,7 +326,9 @@ def test_offsets_beyond_32_bits(b):
     b.distill_topk_fwd_bwd(S, *a, loss, S)
     dS2 = rows_of(2, V, BF, 0.0)
     b.distill_topk_fwd_bwd(small.S, *small.device(), loss2, dS2)
-    assert torch.equal(S[-2:], dS2) and torch.equal(loss[-2:], loss2) and not torch.any(S[:-2]) and not torch.any(loss[:-2])
+    # calls of two lengths may take two kernels: sums in another order, and a gradient that rounds to the neighbour
+    assert torch.allclose(loss[-2:], loss2, rtol=0, atol=2 * (V / 32 + 64) * U) and torch.allclose(S[-2:].float(), dS2.float(), rtol=2.0 ** -7, atol=0)
+    assert not torch.any(S[:-2]) and not torch.any(loss[:-2])
 
 
 def test_replays_and_streams(b):

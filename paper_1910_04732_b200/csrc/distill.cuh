@@ -377,33 +377,62 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G) part_kernel(const Args a) {
   }
 }
 
-// ---- rows that one block of G threads walks, persistent over the rows.  Every thread copies its own 16-byte pieces to its own places in
-// shared memory, N pieces ahead, and waits for nobody to read them: the copies run on through the reductions and across rows.
-// RES (loss and gradient): the row fits the N places of every thread; the second pass finds it there, and as each place is read for the last
-// time the next row's piece is asked for.  Otherwise the places are a ring of batches, and a row that needs two passes is read twice, the
-// second time from L2.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+// ---- rows that one block of G threads walks, persistent over the rows.  A thread has a batch of four 16-byte pieces in registers and the next
+// one on its way, across the end of a pass and of a row; loss and gradient read a row twice, the second time from L1 or L2 (592 rows in flight are
+// at most 150 MB for the widest vocabularies and 38 MB at 128k words; measured DRAM traffic there: each logit once in, once out).
+constexpr int kBatch = 4;
+
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^(x c - m) of elements 2 i and 2 i + 1
 template <typename T>
-__device__ __forceinline__ void copy_piece(uint32_t dst, const T* row, int piece, int V, int vec) {
-  const int at = piece * kPer<T>, left = (V - at) * (int)sizeof(T);
-  if (vec) { copy16(dst, row + at, min(left, 16)); return; }      // (what lies behind the row is hidden with the listed words)
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (4 * e < left) copy4(dst + 4 * e, reinterpret_cast<const float*>(row) + at + e);
+__device__ __forceinline__ uint64_t pair_exp(const uint4& v, int i, uint64_t c2, uint64_t neg_m2) {
+  const float2 x = unpack2(fma2(pack2(elem<T>(v, 2 * i), elem<T>(v, 2 * i + 1)), c2, neg_m2));
+  return pack2(ex2(x.x), ex2(x.y));
 }
-
-constexpr int kPlaces = 12, kBatch = 4;
-__host__ __device__ inline size_t row_smem(int g, int V, int K) { return (size_t)kPlaces * g * 16 + part_smem(V + 8, K); }
-
-template <typename T, int MODE, int G, bool RES>
+__device__ __forceinline__ uint32_t hmax2_word(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <typename T>
+__device__ __forceinline__ float batch_max(const uint4 (&d)[kBatch]) {
+  if (sizeof(T) == 4) {
+    float m = piece_max<T>(d[0]);
+#pragma unroll
+    for (int i = 1; i < kBatch; ++i) m = fmaxf(m, piece_max<T>(d[i]));
+    return m;
+  }
+  uint32_t m = hmax2_word(hmax2_word(d[0].x, d[0].y), hmax2_word(d[0].z, d[0].w));
+#pragma unroll
+  for (int i = 1; i < kBatch; ++i) m = hmax2_word(m, hmax2_word(hmax2_word(d[i].x, d[i].y), hmax2_word(d[i].z, d[i].w)));
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+}
+template <typename T, int MODE, int G>
 __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
-  constexpr int NW = warps_of(G), N = kPlaces;
-  static_assert(!RES || MODE == BOTH, "one pass keeps nothing");
+  constexpr int NW = warps_of(G);
   extern __shared__ __align__(16) unsigned char smem[];
   struct First { float t, n, x, m, s; };
   struct Second { double a, kl; float top; };
@@ -411,17 +440,14 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
   __shared__ Second second[NW];
   __shared__ int s_dup;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  uint4* tile = reinterpret_cast<uint4*>(smem) + tid;                    // place i of this thread: tile[i * G]
-  const uint32_t tile_addr = (uint32_t)__cvta_generic_to_shared(tile);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(smem + (size_t)N * G * 16);
-  const int words4 = (a.V + 8 + 127) / 128, pieces = (a.V + kPer<T> - 1) / kPer<T>;
+  uint32_t* bits = reinterpret_cast<uint32_t*>(smem);
+  const int words4 = (a.V + 127) / 128, pieces = (a.V + kPer<T> - 1) / kPer<T>;
   int* slot_idx = reinterpret_cast<int*>(bits + 4 * words4);
   float* slot_t = reinterpret_cast<float*>(slot_idx + a.K);
   float* slot_x = slot_t + a.K;
   for (int i = tid; i < words4; i += G) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
   if (tid == 0) s_dup = 0;
   __syncthreads();
-  if (tid < 8 && a.V + tid < pieces * kPer<T>) atomicOr(&bits[(a.V + tid) >> 5], 1u << ((a.V + tid) & 31));
   pdl_wait();
   pdl_launch_dependents();
   const T* S0 = reinterpret_cast<const T*>(a.S);
@@ -439,44 +465,51 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
     if (MODE & BWD)
       for (int p = tid; p < pieces; p += G) store_piece<T>(dS0 + row * a.ldds, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
   };
-  auto active_from = [&](int64_t row, bool write) {                      // the next row of this block that is looked at
-    while (row < a.T && factor(row) == 0.f) { if (write) nothing(row); row += gridDim.x; }
+  auto active_from = [&](int64_t row) {                                  // the next row of this block that is looked at
+    while (row < a.T && factor(row) == 0.f) { nothing(row); row += gridDim.x; }
     return row;
   };
-  const int batches = (pieces + G * kBatch - 1) / (G * kBatch), passes = MODE == BOTH && !RES ? 2 : 1;
-  // the copies' own position: row, pass, batch (ring) -- one commit per batch or place, whether it copies or not
-  int64_t row = active_from(blockIdx.x, true), ahead = row;
-  int ahead_batch = 0, ring_in = 0, ring_out = 0;
-  auto copy_batch = [&]() {
-    if (ahead < a.T) {
-      const T* S = S0 + ahead * a.lds;
-      const int b = ahead_batch >= batches ? ahead_batch - batches : ahead_batch;
+  const int batches = (pieces + G * kBatch - 1) / (G * kBatch);
+  const int whole = a.vec ? a.V / (kPer<T> * G * kBatch) : 0;            // batches whose pieces are all there
+  uint4 d[kBatch], ahead[kBatch];
+  auto load = [&](uint4 (&to)[kBatch], const T* S, int b) {
+    if (b < whole) {
+      const uint4* p = reinterpret_cast<const uint4*>(S) + b * kBatch * G + tid;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) to[i] = p[i * G];
+    } else {
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
         const int p = (b * kBatch + i) * G + tid;
-        if (p < pieces) copy_piece<T>(tile_addr + (uint32_t)((ring_in * kBatch + i) * G * 16), S, p, a.V, a.vec);
+        to[i] = p < pieces ? load_piece<T>(S, p, a.V, a.vec) : make_uint4(neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>());
       }
-      if (++ahead_batch == passes * batches) { ahead_batch = 0; ahead = active_from(ahead + gridDim.x, false); }
     }
-    if (++ring_in == N / kBatch) ring_in = 0;
-    copies_commit();
   };
-  auto copy_place = [&](int i, int64_t r) {
-    const int p = i * G + tid;
-    if (r < a.T && p < pieces) copy_piece<T>(tile_addr + (uint32_t)(i * G * 16), S0 + r * a.lds, p, a.V, a.vec);
-    copies_commit();
-  };
-  if (RES) {
+  auto hide_listed = [&](int b) {
+    const uint8_t* at = reinterpret_cast<const uint8_t*>(bits);
+    uint32_t l[kBatch], any = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) copy_place(i, row);
-  } else {
-    for (int i = 0; i < N / kBatch; ++i) copy_batch();
-  }
+    for (int i = 0; i < kBatch; ++i) {
+      const int p = (b * kBatch + i) * G + tid;
+      l[i] = 0;
+      if (b < whole || p < pieces) l[i] = kPer<T> == 8 ? at[p] : (at[p >> 1] >> (4 * (tid & 1))) & 15u;      // (G is even)
+      any |= l[i];
+    }
+    if (any) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (l[i]) hide<T>(d[i], l[i]);
+    }
+  };
+  int64_t row = active_from(blockIdx.x);
+  if (row < a.T) load(ahead, S0 + row * a.lds, 0);
   while (row < a.T) {
     const T* S = S0 + row * a.lds;
     const float w = a.weight ? a.weight[row] : 1.f;
     float g = w * a.inv_tau;
     if (MODE == BWD && a.dloss) g = a.dloss[row] * g;
+    const int64_t next = active_from(row + gridDim.x);
+    const T* S_next = next < a.T ? S0 + next * a.lds : nullptr;
     __syncthreads();                                                     // the bits of the row before are clear
     for (int j = tid; j < a.K; j += G) {
       int idx = a.t_idx[row * a.ldi + j];
@@ -509,47 +542,33 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
       }
     // ---- first pass: maximum and sum outside the list, kept relative to the maximum so far
     float m = -INFINITY, ref = 0.f, s = 0.f;
-    auto take = [&](const uint4& v) {
-      const float mv = piece_max<T>(v);
-      if (mv > m) {
-        const float to = __fmul_rn(mv, a.c);
-        s *= ex2(m == -INFINITY ? -INFINITY : ref - to);
-        m = mv; ref = to;
-      }
-      s += piece_sum<T>(v, a.c, ref);
-    };
-    if (RES) {
-      auto place = [&](int i) {
-        const int p = i * G + tid;
-        if (p < pieces) {
-          uint4 v = tile[i * G];
-          const uint32_t listed = listed_of<T>(bits, p);
-          if (listed) { hide<T>(v, listed); tile[i * G] = v; }
-          take(v);
-        }
-      };
-      copies_wait<N - 4>();
-      place(0); place(1); place(2); place(3);
-      copies_wait<N - 8>();
-      place(4); place(5); place(6); place(7);
-      copies_wait<0>();
-      place(8); place(9); place(10); place(11);
-    } else if (MODE & FWD) {
+    if (MODE & FWD) {
+      const uint64_t c2 = pack2(a.c, a.c);
+      uint64_t s2 = pack2(0.f, 0.f), neg_ref2 = pack2(0.f, 0.f);
       for (int b = 0; b < batches; ++b) {
-        copies_wait<N / kBatch - 1>();
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) d[i] = ahead[i];
+        if (b + 1 < batches) load(ahead, S, b + 1);
+        else if (MODE == BOTH) load(ahead, S, 0);
+        else if (S_next) load(ahead, S_next, 0);
+        hide_listed(b);
+        const float mv = batch_max<T>(d);
+        if (mv > m) {
+          const float to = __fmul_rn(mv, a.c), by = ex2(m == -INFINITY ? -INFINITY : ref - to);
+          s2 = mul2(s2, pack2(by, by));
+          m = mv; ref = to;
+          neg_ref2 = pack2(-to, -to);
+        }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-          const int p = (b * kBatch + i) * G + tid;
-          if (p < pieces) {
-            uint4 v = tile[(ring_out * kBatch + i) * G];
-            const uint32_t listed = listed_of<T>(bits, p);
-            if (listed) hide<T>(v, listed);
-            take(v);
-          }
+          uint64_t e = pair_exp<T>(d[i], 0, c2, neg_ref2);
+#pragma unroll
+          for (int j = 1; j < kPer<T> / 2; ++j) e = add2(e, pair_exp<T>(d[i], j, c2, neg_ref2));
+          s2 = add2(s2, e);
         }
-        if (++ring_out == N / kBatch) ring_out = 0;
-        copy_batch();
       }
+      const float2 both = unpack2(s2);
+      s = both.x + both.y;
     }
     f.m = m; f.s = s;
     // ---- over the block
@@ -621,38 +640,34 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
       }
     }
     // ---- second pass: the gradient
-    const int64_t next = RES ? active_from(row + gridDim.x, true) : 0;
     if (MODE & BWD) {
       T* dS = dS0 + row * a.ldds;
       const float pull = l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - mc - l2all) - r * ex2(-l2rest));
-      if (RES) {
+      const uint64_t c2 = pack2(a.c, a.c), neg_ref2 = pack2(-m_rest, -m_rest), pull2 = pack2(pull, pull);
+      for (int b = 0; b < batches; ++b) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int p = i * G + tid;
-          if (p < pieces) {
-            uint4 o = piece_grad<T>(tile[i * G], a.c, m_rest, pull);
-            if (empty) o = make_uint4(0, 0, 0, 0);
-            store_piece<T>(dS, p, a.V, a.vec, o);
-          }
-          copy_place(i, next);
-        }
-      } else {
-        for (int b = 0; b < batches; ++b) {
-          copies_wait<N / kBatch - 1>();
+        for (int i = 0; i < kBatch; ++i) d[i] = ahead[i];
+        if (b + 1 < batches) load(ahead, S, b + 1);
+        else if (S_next) load(ahead, S_next, 0);
+        hide_listed(b);
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int p = (b * kBatch + i) * G + tid;
-            if (p < pieces) {
-              uint4 v = tile[(ring_out * kBatch + i) * G];
-              const uint32_t listed = listed_of<T>(bits, p);
-              if (listed) hide<T>(v, listed);
-              v = piece_grad<T>(v, a.c, m_rest, pull);
-              if (empty) v = make_uint4(0, 0, 0, 0);
-              store_piece<T>(dS, p, a.V, a.vec, v);
+        for (int i = 0; i < kBatch; ++i) {
+          uint4 o;
+          uint32_t* ow = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+          for (int j = 0; j < kPer<T> / 2; ++j) {
+            const float2 e = unpack2(mul2(pair_exp<T>(d[i], j, c2, neg_ref2), pull2));
+            if (sizeof(T) == 4) {
+              ow[2 * j] = __float_as_uint(e.x); ow[2 * j + 1] = __float_as_uint(e.y);
+            } else {
+              const __nv_bfloat162 hh = __floats2bfloat162_rn(e.x, e.y);
+              ow[j] = *reinterpret_cast<const uint32_t*>(&hh);
             }
           }
-          if (++ring_out == N / kBatch) ring_out = 0;
-          copy_batch();
+          if (empty) o = make_uint4(0, 0, 0, 0);
+          const int p = (b * kBatch + i) * G + tid;
+          if (b < whole) __stcs(reinterpret_cast<uint4*>(dS) + p, o);
+          else if (p < pieces) store_piece<T>(dS, p, a.V, a.vec, o);
         }
       }
       __syncthreads();                                                   // the zeros of the listed words are written
@@ -661,9 +676,8 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
     }
     for (int j = tid; j < a.K; j += G)
       if (slot_idx[j] >= 0) atomicAnd(&bits[slot_idx[j] >> 5], ~(1u << (slot_idx[j] & 31)));
-    row = RES ? next : active_from(row + gridDim.x, true);
+    row = next;
   }
-  copies_wait<0>();
 }
 
 }  // namespace distill

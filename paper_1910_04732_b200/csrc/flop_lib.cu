@@ -1280,12 +1280,12 @@ int launch_distill_part(const distill::Args& a, int parts, cudaStream_t st) {
   FLOP_CUDA(cudaGetLastError());
   return FLOP_OK;
 }
-template <typename T, int MODE, int G, bool RES>
+template <typename T, int MODE, int G>
 int launch_distill_row(const distill::Args& a, cudaStream_t st) {
   static OncePerDevice configured;
-  auto kern = distill::row_kernel<T, MODE, G, RES>;
-  FLOP_TRY(allow_smem(configured, kSmemBudget, kern));
-  const size_t smem = distill::row_smem(G, a.V, a.K);
+  auto kern = distill::row_kernel<T, MODE, G>;
+  FLOP_TRY(allow_smem(configured, distill::part_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
+  const size_t smem = distill::part_smem(a.V, a.K);
   const int resident = (int)std::min<size_t>(1024 / G, (size_t)(228 * 1024) / (smem + 2048));
   launch_k(kern, dim3((unsigned)std::min<int64_t>(a.T, (int64_t)num_sms() * std::max(resident, 1))), dim3(G), smem, st, a);
   count_launch();
@@ -1306,15 +1306,9 @@ int launch_distill_inst(const distill::Args& a, cudaStream_t st) {
     if (pieces <= (int64_t)parts * 2048) return launch_distill_part<T, MODE, 256, 8>(a, parts, st);
     return launch_distill_part<T, MODE, 512, 8>(a, parts, st);
   }
-  if constexpr (MODE == distill::BOTH) {
-    if (pieces <= distill::kPlaces * 128) return launch_distill_row<T, MODE, 128, true>(a, st);
-    if (pieces <= distill::kPlaces * 256) return launch_distill_row<T, MODE, 256, true>(a, st);
-    if (pieces <= distill::kPlaces * 512) return launch_distill_row<T, MODE, 512, true>(a, st);
-  } else if (pieces <= 1024) {
-    return launch_distill_row<T, MODE, 128, false>(a, st);
-  }
-  if (pieces <= 4096 || a.V > distill::kMaxVocab / 2) return launch_distill_row<T, MODE, 256, false>(a, st);
-  return launch_distill_row<T, MODE, 512, false>(a, st);
+  if (pieces <= 1024) return launch_distill_row<T, MODE, 128>(a, st);
+  if (pieces <= 4096) return launch_distill_row<T, MODE, 256>(a, st);
+  return launch_distill_row<T, MODE, 512>(a, st);
 }
 template <int MODE>
 int distill_impl(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi, int64_t K,

@@ -24,7 +24,7 @@ namespace flop {
 namespace distill {
 
 constexpr int kMaxSlots = 1024;
-constexpr int kMaxVocab = 1 << 20;        // a bit per word in shared memory: 128 KB
+constexpr int kMaxVocab = 1 << 19;        // two bits per word in shared memory: 128 KB
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr double kLn2d = 0.6931471805599453;
 
@@ -430,69 +430,211 @@ __device__ __forceinline__ float batch_max(const uint4 (&d)[kBatch]) {
   for (int i = 1; i < kBatch; ++i) m = hmax2_word(m, hmax2_word(hmax2_word(d[i].x, d[i].y), hmax2_word(d[i].z, d[i].w)));
   return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
 }
+// Named barriers of a block (0 is __syncthreads): hardware barriers of all its G threads, some of which only arrive.
+__device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+
+__host__ __device__ inline size_t row_smem(int V, int K) { return 2 * part_smem(V, K); }      // this row's list and the next one's
+
+// The last warp of the block has the lists, one row ahead of the others: it reads a row's list, sets its bits and does everything that
+// takes only the slots while the other warps are at the row before, takes the loss when their sums are there, and writes the K entries of the
+// gradient when they are through.  Barriers, in the order the other warps (M) and this one (L) meet them, row by row:
+//     kBits    L arrives when the row's bits are set              M waits before its first look at them
+//     kSums    both wait: M's sums and L's numbers of the row are written
+//     kStored  M arrives when the row's gradient is written       L waits before it writes the listed words and clears the bits
 template <typename T, int MODE, int G>
 __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
-  constexpr int NW = warps_of(G);
+  constexpr int M = G - 32, NW = M / 32;
+  constexpr int kBits = 1, kSums = 2, kStored = 3;
   extern __shared__ __align__(16) unsigned char smem[];
-  struct First { float t, n, x, m, s; };
-  struct Second { double a, kl; float top; };
-  __shared__ First first[NW];
-  __shared__ Second second[NW];
-  __shared__ int s_dup;
+  struct Sums { float m, s; };                                           // maximum (logit) and sum outside the list, relative to 2^(m c)
+  struct Info { float top_ref, top, r, mc, l2all, m_rest, l2rest; int empty; };
+  __shared__ Sums sums[2][NW];
+  __shared__ Info info[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  uint32_t* bits = reinterpret_cast<uint32_t*>(smem);
   const int words4 = (a.V + 127) / 128, pieces = (a.V + kPer<T> - 1) / kPer<T>;
-  int* slot_idx = reinterpret_cast<int*>(bits + 4 * words4);
-  float* slot_t = reinterpret_cast<float*>(slot_idx + a.K);
-  float* slot_x = slot_t + a.K;
-  for (int i = tid; i < words4; i += G) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
-  if (tid == 0) s_dup = 0;
+  const size_t side_bytes = part_smem(a.V, a.K);
+  for (size_t i = tid; i < 2 * side_bytes / 16; i += G) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
   const T* S0 = reinterpret_cast<const T*>(a.S);
   T* dS0 = reinterpret_cast<T*>(a.dS);
-  auto factor = [&](int64_t row) {                                       // what decides whether a row is looked at
-    float g = a.weight ? a.weight[row] : 1.f;
-    if (MODE == BWD && a.dloss) g *= a.dloss[row];
-    return g;
-  };
-  auto nothing = [&](int64_t row) {
-    if ((MODE & FWD) && tid == 0) {
-      a.loss[row] = 0.f;
-      if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
-    }
-    if (MODE & BWD)
-      for (int p = tid; p < pieces; p += G) store_piece<T>(dS0 + row * a.ldds, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
-  };
   auto active_from = [&](int64_t row) {                                  // the next row of this block that is looked at
-    while (row < a.T && factor(row) == 0.f) { nothing(row); row += gridDim.x; }
+    for (; row < a.T; row += gridDim.x) {
+      float g = a.weight ? a.weight[row] : 1.f;
+      if (MODE == BWD && a.dloss) g *= a.dloss[row];
+      if (g != 0.f) break;
+      if (warp == NW) {
+        if ((MODE & FWD) && lane == 0) {
+          a.loss[row] = 0.f;
+          if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
+        }
+      } else if (MODE & BWD) {
+        for (int p = tid; p < pieces; p += M) store_piece<T>(dS0 + row * a.ldds, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
+      }
+    }
     return row;
   };
-  const int batches = (pieces + G * kBatch - 1) / (G * kBatch);
-  const int whole = a.vec ? a.V / (kPer<T> * G * kBatch) : 0;            // batches whose pieces are all there
+  auto factor = [&](int64_t row) {                                       // of the row's gradient
+    const float g = (a.weight ? a.weight[row] : 1.f) * a.inv_tau;
+    return MODE == BWD && a.dloss ? a.dloss[row] * g : g;
+  };
+  int64_t row = active_from(blockIdx.x);
+  if (row >= a.T) return;
+
+  if (warp == NW) {
+    // ------------------------------------------------------------------------------------ the lists
+    struct List { uint32_t* bits; int* idx; float *t, *x; };
+    auto list_of = [&](int side) {
+      List l;
+      l.bits = reinterpret_cast<uint32_t*>(smem + side * side_bytes);
+      l.idx = reinterpret_cast<int*>(l.bits + 4 * words4);
+      l.t = reinterpret_cast<float*>(l.idx + a.K);
+      l.x = l.t + a.K;
+      return l;
+    };
+    double sum_q = 0.0, kl = 0.0;                                        // of the row whose info was written last
+    auto read_list = [&](int side, int64_t row) {
+      const List l = list_of(side);
+      const T* S = S0 + row * a.lds;
+      bool dup = false;
+      for (int j = lane; j < a.K; j += 32) {
+        int idx = a.t_idx[row * a.ldi + j];
+        if (idx < 0 || idx >= a.V) idx = -1;
+        l.idx[j] = idx;
+        if (idx < 0) continue;
+        dup |= atomicOr(&l.bits[idx >> 5], 1u << (idx & 31)) >> (idx & 31) & 1u;
+        l.t[j] = a.t_logits[row * a.ldt + j];
+        l.x[j] = to_f32(S[idx]);
+      }
+      __syncwarp();
+      bar_arrive(kBits, G);
+      if (__any_sync(0xffffffffu, dup)) {                                // rare: the first of equal indices stays
+        uint32_t drop = 0;
+        for (int j = lane, n = 0; j < a.K; j += 32, ++n)
+          if (l.idx[j] >= 0)
+            for (int i = 0; i < j; ++i)
+              if (l.idx[i] == l.idx[j]) { drop |= 1u << n; break; }
+        __syncwarp();
+        for (int j = lane, n = 0; j < a.K; j += 32, ++n)
+          if (drop >> n & 1u) l.idx[j] = -1;
+        __syncwarp();
+      }
+      float mt = -INFINITY, n = 0.f, mx = -INFINITY;
+      for (int j = lane; j < a.K; j += 32)
+        if (l.idx[j] >= 0) { mt = nan_max(mt, l.t[j]); n += 1.f; mx = fmaxf(mx, l.x[j]); }
+      mt = warp_all(mt, nan_max); n = warp_all(n, add<float>); mx = warp_all(mx, max2);
+      const double t_ref = a.t_lse ? (double)a.t_lse[row] : (double)mt * a.inv_tau_d;
+      // the student's exponentials on the list relative to the largest there
+      const float ref = !(MODE & FWD) ? 0.f : mx == -INFINITY ? 0.f : __fmul_rn(mx, a.c);
+      float top = 0.f;
+      sum_q = 0.0; kl = 0.0;
+      for (int j = lane; j < a.K; j += 32) {
+        if (l.idx[j] < 0) continue;
+        const double lq = (double)l.t[j] * a.inv_tau_d - t_ref;
+        const float q = exp_of(lq);
+        l.t[j] = q;
+        sum_q += (double)q;
+        if (MODE & FWD) {
+          const double lx = ((double)l.x[j] * (double)a.c - (double)ref) * kLn2d;
+          const float e = exp_of(lx);
+          l.x[j] = e;
+          top += e;
+          if (!(q <= 0.f)) kl += (double)q * (lq - lx);
+        }
+      }
+      sum_q = warp_all(sum_q, add<double>);
+      if (MODE & FWD) { kl = warp_all(kl, add<double>); top = warp_all(top, add<float>); }
+      if (lane == 0) {
+        Info& o = info[side];
+        o.top_ref = ref; o.top = top;
+        o.r = a.t_lse && n < (float)a.V ? (float)fmax(0.0, 1.0 - sum_q) : 0.f;
+        o.empty = n == 0.f || (!a.t_lse && mt == -INFINITY);             // an empty list, or one that gives every word nothing
+        if (MODE == BWD) { const float* st = a.stats_in + 4 * row; o.mc = st[0]; o.l2all = st[1]; o.m_rest = st[2]; o.l2rest = st[3]; }
+      }
+      __syncwarp();
+    };
+    // what is left of a row when its gradient is written: the listed words, and their bits
+    auto finish = [&](int side, int64_t row, float all_inv, float q_norm) {
+      const List l = list_of(side);
+      const Info o = info[side];
+      if (MODE & BWD) {
+        bar_sync(kStored, G);
+        const float g = factor(row);
+        for (int j = lane; j < a.K; j += 32)
+          if (l.idx[j] >= 0 && !o.empty) {
+            const float p = MODE == BWD ? ex2(fmaf(l.x[j], a.c, -o.mc) - o.l2all) : l.x[j] * all_inv;
+            dS0[row * a.ldds + l.idx[j]] = from_f32<T>(g * (p - l.t[j] * q_norm));
+          }
+      }
+      for (int j = lane; j < a.K; j += 32)
+        if (l.idx[j] >= 0) atomicAnd(&l.bits[l.idx[j] >> 5], ~(1u << (l.idx[j] & 31)));
+      __syncwarp();
+    };
+    int side = 0;
+    read_list(0, row);
+    for (;;) {
+      const int64_t next = active_from(row + gridDim.x);
+      bar_sync(kSums, G);
+      const double a_q = sum_q;
+      float all_inv = 0.f;
+      const float q_norm = a.t_lse ? 1.f : (float)(1.0 / a_q);
+      if (MODE & FWD) {
+        const Info o = info[side];
+        const Sums u = lane < NW ? sums[side][lane] : Sums{-INFINITY, 0.f};
+        const float m = warp_all(u.m, max2), m_rest = m == -INFINITY ? 0.f : __fmul_rn(m, a.c);
+        const float s = warp_all(u.m == -INFINITY ? u.s : u.s * pow2_of(__fmul_rn(u.m, a.c) - m_rest), add<float>);
+        // relative to the larger reference
+        const float mc = o.top > 0.f || o.top != o.top ? fmaxf(o.top_ref, m == -INFINITY ? o.top_ref : m_rest) : m_rest;
+        const float on = o.top * pow2_of(o.top_ref - mc);
+        const float all = on + (s > 0.f ? s * pow2_of(m_rest - mc) : s);
+        all_inv = pow2_of(o.top_ref - mc) / all;
+        if (lane == 0) {
+          const double l2a = log2_of(all);
+          // the terms' logarithms are relative to the list's reference
+          const double log_all = (l2a + (double)mc - (double)o.top_ref) * kLn2d;
+          double v = a.t_lse ? kl + a_q * log_all : kl / a_q - log2_of((float)a_q) * kLn2d + log_all;
+          if (o.r > 0.f) v += (double)o.r * (log_left(a_q, o.r) - log_share(s, m_rest, mc, on, l2a));
+          a.loss[row] = o.empty ? 0.f : (a.weight ? a.weight[row] : 1.f) * (float)v;
+          if (a.stats) { float* st = a.stats + 4 * row; st[0] = mc; st[1] = (float)l2a; st[2] = m_rest; st[3] = log2f(s); }
+        }
+      }
+      if (next < a.T) read_list(side ^ 1, next);
+      finish(side, row, all_inv, q_norm);
+      if (next >= a.T) break;
+      row = next;
+      side ^= 1;
+    }
+    return;
+  }
+
+  // ------------------------------------------------------------------------------------ the vocabulary
+  const int batches = (pieces + M * kBatch - 1) / (M * kBatch);
+  const int whole = a.vec ? a.V / (kPer<T> * M * kBatch) : 0;            // batches whose pieces are all there
   uint4 d[kBatch], ahead[kBatch];
   auto load = [&](uint4 (&to)[kBatch], const T* S, int b) {
     if (b < whole) {
-      const uint4* p = reinterpret_cast<const uint4*>(S) + b * kBatch * G + tid;
+      const uint4* p = reinterpret_cast<const uint4*>(S) + b * kBatch * M + tid;
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) to[i] = p[i * G];
+      for (int i = 0; i < kBatch; ++i) to[i] = p[i * M];
     } else {
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const int p = (b * kBatch + i) * G + tid;
+        const int p = (b * kBatch + i) * M + tid;
         to[i] = p < pieces ? load_piece<T>(S, p, a.V, a.vec) : make_uint4(neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>(), neg_inf_word<T>());
       }
     }
   };
+  int side = 0;
   auto hide_listed = [&](int b) {
-    const uint8_t* at = reinterpret_cast<const uint8_t*>(bits);
+    const uint8_t* at = smem + side * side_bytes;
     uint32_t l[kBatch], any = 0;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int p = (b * kBatch + i) * G + tid;
+      const int p = (b * kBatch + i) * M + tid;
       l[i] = 0;
-      if (b < whole || p < pieces) l[i] = kPer<T> == 8 ? at[p] : (at[p >> 1] >> (4 * (tid & 1))) & 15u;      // (G is even)
+      if (b < whole || p < pieces) l[i] = kPer<T> == 8 ? at[p] : (at[p >> 1] >> (4 * (tid & 1))) & 15u;      // (M is even)
       any |= l[i];
     }
     if (any) {
@@ -501,55 +643,23 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
         if (l[i]) hide<T>(d[i], l[i]);
     }
   };
-  int64_t row = active_from(blockIdx.x);
-  if (row < a.T) load(ahead, S0 + row * a.lds, 0);
-  while (row < a.T) {
+  const uint64_t c2 = pack2(a.c, a.c);
+  load(ahead, S0 + row * a.lds, 0);
+  for (;;) {
     const T* S = S0 + row * a.lds;
-    const float w = a.weight ? a.weight[row] : 1.f;
-    float g = w * a.inv_tau;
-    if (MODE == BWD && a.dloss) g = a.dloss[row] * g;
     const int64_t next = active_from(row + gridDim.x);
     const T* S_next = next < a.T ? S0 + next * a.lds : nullptr;
-    __syncthreads();                                                     // the bits of the row before are clear
-    for (int j = tid; j < a.K; j += G) {
-      int idx = a.t_idx[row * a.ldi + j];
-      if (idx < 0 || idx >= a.V) idx = -1;
-      slot_idx[j] = idx;
-      if (idx < 0) continue;
-      if (atomicOr(&bits[idx >> 5], 1u << (idx & 31)) >> (idx & 31) & 1u) s_dup = 1;
-      slot_t[j] = a.t_logits[row * a.ldt + j];
-      slot_x[j] = to_f32(S[idx]);
-    }
-    __syncthreads();
-    if (s_dup) {                                                         // rare: the first of equal indices stays
-      uint32_t drop = 0;
-      for (int j = tid, n = 0; j < a.K; j += G, ++n)
-        if (slot_idx[j] >= 0)
-          for (int i = 0; i < j; ++i)
-            if (slot_idx[i] == slot_idx[j]) { drop |= 1u << n; break; }
-      __syncthreads();
-      for (int j = tid, n = 0; j < a.K; j += G, ++n)
-        if (drop >> n & 1u) slot_idx[j] = -1;
-      if (tid == 0) s_dup = 0;
-      __syncthreads();
-    }
-    First f{-INFINITY, 0.f, -INFINITY, -INFINITY, 0.f};
-    for (int j = tid; j < a.K; j += G)
-      if (slot_idx[j] >= 0) {
-        f.t = nan_max(f.t, slot_t[j]);
-        f.n += 1.f;
-        if (MODE & FWD) f.x = fmaxf(f.x, slot_x[j]);
-      }
-    // ---- first pass: maximum and sum outside the list, kept relative to the maximum so far
-    float m = -INFINITY, ref = 0.f, s = 0.f;
+    bar_sync(kBits, G);
+    float m = -INFINITY;
     if (MODE & FWD) {
-      const uint64_t c2 = pack2(a.c, a.c);
+      // first pass: maximum and sum outside the list, kept relative to the maximum so far
+      float ref = 0.f;
       uint64_t s2 = pack2(0.f, 0.f), neg_ref2 = pack2(0.f, 0.f);
       for (int b = 0; b < batches; ++b) {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) d[i] = ahead[i];
         if (b + 1 < batches) load(ahead, S, b + 1);
-        else if (MODE == BOTH) load(ahead, S, 0);
+        else if (MODE == BOTH && batches > 1) load(ahead, S, batches - 2);
         else if (S_next) load(ahead, S_next, 0);
         hide_listed(b);
         const float mv = batch_max<T>(d);
@@ -568,92 +678,45 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
         }
       }
       const float2 both = unpack2(s2);
-      s = both.x + both.y;
+      float s = both.x + both.y;
+      const float mw = warp_all(m, max2);
+      s = warp_all(m == -INFINITY ? s : s * ex2(ref - __fmul_rn(mw, a.c)), add<float>);
+      if (lane == 0) sums[side][warp] = Sums{mw, s};
     }
-    f.m = m; f.s = s;
-    // ---- over the block
-    f.t = warp_all(f.t, nan_max);
-    f.n = warp_all(f.n, add<float>);
-    if (MODE & FWD) {
-      f.x = warp_all(f.x, max2);
-      f.m = warp_all(m, max2);
-      f.s = warp_all(m == -INFINITY ? s : s * ex2(ref - __fmul_rn(f.m, a.c)), add<float>);
-    }
-    if (lane == 0) first[warp] = f;
-    __syncthreads();
-    {
-      const First o = lane < NW ? first[lane] : First{-INFINITY, 0.f, -INFINITY, -INFINITY, 0.f};
-      f.t = warp_all(o.t, nan_max);
-      f.n = warp_all(o.n, add<float>);
-      if (MODE & FWD) {
-        f.x = warp_all(o.x, max2);
-        f.m = warp_all(o.m, max2);
-        f.s = warp_all(o.m == -INFINITY ? o.s : o.s * pow2_of(__fmul_rn(o.m, a.c) - __fmul_rn(f.m, a.c)), add<float>);
-      }
-    }
-    const bool empty = f.n == 0.f || (!a.t_lse && f.t == -INFINITY);     // an empty list, or one that gives every word nothing
-    float mc, l2all = 0.f, m_rest, l2rest;
-    if (MODE & FWD) {
-      m_rest = f.m == -INFINITY ? 0.f : __fmul_rn(f.m, a.c);
-      mc = __fmul_rn(fmaxf(f.m, f.x), a.c);
-      l2rest = log2f(f.s);
-    } else {
-      const float* o = a.stats_in + 4 * row;
-      mc = o[0]; l2all = o[1]; m_rest = o[2]; l2rest = o[3];
-    }
-    const double t_ref = a.t_lse ? (double)a.t_lse[row] : (double)f.t * a.inv_tau_d;
-    Second h{0.0, 0.0, 0.f};
-    for (int j = tid; j < a.K; j += G) {
-      if (slot_idx[j] < 0) continue;
-      const double lq = (double)slot_t[j] * a.inv_tau_d - t_ref;
-      const float q = exp_of(lq);
-      slot_t[j] = q;
-      h.a += (double)q;
-      if (MODE & FWD) {
-        const double lx = ((double)slot_x[j] * (double)a.c - (double)mc) * kLn2d;
-        h.top += exp_of(lx);
-        if (!(q <= 0.f)) h.kl += (double)q * (lq - lx);
-      }
-    }
-    if (a.K > 32 * warp) {                                               // (the other warps have no slot)
-      h.a = warp_all(h.a, add<double>);
-      if (MODE & FWD) { h.kl = warp_all(h.kl, add<double>); h.top = warp_all(h.top, add<float>); }
-    }
-    if (lane == 0) second[warp] = h;
-    __syncthreads();
-    {
-      const Second o = lane < NW ? second[lane] : Second{0.0, 0.0, 0.f};
-      h.a = warp_all(o.a, add<double>);
-      if (MODE & FWD) { h.kl = warp_all(o.kl, add<double>); h.top = warp_all(o.top, add<float>); }
-    }
-    const float r = a.t_lse && f.n < (float)a.V ? (float)fmax(0.0, 1.0 - h.a) : 0.f;
-    const float q_norm = a.t_lse ? 1.f : (float)(1.0 / h.a);
-    if (MODE & FWD) {
-      const double l2a = log2_of(h.top + (f.s > 0.f ? f.s * pow2_of(m_rest - mc) : f.s));
-      l2all = (float)l2a;
-      if (tid == 0) {
-        double kl = h.kl + (a.t_lse ? h.a : 0.0) * l2a * kLn2d;
-        if (!a.t_lse) kl = h.kl / h.a - log2_of((float)h.a) * kLn2d + l2a * kLn2d;
-        if (r > 0.f) kl += (double)r * (log_left(h.a, r) - log_share(f.s, m_rest, mc, h.top, l2a));
-        a.loss[row] = empty ? 0.f : w * (float)kl;
-        if (a.stats) { float* o = a.stats + 4 * row; o[0] = mc; o[1] = l2all; o[2] = m_rest; o[3] = l2rest; }
-      }
-    }
-    // ---- second pass: the gradient
+    bar_sync(kSums, G);
     if (MODE & BWD) {
+      // second pass: outside the list 2^(x - m_rest) times what is common to the row
+      const Info& o = info[side];
+      const float g = factor(row), r = o.r;
+      float m_rest, pull;
+      if (MODE == BWD) {
+        m_rest = o.m_rest;
+        pull = o.l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - o.mc - o.l2all) - r * ex2(-o.l2rest));
+      } else {
+        const Sums u = lane < NW ? sums[side][lane] : Sums{-INFINITY, 0.f};
+        const float ma = warp_all(u.m, max2);
+        m_rest = ma == -INFINITY ? 0.f : __fmul_rn(ma, a.c);
+        const float s = warp_all(u.m == -INFINITY ? u.s : u.s * ex2(__fmul_rn(u.m, a.c) - m_rest), add<float>);
+        // 1 / (all words' sum) - r / (the rest's), both relative to the rest's maximum; a list far above it makes the first one 0
+        pull = s == 0.f ? 0.f : g * (1.f / (s + (o.top == 0.f ? 0.f : o.top * ex2(o.top_ref - m_rest))) - r / s);
+      }
+      const bool empty = o.empty;
       T* dS = dS0 + row * a.ldds;
-      const float pull = l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - mc - l2all) - r * ex2(-l2rest));
-      const uint64_t c2 = pack2(a.c, a.c), neg_ref2 = pack2(-m_rest, -m_rest), pull2 = pack2(pull, pull);
-      for (int b = 0; b < batches; ++b) {
+      const uint64_t neg_ref2 = pack2(-m_rest, -m_rest), pull2 = pack2(pull, pull);
+      // with a first pass before it, backwards: what was read last is here, in L1 or in L2
+      for (int n = 0; n < batches; ++n) {
+        const int b = MODE == BOTH ? batches - 1 - n : n;
+        if (MODE == BWD || n > 0) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) d[i] = ahead[i];
-        if (b + 1 < batches) load(ahead, S, b + 1);
-        else if (S_next) load(ahead, S_next, 0);
-        hide_listed(b);
+          for (int i = 0; i < kBatch; ++i) d[i] = ahead[i];
+          if (n + 1 < batches) load(ahead, S, MODE == BOTH ? b - 1 : b + 1);
+          else if (S_next) load(ahead, S_next, 0);
+          hide_listed(b);
+        }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-          uint4 o;
-          uint32_t* ow = reinterpret_cast<uint32_t*>(&o);
+          uint4 o4;
+          uint32_t* ow = reinterpret_cast<uint32_t*>(&o4);
 #pragma unroll
           for (int j = 0; j < kPer<T> / 2; ++j) {
             const float2 e = unpack2(mul2(pair_exp<T>(d[i], j, c2, neg_ref2), pull2));
@@ -664,19 +727,17 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
               ow[j] = *reinterpret_cast<const uint32_t*>(&hh);
             }
           }
-          if (empty) o = make_uint4(0, 0, 0, 0);
-          const int p = (b * kBatch + i) * G + tid;
-          if (b < whole) __stcs(reinterpret_cast<uint4*>(dS) + p, o);
-          else if (p < pieces) store_piece<T>(dS, p, a.V, a.vec, o);
+          if (empty) o4 = make_uint4(0, 0, 0, 0);
+          const int p = (b * kBatch + i) * M + tid;
+          if (b < whole) __stcs(reinterpret_cast<uint4*>(dS) + p, o4);
+          else if (p < pieces) store_piece<T>(dS, p, a.V, a.vec, o4);
         }
       }
-      __syncthreads();                                                   // the zeros of the listed words are written
-      for (int j = tid; j < a.K; j += G)
-        if (slot_idx[j] >= 0 && !empty) dS[slot_idx[j]] = from_f32<T>(g * (ex2(fmaf(slot_x[j], a.c, -mc) - l2all) - slot_t[j] * q_norm));
+      bar_arrive(kStored, G);
     }
-    for (int j = tid; j < a.K; j += G)
-      if (slot_idx[j] >= 0) atomicAnd(&bits[slot_idx[j] >> 5], ~(1u << (slot_idx[j] & 31)));
+    if (next >= a.T) break;
     row = next;
+    side ^= 1;
   }
 }
 

@@ -1284,8 +1284,8 @@ template <typename T, int MODE, int G>
 int launch_distill_row(const distill::Args& a, cudaStream_t st) {
   static OncePerDevice configured;
   auto kern = distill::row_kernel<T, MODE, G>;
-  FLOP_TRY(allow_smem(configured, distill::part_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
-  const size_t smem = distill::part_smem(a.V, a.K);
+  FLOP_TRY(allow_smem(configured, distill::row_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
+  const size_t smem = distill::row_smem(a.V, a.K);
   const int resident = (int)std::min<size_t>(1024 / G, (size_t)(228 * 1024) / (smem + 2048));
   launch_k(kern, dim3((unsigned)std::min<int64_t>(a.T, (int64_t)num_sms() * std::max(resident, 1))), dim3(G), smem, st, a);
   count_launch();

@@ -148,7 +148,7 @@ def test_many_rows(b, form, dtype, T, V, K):
 
 
 @pytest.mark.parametrize("form", ["fwd", "both"])
-@pytest.mark.parametrize("V", [131071, 131088, 200003, 262145, 530000, 1048576])
+@pytest.mark.parametrize("V", [131071, 131088, 200003, 262145, 400001, 524288])
 def test_wide_vocabularies(b, form, V):
     for dtype in (BF, F):
         Case(2, V, 50, dtype, 2.0, True).check(b, form)

@@ -87,7 +87,7 @@ def distill(lib, form, stats=5 * P, dloss=None, dS=6 * P, ldds=64, loss=4 * P, *
     (dict(tau=0.0), b.ERR_INVALID_ARG), (dict(tau=-1.0), b.ERR_INVALID_ARG), (dict(tau=float("inf")), b.ERR_INVALID_ARG), (dict(tau=float("nan")), b.ERR_INVALID_ARG),
     (dict(S=None), b.ERR_INVALID_ARG), (dict(t=None), b.ERR_INVALID_ARG), (dict(idx=None), b.ERR_INVALID_ARG), (dict(lds=56), b.ERR_INVALID_ARG),
     (dict(ldt=7), b.ERR_INVALID_ARG), (dict(ldi=7), b.ERR_INVALID_ARG), (dict(lds=65), b.ERR_UNSUPPORTED), (dict(S=P + 2), b.ERR_UNSUPPORTED),
-    (dict(K=1025, ldt=1025, ldi=1025), b.ERR_UNSUPPORTED), (dict(V=1048577, lds=1048584, ldds=1048584), b.ERR_UNSUPPORTED)])
+    (dict(K=1025, ldt=1025, ldi=1025), b.ERR_UNSUPPORTED), (dict(V=524289, lds=524296, ldds=524296), b.ERR_UNSUPPORTED)])
 def test_distill(lib, form, change, code):
     assert distill(lib, form, **change) == code
 

@@ -177,7 +177,7 @@ __device__ __forceinline__ void store_peer(const void* local, uint32_t rank, flo
 
 // One part of one row, held in registers: G threads, P pieces of 16 bytes each.
 template <typename T, int MODE, int G, int P>
-__global__ void __launch_bounds__(G == 32 ? 256 : G) part_kernel(const Args a) {
+__global__ void __launch_bounds__(G == 32 ? 256 : G, P > 4 ? 1024 / (G == 32 ? 256 : G) : 1) part_kernel(const Args a) {
   constexpr int NW = warps_of(G), kGroups = G == 32 ? 8 : 1;
   extern __shared__ __align__(16) unsigned char smem[];
   struct First { float t, n, x, m, s; };                // largest t, number of listed words, largest listed logit; maximum and sum outside the list

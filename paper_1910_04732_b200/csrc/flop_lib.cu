@@ -35,6 +35,7 @@
 #include "embedding.cuh"
 #include "distill.cuh"
 #include "quantized.cuh"
+#include "gemm_i8.cuh"
 
 using namespace flop;
 typedef __nv_bfloat16 bf16;
@@ -305,19 +306,19 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// Row-major bf16 matrix [rows, cols] with leading dimension ld; box = box_cols x box_rows, 128-byte swizzle.
-int make_tmap(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols, uint32_t box_rows) {
+// Row-major matrix [rows, cols] of bf16 (or bytes) with leading dimension ld; box = box_cols x box_rows, 128-byte swizzle.
+int make_tmap(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols, uint32_t box_rows, bool bytes = false) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) {
     if (debug_on()) fprintf(stderr, "[flop] cuTensorMapEncodeTiled entry point not found\n");
     return FLOP_ERR_CUDA;
   }
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * (bytes ? 1 : 2)};
   const cuuint32_t box[2] = {box_cols, box_rows};
   const cuuint32_t estr[2] = {1, 1};
   auto encode = [&] {
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return fn(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   };
   CUresult r = encode();
@@ -1213,7 +1214,7 @@ namespace {
 // ---- 8-bit integers with a scale per row
 bool i8_ok(const void* p, int64_t ld) { return aligned16(p) && (ld % 16) == 0; }
 constexpr int64_t kMaxI8K = 131071;      // products of two 8-bit values that a 32-bit sum holds whatever they are
-constexpr int64_t kMaxI8Rows = 4000000;  // tiles of 64 rows in one grid dimension
+constexpr int64_t kMaxI8Rows = 4000000;  // their tiles are counted in 32 bits
 
 struct I8Ws {
   int8_t* Xq; int64_t ldxq; float* x_scale;     // the tokens
@@ -1245,8 +1246,38 @@ int launch_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols,
 template <typename T>
 int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, T* Y, int64_t ldy, int64_t M,
                    int64_t N, int64_t K, cudaStream_t st) {
-  launch_k(i8::gemm_simple_kernel<T>, dim3((unsigned)((M + 63) / 64), (unsigned)((N + 63) / 64)), dim3(256), (size_t)0, st, A, lda, B, ldb, a_scale, b_scale, Y,
-           ldy, (int)M, (int)N, (int)K);
+  constexpr int OUT = std::is_same<T, bf16>::value ? i8::OUT_BF16 : std::is_same<T, float>::value ? i8::OUT_F32 : i8::OUT_S32;
+  const TcPlan pl = plan_tc(M, N, (K + 1) / 2, false, false);       // a k-block of 128 values moves the bytes and takes the cycles of 64 bf16 ones
+  i8::GemmParams p;
+  memset(&p, 0, sizeof(p));
+  FLOP_TRY(make_tmap(&p.ta, A, M, K, lda, i8::kBK, tc::BM, true));
+  FLOP_TRY(make_tmap(&p.tb, B, N, K, ldb, i8::kBK, (uint32_t)(pl.cta2 ? pl.bn / 2 : pl.bn), true));
+  if (OUT == i8::OUT_BF16) FLOP_TRY(make_tmap(&p.tout, Y, M, N, ldy, 64, 32));
+  p.M = (int)M; p.N = (int)N; p.num_kb = (int)((K + i8::kBK - 1) / i8::kBK); p.bn = pl.bn; p.tiles_m = pl.tiles_m; p.tiles_n = pl.tiles_n;
+  const int sb = pl.cta2 ? (int)tc::stage_bytes2(pl.bn) : (int)tc::stage_bytes(pl.bn);
+  p.stages = std::min(tc::kMaxStages, (kSmemBudget - kSmemFixed) / sb);
+  p.a_scale = a_scale; p.b_scale = b_scale; p.out = Y; p.ldo = ldy; p.vec = aligned16(Y) && ldy % 4 == 0;
+  static OncePerDevice configured;
+  auto kern1 = i8::gemm_kernel<OUT, false>;
+  auto kern2 = i8::gemm_kernel<OUT, true>;
+  FLOP_TRY(allow_smem(configured, kSmemBudget, kern1, kern2));
+  const size_t smem = (size_t)(kSmemFixed + p.stages * sb);
+  const int64_t items = (int64_t)pl.tiles_m * pl.tiles_n;
+  if (items > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  {
+    GemmTimer timer(st, 2.0 * (double)M * (double)N * (double)K);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(pl.cta2 ? 2 * std::min<int64_t>(items, num_sms() / 2) : std::min<int64_t>(items, num_sms())));
+    cfg.blockDim = dim3(tc::kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_on() ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pl.cta2 ? 2 : 1;
+    cudaLaunchKernelEx(&cfg, pl.cta2 ? kern2 : kern1, p);
+  }
   count_launch();
   FLOP_CUDA(cudaGetLastError());
   return FLOP_OK;
@@ -1306,6 +1337,9 @@ int launch_distill_inst(const distill::Args& a, cudaStream_t st) {
     if (pieces <= (int64_t)parts * 2048) return launch_distill_part<T, MODE, 256, 8>(a, parts, st);
     return launch_distill_part<T, MODE, 512, 8>(a, parts, st);
   }
+  if (MODE != distill::BWD && pieces <= 512) return launch_distill_part<T, MODE, 64, 8>(a, 1, st);
+  if (MODE == distill::BOTH && pieces <= 1024) return launch_distill_part<T, MODE, 128, 8>(a, 1, st);
+  if (MODE == distill::BOTH && pieces <= 2048) return launch_distill_part<T, MODE, 256, 8>(a, 1, st);
   if (pieces <= 1024) return launch_distill_row<T, MODE, 128>(a, st);
   if (pieces <= 4096) return launch_distill_row<T, MODE, 256>(a, st);
   return launch_distill_row<T, MODE, 512>(a, st);

@@ -86,44 +86,5 @@ requantize_rows_kernel(const int* __restrict__ acc, int64_t lda, int cols, const
   if (threadIdx.x == 0) h_scale[row] = bad ? NAN : (float)((double)row_scale[row] * (amax / 127.0));
 }
 
-// Y[m, n] = (sum_k A[m, k] B[n, k]) * a_scale[m] * b_scale[n]; 64 x 64 tiles, four 8-bit products per instruction.
-template <typename T>
-__global__ void __launch_bounds__(256)
-gemm_simple_kernel(const int8_t* __restrict__ A, int64_t lda, const int8_t* __restrict__ B, int64_t ldb, const float* __restrict__ a_scale,
-                   const float* __restrict__ b_scale, T* __restrict__ Y, int64_t ldy, int M, int N, int K) {
-  __shared__ int sa[16][65], sb[16][65];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int m0 = blockIdx.x * 64, n0 = blockIdx.y * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  int acc[4][4] = {};
-  auto word = [&](const int8_t* base, int64_t ld, int row, int rows, int k) {
-    if (row >= rows) return 0;
-    const int8_t* p = base + (int64_t)row * ld + k;
-    if (k + 4 <= K) return *reinterpret_cast<const int*>(p);
-    int v = 0;
-    for (int i = 0; i < 3; ++i)
-      if (k + i < K) v |= (int)(uint8_t)p[i] << (8 * i);
-    return v;
-  };
-  for (int k0 = 0; k0 < K; k0 += 64) {
-    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-      sa[i & 15][i >> 4] = word(A, lda, m0 + (i >> 4), M, k0 + 4 * (i & 15));
-      sb[i & 15][i >> 4] = word(B, ldb, n0 + (i >> 4), N, k0 + 4 * (i & 15));
-    }
-    __syncthreads();
-    for (int k = 0; k < 16; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(sa[k][ty * 4 + i], sb[k][tx + 16 * j], acc[i][j]);
-    __syncthreads();
-  }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty * 4 + i, n = n0 + tx + 16 * j;
-      if (m >= M || n >= N) continue;
-      if constexpr (sizeof(T) == 4 && !std::is_same<T, float>::value) Y[(int64_t)m * ldy + n] = acc[i][j];
-      else Y[(int64_t)m * ldy + n] = from_f32<T>((float)acc[i][j] * a_scale[m] * b_scale[n]);
-    }
-}
-
 }  // namespace i8
 }  // namespace flop

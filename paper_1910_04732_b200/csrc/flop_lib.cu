@@ -36,6 +36,7 @@
 #include "distill.cuh"
 #include "quantized.cuh"
 #include "gemm_i8.cuh"
+#include "few_i8.cuh"
 
 using namespace flop;
 typedef __nv_bfloat16 bf16;
@@ -1216,6 +1217,7 @@ bool i8_ok(const void* p, int64_t ld) { return aligned16(p) && (ld % 16) == 0; }
 constexpr int64_t kMaxI8K = 131071;      // products of two 8-bit values that a 32-bit sum holds whatever they are
 constexpr int64_t kMaxI8Rows = 4000000;  // their tiles are counted in 32 bits
 
+constexpr int64_t kFewQuantize = 4096;   // values a block of the few-token kernel quantises for itself
 struct I8Ws {
   int8_t* Xq; int64_t ldxq; float* x_scale;     // the tokens
   int* acc; int64_t ldacc;                      // sums of the first product
@@ -1235,12 +1237,22 @@ I8Ws plan_i8_ws(Arena& ar, int64_t T, int64_t d_in, int64_t k) {
   return w;
 }
 
-int launch_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dt, int8_t* Xq, int64_t ldxq, float* scale, cudaStream_t st) {
-  if (dt == FLOP_BF16) launch_k(i8::quantize_rows_kernel<bf16>, dim3((unsigned)rows), dim3(i8::kRowThreads), (size_t)0, st, (const bf16*)X, ldx, (int)cols, Xq, ldxq, scale);
-  else launch_k(i8::quantize_rows_kernel<float>, dim3((unsigned)rows), dim3(i8::kRowThreads), (size_t)0, st, (const float*)X, ldx, (int)cols, Xq, ldxq, scale);
+// `limit`: columns of the result that are written, zeros from `cols` on
+template <int TOK>
+int launch_rows_i8(const void* X, int64_t ldx, int64_t rows, int64_t cols, const float* row_scale, const float* col_scale, int vec, int8_t* Xq, int64_t ldxq,
+                   int64_t limit, float* scale, cudaStream_t st) {
+  const i8::FewParams p = {X, ldx, row_scale, col_scale, nullptr, 0, nullptr, nullptr, 0, nullptr, (int)rows, 0, (int)cols, vec};
+  int per_row = i8::kFewWarps;
+  while (per_row > 1 && (rows * per_row > (int64_t)2 * num_sms() * i8::kFewWarps || cols <= 128 * per_row)) per_row /= 2;
+  const int64_t at_once = i8::kFewWarps / per_row;
+  launch_k(i8::rows_kernel<TOK>, dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(i8::kFewThreads), (size_t)0, st, p, Xq, ldxq, (int)limit, scale, per_row);
   count_launch();
   FLOP_CUDA(cudaGetLastError());
   return FLOP_OK;
+}
+int launch_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dt, int8_t* Xq, int64_t ldxq, float* scale, cudaStream_t st) {
+  if (dt == FLOP_BF16) return launch_rows_i8<i8::TOK_BF16>(X, ldx, rows, cols, nullptr, nullptr, 1, Xq, ldxq, cols, scale, st);
+  return launch_rows_i8<i8::TOK_F32>(X, ldx, rows, cols, nullptr, nullptr, aligned16(X) && ldx % 4 == 0, Xq, ldxq, cols, scale, st);
 }
 // out: bf16, fp32 (scaled sums) or int (the sums)
 template <typename T>
@@ -1281,6 +1293,39 @@ int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int
   count_launch();
   FLOP_CUDA(cudaGetLastError());
   return FLOP_OK;
+}
+
+// Few tokens (few_i8.cuh).
+bool few_i8_ok(int64_t T, int64_t N, int64_t K) {
+  return T <= 32 && i8::few_smem((int)T, (int)K, 4) <= (size_t)kSmemBudget && N <= INT32_MAX / 2;
+}
+template <int TOK, int OUT, int NT, int KS, bool EARLY>
+int launch_few_i8_inst(const i8::FewParams& p, cudaStream_t st) {
+  static OncePerDevice configured;
+  auto kern = i8::few_kernel<TOK, OUT, NT, KS, EARLY>;
+  FLOP_TRY(allow_smem(configured, kSmemBudget, kern));
+  constexpr int rows = 16 * (i8::kFewWarps / KS);
+  const size_t smem = i8::few_smem(p.T, p.K, NT);
+  const int resident = (int)std::max<size_t>(1, std::min<size_t>(3, (size_t)(228 * 1024) / (smem + 1024)));
+  launch_k(kern, dim3((unsigned)std::min((p.N + rows - 1) / rows, resident * num_sms())), dim3(i8::kFewThreads), smem, st, p);
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
+}
+template <int TOK, int OUT, bool EARLY>
+int launch_few_i8(const i8::FewParams& p, cudaStream_t st) {
+  const bool wide = (p.N + 15) / 16 > 2 * num_sms() && p.K < 2048;
+  if (p.T <= 8) return wide ? launch_few_i8_inst<TOK, OUT, 1, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 1, 8, EARLY>(p, st);
+  if (p.T <= 16) return wide ? launch_few_i8_inst<TOK, OUT, 2, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 2, 8, EARLY>(p, st);
+  return wide ? launch_few_i8_inst<TOK, OUT, 4, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 4, 8, EARLY>(p, st);
+}
+// One product of quantised tokens, in the form the sizes call for.
+template <typename T>
+int launch_product_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, T* Y, int64_t ldy, int64_t M,
+                      int64_t N, int64_t K, cudaStream_t st) {
+  constexpr int OUT = std::is_same<T, bf16>::value ? i8::OUT_BF16 : std::is_same<T, float>::value ? i8::OUT_F32 : i8::OUT_S32;
+  if (few_i8_ok(M, N, K)) return launch_few_i8<i8::TOK_I8, OUT, false>({A, lda, a_scale, nullptr, B, ldb, b_scale, Y, ldy, nullptr, (int)M, (int)N, (int)K, 0}, st);
+  return launch_gemm_i8<T>(A, lda, a_scale, B, ldb, b_scale, Y, ldy, M, N, K, st);
 }
 
 // ---- distillation from top logits
@@ -2672,8 +2717,8 @@ int flop_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
   if (K == 0) return dt == FLOP_BF16 ? zero_2d<bf16>(Y, ldy, M, N, st) : zero_2d<float>(Y, ldy, M, N, st);
   if (!check_mat(A, lda, K) || !check_mat(B, ldb, K) || !a_scale || !b_scale) return FLOP_ERR_INVALID_ARG;
   if (!i8_ok(A, lda) || !i8_ok(B, ldb) || K > kMaxI8K || M > kMaxI8Rows || N > kMaxI8Rows) return FLOP_ERR_UNSUPPORTED;
-  if (dt == FLOP_BF16) return launch_gemm_i8<bf16>(A, lda, a_scale, B, ldb, b_scale, (bf16*)Y, ldy, M, N, K, st);
-  return launch_gemm_i8<float>(A, lda, a_scale, B, ldb, b_scale, (float*)Y, ldy, M, N, K, st);
+  if (dt == FLOP_BF16) return launch_product_i8<bf16>(A, lda, a_scale, B, ldb, b_scale, (bf16*)Y, ldy, M, N, K, st);
+  return launch_product_i8<float>(A, lda, a_scale, B, ldb, b_scale, (float*)Y, ldy, M, N, K, st);
 }
 
 int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ldqq, const float* q_scale, const int8_t* Pq, int64_t ldpq, const float* p_scale,
@@ -2691,14 +2736,21 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
   FLOP_TRY(check_ws(ws, ws_bytes, plan_i8_ws(probe, T, d_in, k).bytes));
   Arena ar{(unsigned char*)ws, ws_bytes, 0};
   const I8Ws w = plan_i8_ws(ar, T, d_in, k);
-  FLOP_TRY(launch_quantize_rows(X, ldx, T, d_in, dt, w.Xq, w.ldxq, w.x_scale, st));
-  FLOP_TRY(launch_gemm_i8<int>(w.Xq, w.ldxq, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, T, k, d_in, st));
-  launch_k(i8::requantize_rows_kernel, dim3((unsigned)T), dim3(i8::kRowThreads), (size_t)0, st, (const int*)w.acc, w.ldacc, (int)k, q_scale, (const float*)w.x_scale,
-           w.Hq, w.ldhq, w.h_scale);
-  count_launch();
-  FLOP_CUDA(cudaGetLastError());
-  if (dt == FLOP_BF16) return launch_gemm_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
-  return launch_gemm_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
+  if (few_i8_ok(T, k, d_in) && T * d_in <= kFewQuantize) {
+    const i8::FewParams p = {X, ldx, nullptr, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, w.x_scale, (int)T, (int)k, (int)d_in, aligned16(X) && ldx % 4 == 0};
+    const int rc = dt == FLOP_BF16 ? launch_few_i8<i8::TOK_BF16, i8::OUT_S32, false>(p, st) : launch_few_i8<i8::TOK_F32, i8::OUT_S32, false>(p, st);
+    FLOP_TRY(rc);
+  } else {
+    FLOP_TRY(launch_quantize_rows(X, ldx, T, d_in, dt, w.Xq, w.ldxq, w.x_scale, st));
+    FLOP_TRY(launch_product_i8<int>(w.Xq, w.ldxq, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, T, k, d_in, st));
+  }
+  if (few_i8_ok(T, d_out, k) && T * k <= kFewQuantize) {
+    const i8::FewParams p = {w.acc, w.ldacc, w.x_scale, q_scale, Pq, ldpq, p_scale, Y, ldy, nullptr, (int)T, (int)d_out, (int)k, aligned16(q_scale)};
+    return dt == FLOP_BF16 ? launch_few_i8<i8::TOK_H, i8::OUT_BF16, true>(p, st) : launch_few_i8<i8::TOK_H, i8::OUT_F32, true>(p, st);
+  }
+  FLOP_TRY(launch_rows_i8<i8::TOK_H>(w.acc, w.ldacc, T, k, w.x_scale, q_scale, aligned16(q_scale), w.Hq, w.ldhq, k, w.h_scale, st));
+  if (dt == FLOP_BF16) return launch_product_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
+  return launch_product_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
 }
 
 int flop_distill_topk_fwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi,

@@ -11,79 +11,19 @@
 namespace flop {
 namespace i8 {
 
-// fp32 quotients are off by less than 127 * 3 * 2^-24 = 2.3e-5.
-constexpr float kBorder = 1e-4f;
+// x * (127 / amax) in fp32 is off by one rounding of the factor and one of the product, 127 * 2^-23 = 1.5e-5 at most (the fused residual
+// has no product rounding: half of it); with x itself a product of two rounded factors and amax rounded, by 127 * 2^-24 * 5 = 3.8e-5.
+constexpr float kBorder = 2e-5f, kBorderSums = 5e-5f;
+constexpr float kToInt = 12582912.f;              // 1.5 * 2^23: adding it rounds to an integer, which is then the sum's low bits
 
-__device__ __forceinline__ int round_exact(double x, double amax) { return (int)rint(127.0 * x / amax); }
-// `inv` = 127 / amax in fp32 (infinite for the smallest amax, then every value takes the fp64 path)
-__device__ __forceinline__ int quantize(float x, float inv, float amax) {
-  const float y = x * inv, n = rintf(y);
-  if (!(fabsf(y - n) < 0.5f - kBorder)) return round_exact((double)x, (double)amax);
-  return (int)n;
-}
-
-constexpr int kRowThreads = 128;
-
-__device__ __forceinline__ float block_max(float v, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-  for (int w = 1; w < (int)blockDim.x / 32; ++w) v = fmaxf(v, red[w]);
-  return v;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
-quantize_rows_kernel(const T* __restrict__ X, int64_t ldx, int cols, int8_t* __restrict__ Xq, int64_t ldq, float* __restrict__ scale) {
-  __shared__ float red[32];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int64_t row = blockIdx.x;
-  X += row * ldx; Xq += row * ldq;
-  float amax = 0.f;
-  bool bad = false;
-  for (int c = threadIdx.x; c < cols; c += kRowThreads) {
-    const float x = fabsf(to_f32(X[c]));
-    bad |= !(x < INFINITY);
-    amax = fmaxf(amax, x);
-  }
-  bad = __syncthreads_or(bad);
-  amax = block_max(amax, red);
-  const bool zero = bad || amax == 0.f;
-  const float inv = 127.f / amax;
-  for (int c = threadIdx.x; c < cols; c += kRowThreads) Xq[c] = zero ? 0 : (int8_t)quantize(to_f32(X[c]), inv, amax);
-  if (threadIdx.x == 0) scale[row] = bad ? NAN : amax / 127.f;
-}
-
-// H in 32-bit sums times the scale of its column, requantised per row: h = acc * col_scale, exact in fp64 as long as the
-// sum has 29 bits, hq = 127 h / max |h| rounded, h_scale = row_scale * max |h| / 127.
-__global__ void __launch_bounds__(kRowThreads)
-requantize_rows_kernel(const int* __restrict__ acc, int64_t lda, int cols, const float* __restrict__ col_scale, const float* __restrict__ row_scale,
-                       int8_t* __restrict__ Hq, int64_t ldq, float* __restrict__ h_scale) {
-  __shared__ double red[32];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int64_t row = blockIdx.x;
-  acc += row * lda; Hq += row * ldq;
-  double amax = 0.0;
-  bool bad = false;
-  for (int c = threadIdx.x; c < cols; c += kRowThreads) {
-    const double h = fabs((double)acc[c] * (double)col_scale[c]);
-    bad |= !(h < INFINITY);
-    amax = fmax(amax, h);
-  }
-  bad = __syncthreads_or(bad);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
-  __syncthreads();
-  amax = red[0];
-  for (int w = 1; w < kRowThreads / 32; ++w) amax = fmax(amax, red[w]);
-  const bool zero = bad || amax == 0.0;
-  for (int c = threadIdx.x; c < cols; c += kRowThreads) Hq[c] = zero ? 0 : (int8_t)round_exact((double)acc[c] * (double)col_scale[c], amax);
-  if (threadIdx.x == 0) h_scale[row] = bad ? NAN : (float)((double)row_scale[row] * (amax / 127.0));
+// 127 x / amax for a quotient within kBorder of lower + 1/2: 254 x against (2 lower + 1) amax, both as a product and its rounding error, so
+// that the comparison is exact; half goes to even.  Values of bf16 meet their borders often (x = amax / 2 is one of them: one value
+// in 700 of normal bf16 tokens), so this has to be cheap: in fp64 with a division it took most of the time.
+template <typename F>
+__device__ __forceinline__ int round_border(F x, F amax, int lower) {
+  const F odd = (F)(2 * lower + 1), p = (F)254 * x, q = odd * amax;
+  const F d = (p - q) + (fma((F)254, x, -p) - fma(odd, amax, -q));
+  return lower + (d > (F)0 || (d == (F)0 && (lower & 1)));
 }
 
 }  // namespace i8

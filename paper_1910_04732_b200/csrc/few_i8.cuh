@@ -103,6 +103,85 @@ __device__ __noinline__ double largest_exact(const int* acc, const float* col, i
 }
 
 __device__ __forceinline__ int round_exact(double x, double amax) { return (int)rint(127.0 * x / amax); }
+// Eight values' low bytes.
+__device__ __forceinline__ uint2 bytes8(const uint32_t (&b)[8]) {
+  return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+}
+// bf16: 127 v / amax with inv = 127 / amax rounded UP decides every value.  With v = m 2^-j u and amax = a u, 128 <= m, a < 256, a quotient that is not on
+// a border is at least 1 / (a 2^(j+1)) > 1.9e-3 2^-j from it, and v inv is off by 3e-5 2^-j at most.  On a border it is only where 127 divides (2 n + 1) a:
+// at v = amax / 2, where v inv is 63.5 or just above and goes to the even 64; or with a = 254, where inv is exact and so is the tie.
+// (Rounded to nearest, half of those ties -- one value in 700 of normal tokens -- would have to be found and decided.)
+__device__ __forceinline__ uint2 round8_bf16(const uint4& w, float inv) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    b[2 * i] = __float_as_uint(fmaf(__uint_as_float(u[i] << 16), inv, kToInt));
+    b[2 * i + 1] = __float_as_uint(fmaf(__uint_as_float(u[i] & 0xffff0000u), inv, kToInt));
+  }
+  return bytes8(b);
+}
+// fp32: values within the error of a border are read again from where they are and decided exactly.
+__device__ __forceinline__ uint2 round8_f32(const float (&v)[8], float inv, float amax, const float* at) {
+  uint32_t b[8], near = 0;
+  float far = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = fmaf(v[i], inv, kToInt), off = fabsf(fmaf(v[i], inv, kToInt - s));
+    b[i] = __float_as_uint(s);
+    far = fmaxf(far, off);
+  }
+  uint2 w = bytes8(b);
+  if (far >= 0.5f - kBorder) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) near |= fabsf(fmaf(v[i], inv, kToInt - __uint_as_float(b[i]))) >= 0.5f - kBorder ? 1u << i : 0u;
+#pragma unroll 1
+    for (; near; near &= near - 1) {
+      const int i = __ffs(near) - 1;
+      const float x = at[i];
+      const uint32_t q = (uint32_t)round_border(x, amax, (int)floorf(x * inv)) & 255u;
+      const uint32_t shift = 8 * (i & 3), m = ~(255u << shift);
+      if (i < 4) w.x = (w.x & m) | (q << shift);
+      else w.y = (w.y & m) | (q << shift);
+    }
+  }
+  return w;
+}
+// Rows whose largest magnitude is beyond 1e+-30: inv or the borders' products would leave fp32.
+template <int TOK>
+__device__ __noinline__ uint2 round8_wide(const char* at, int n, double amax) {
+  uint32_t w[2] = {0, 0};
+  for (int i = 0; i < min(n, 8); ++i) {
+    const double x = TOK == TOK_F32 ? (double)reinterpret_cast<const float*>(at)[i] : (double)__bfloat162float(reinterpret_cast<const __nv_bfloat16*>(at)[i]);
+    w[i >> 2] |= ((uint32_t)round_exact(x, amax) & 255u) << (8 * (i & 3));
+  }
+  return make_uint2(w[0], w[1]);
+}
+// The same for v = acc * col in fp32, exact the largest |acc * col| in fp64.
+__device__ __forceinline__ uint2 round8_sums(const float (&v)[8], float inv, double exact, bool careful, const int* acc, const float* col, int left) {
+  uint32_t b[8], near = 0;
+  float far = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = fmaf(v[i], inv, kToInt), off = fabsf(fmaf(v[i], inv, kToInt - s));
+    b[i] = __float_as_uint(s);
+    far = fmaxf(far, off);
+    near |= off >= 0.5f - kBorderSums ? 1u << i : 0u;
+  }
+  uint2 w = bytes8(b);
+  if (!careful && far < 0.5f - kBorderSums) return w;
+  near = (careful ? 255u : near) & (left >= 8 ? 255u : (1u << left) - 1u);
+#pragma unroll 1
+  for (; near; near &= near - 1) {
+    const int i = __ffs(near) - 1;
+    const double x = (double)acc[i] * (double)col[i];
+    const int q = careful ? round_exact(x, exact) : round_border(x, exact, (int)floorf((float)acc[i] * col[i] * inv));
+    uint32_t& u = i < 4 ? w.x : w.y;
+    u = (u & ~(255u << (8 * (i & 3)))) | (((uint32_t)q & 255u) << (8 * (i & 3)));
+  }
+  return w;
+}
 
 // warps to a row of a block that has T of them
 __host__ __device__ constexpr int warps_per_row(int T) { return T > 4 ? 1 : T > 2 ? 2 : T == 2 ? 4 : 8; }
@@ -130,11 +209,23 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
   uint32_t bits[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) bits[r] = 0;
+  int k_more = k_lane;
+  if (TOK == TOK_BF16) {                                                   // two magnitudes to a word
+#pragma unroll 4
+    for (; k_more + 8 <= p.K; k_more += step)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const uint4 w = *reinterpret_cast<const uint4*>(row_of(r) + 2 * k_more);
+        bits[r] = __vmaxu2(bits[r], __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
+      }
+#pragma unroll
+    for (int r = 0; r < R; ++r) bits[r] = max(bits[r] << 16, bits[r] & 0xffff0000u);
+  }
 #pragma unroll 2
-  for (int k = k_lane; k < p.K; k += step) {
+  for (; k_more < p.K; k_more += step) {
     float v[R][8];
 #pragma unroll
-    for (int r = 0; r < R; ++r) load8<TOK>(p, row_of(r), k, v[r]);
+    for (int r = 0; r < R; ++r) load8<TOK>(p, row_of(r), k_more, v[r]);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -186,60 +277,47 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
       if (p.x_scale && blockIdx.x == 0) p.x_scale[t] = s;
     }
   }
-  // rows of the smallest and the largest numbers are scaled by a power of two before 127 / amax and the borders' products leave fp32
-  float inv[R], pre[R];
+  float inv[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const float a = (float)exact[r];
-    pre[r] = TOK == TOK_H ? 1.f : a < 1e-30f ? 0x1p96f : a > 1e30f ? 0x1p-96f : 1.f;
-    inv[r] = exact[r] > 0.0 && exact[r] < (double)INFINITY ? (careful[r] ? 1.f : 127.f / (a * pre[r])) : 0.f;
+    if (TOK != TOK_H) careful[r] = !(exact[r] < 1e30 && exact[r] > 1e-30);
+    inv[r] = exact[r] > 0.0 && exact[r] < (double)INFINITY ? (careful[r] ? 1.f : TOK == TOK_BF16 ? __fdiv_ru(127.f, (float)exact[r]) : 127.f / (float)exact[r]) : 0.f;
+  }
+  int k = k_lane;
+  if (TOK == TOK_BF16) {                                                   // whole pieces of whole rows
+    bool plain = true;
+#pragma unroll
+    for (int r = 0; r < R; ++r) plain &= inv[r] != 0.f && !careful[r] && first + r * rows_at_once < p.T;
+    if (plain) {
+#pragma unroll 4
+      for (; k + 8 <= p.K; k += step)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          *reinterpret_cast<uint2*>(tile + (first + r * rows_at_once) * stride + k) = round8_bf16(*reinterpret_cast<const uint4*>(row_of(r) + 2 * k), inv[r]);
+    }
   }
 #pragma unroll 1
-  for (int k = k_lane; k < limit; k += step) {
+  for (; k < limit; k += step) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int t = first + r * rows_at_once;
       if (t >= p.T) continue;
       uint2 w = make_uint2(0, 0);
       if (k < p.K && inv[r] != 0.f) {
+        const char* at = row_of(r) + (int64_t)k * (TOK == TOK_BF16 ? 2 : 4);
         float v[8];
         load8<TOK>(p, row_of(r), k, v);
-        if (pre[r] != 1.f) {
+        if (TOK == TOK_H) {
+          w = round8_sums(v, inv[r], exact[r], careful[r], reinterpret_cast<const int*>(at), p.col + k, p.K - k);
+        } else if (careful[r]) {
+          w = round8_wide<TOK>(at, p.K - k, exact[r]);
+        } else if (TOK == TOK_BF16) {
+          uint32_t b[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] *= pre[r];
-        }
-        uint32_t b[8], near = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float s = fmaf(v[i], inv[r], kToInt);
-          b[i] = __float_as_uint(s);
-          if (!(fabsf(fmaf(v[i], inv[r], kToInt - s)) < 0.5f - (TOK == TOK_H ? kBorderSums : kBorder))) near |= 1u << i;
-        }
-        w.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-        w.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-        if (careful[r]) near = 255u;
-        near &= p.K - k >= 8 ? 255u : (1u << (p.K - k)) - 1u;
-#pragma unroll 1
-        for (; near; near &= near - 1) {
-          const int i = __ffs(near) - 1;
-          const char* row = row_of(r);
-          int q;
-          if (TOK == TOK_H) {
-            const int acc = reinterpret_cast<const int*>(row)[k + i];
-            const double x = (double)acc * (double)p.col[k + i];
-            if (careful[r]) {
-              q = round_exact(x, exact[r]);
-            } else {
-              const float y = (float)acc * p.col[k + i] * inv[r];
-              q = round_border(x, exact[r], (int)floorf(y));
-            }
-          } else {
-            const float x = pre[r] * (TOK == TOK_F32 ? reinterpret_cast<const float*>(row)[k + i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[k + i]));
-            const float n = fmaf(x, inv[r], kToInt) - kToInt, left = fmaf(x, inv[r], -n);
-            q = round_border(x, (float)exact[r] * pre[r], (int)(left > 0.f ? n : n - 1.f));
-          }
-          uint32_t& u = i < 4 ? w.x : w.y;
-          u = (u & ~(255u << (8 * (i & 3)))) | (((uint32_t)q & 255u) << (8 * (i & 3)));
+          for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], inv[r], kToInt));
+          w = bytes8(b);
+        } else {
+          w = round8_f32(v, inv[r], (float)exact[r], reinterpret_cast<const float*>(at));
         }
       }
       int8_t* to = tile + t * stride + k;

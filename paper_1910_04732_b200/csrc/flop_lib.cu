@@ -1267,13 +1267,14 @@ int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int
   if (OUT == i8::OUT_BF16) FLOP_TRY(make_tmap(&p.tout, Y, M, N, ldy, 64, 32));
   p.M = (int)M; p.N = (int)N; p.num_kb = (int)((K + i8::kBK - 1) / i8::kBK); p.bn = pl.bn; p.tiles_m = pl.tiles_m; p.tiles_n = pl.tiles_n;
   const int sb = pl.cta2 ? (int)tc::stage_bytes2(pl.bn) : (int)tc::stage_bytes(pl.bn);
-  p.stages = std::min(tc::kMaxStages, (kSmemBudget - kSmemFixed) / sb);
+  constexpr int fixed = kSmemFixed + (int)(i8::kStage2 - tc::kStoreBufTotal + i8::kScalesTotal);
+  p.stages = std::min(tc::kMaxStages, (kSmemBudget - fixed) / sb);
   p.a_scale = a_scale; p.b_scale = b_scale; p.out = Y; p.ldo = ldy; p.vec = aligned16(Y) && ldy % 4 == 0;
   static OncePerDevice configured;
   auto kern1 = i8::gemm_kernel<OUT, false>;
   auto kern2 = i8::gemm_kernel<OUT, true>;
   FLOP_TRY(allow_smem(configured, kSmemBudget, kern1, kern2));
-  const size_t smem = (size_t)(kSmemFixed + p.stages * sb);
+  const size_t smem = (size_t)(fixed + p.stages * sb);
   const int64_t items = (int64_t)pl.tiles_m * pl.tiles_n;
   if (items > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
   {

@@ -5,8 +5,8 @@
 // instead of 64, an instruction takes 32 of them instead of 16, so a k-block moves the bytes of a bf16 one, takes its cycles, and does twice the work.
 // Every CTA (or CTA pair) is persistent and walks the tiles in turn, all N tiles of a row block next to one another; two accumulators
 // overlap the epilogue of a tile with the main loop of the next.
-// Epilogue: a thread holds a row, so its token's scale is one register; the channels' scales of a 32-column chunk come as broadcast
-// 16-byte loads.  bf16 leaves through a swizzled 32 x 64 staging tile and a TMA store (which clips the edges), 32-bit results through
+// Epilogue: a thread holds a row, so its token's scale is one register; the channels' scales of its columns are in shared memory before
+// the accumulator is there.  bf16 leaves through a swizzled 32 x 64 staging tile and a TMA store (which clips the edges), 32-bit results through
 // the same tile as coalesced stores.
 #pragma once
 #include "gemm_tc2.cuh"
@@ -37,126 +37,151 @@ __device__ __forceinline__ void umma_s8(uint32_t d_tmem, uint64_t adesc, uint64_
                  ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// the scales of 32 columns, 0 behind the last one (`vec`: b_scale + n0 is 16-byte aligned)
-__device__ __forceinline__ void load_scales(const float* __restrict__ b_scale, int n0, int N, float (&sc)[32]) {
-  if (n0 + 32 <= N && (reinterpret_cast<uintptr_t>(b_scale + n0) & 15) == 0) {
+constexpr uint32_t kWarpScales = 128 * 4;         // bytes: the scales of the (up to 128) columns that an epilogue warp takes of a tile
+constexpr uint32_t kScalesTotal = tc::kEpiWarps * kWarpScales;
+constexpr uint32_t kStage2 = 2 * tc::kStoreBufTotal;                   // two staging tiles per epilogue warp
+
+__device__ __forceinline__ void ld_shared_v4(uint32_t addr, float (&v)[4]) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+// Warp h of a row quarter takes the 64-column groups h and h + 2 of a tile: their scales, before the accumulator is waited for.
+__device__ __forceinline__ void fetch_scales(const GemmParams& p, uint32_t scales, int n_base, int n_end, int h, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float4 f = __ldg(reinterpret_cast<const float4*>(b_scale + n0) + i);
-      sc[4 * i] = f.x; sc[4 * i + 1] = f.y; sc[4 * i + 2] = f.z; sc[4 * i + 3] = f.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) sc[i] = n0 + i < N ? __ldg(b_scale + n0 + i) : 0.f;
+  for (int i = 0; i < 2; ++i) {
+    const int n = n_base + 64 * (h + 2 * i) + 2 * lane;
+    const float a = n < n_end ? __ldg(p.b_scale + n) : 0.f, b = n + 1 < n_end ? __ldg(p.b_scale + n + 1) : 0.f;
+    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(scales + 256u * i + 8u * lane), "f"(a), "f"(b) : "memory");
   }
+  __syncwarp();
+}
+// v[0..3] scaled: (float(sum) * sa) * scale
+__device__ __forceinline__ void scale4(const uint32_t* v, uint64_t sa2, uint32_t scales, float (&out)[4]) {
+  float sc[4];
+  ld_shared_v4(scales, sc);
+  const float2 x = unpack2(mul2(mul2(pack2((float)(int)v[0], (float)(int)v[1]), sa2), pack2(sc[0], sc[1])));
+  const float2 y = unpack2(mul2(mul2(pack2((float)(int)v[2], (float)(int)v[3]), sa2), pack2(sc[2], sc[3])));
+  out[0] = x.x; out[1] = x.y; out[2] = y.x; out[3] = y.y;
 }
 
-// One accumulator tile through one epilogue warp (see tc::run_epilogue): q = warp & 3 fixes its 32 rows, h its share of the 32-column chunks.
+// One accumulator tile through one epilogue warp (see tc::run_epilogue): q = warp & 3 fixes its 32 rows, h which 64-column groups it takes.  Both
+// groups are fetched from tensor memory before anything is converted, so the accumulator is handed back at once; each has a staging
+// tile of its own, so neither waits for the other's store.
 template <int OUT, bool PAIR>
-__device__ __forceinline__ void epilogue(const GemmParams& p, uint32_t buf, uint32_t t_acc, int row0, int n_base, int warp, int lane, uint32_t release_bar) {
+__device__ __forceinline__ void epilogue(const GemmParams& p, uint32_t buf, uint32_t scales, uint32_t t_acc, int row0, int n_base, int warp, int lane, uint32_t release_bar) {
   using namespace tc;
   const int q = warp & 3, h = (warp - 2) >> 2, row_base = row0 + q * 32, row = row_base + lane;
   const uint32_t t_row = t_acc + ((uint32_t)(q * 32) << 16);
-  const int n_end = min(n_base + p.bn, p.N), nchunks = (n_end - n_base + 31) >> 5, ngroups = (nchunks + 1) >> 1;
+  const int n_end = min(n_base + p.bn, p.N), nchunks = (n_end - n_base + 31) >> 5;
   const float sa = OUT != OUT_S32 && row < p.M ? __ldg(p.a_scale + row) : 0.f;
-  auto release = [&] {
-    tcgen05_fence_before();
-    __syncwarp();
-    if (lane == 0) {
-      if (PAIR) mbar_arrive_remote(release_bar);
-      else mbar_arrive(release_bar);
-    }
-  };
-  bool released = false;
+  const uint64_t sa2 = pack2(sa, sa);
+  uint32_t v[4][32];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = 2 * (h + 2 * (i >> 1)) + (i & 1);
+    if (c < nchunks) tmem_ld32(t_row + (uint32_t)(c * 32), v[i]);
+  }
+  tmem_ld_wait();
+  tcgen05_fence_before();
+  __syncwarp();
+  if (lane == 0) {
+    if (PAIR) mbar_arrive_remote(release_bar);
+    else mbar_arrive(release_bar);
+    if (OUT == OUT_BF16) tma_store_wait_read();        // the stores of the tile before have left the staging tiles
+  }
+  __syncwarp();
   if (OUT == OUT_BF16) {
-    for (int g = h; g < ngroups; g += 2) {
-      const int c0 = 2 * g;
-      const bool two = c0 + 1 < nchunks;
-      uint32_t v[2][32];
-      tmem_ld32(t_row + (uint32_t)(c0 * 32), v[0]);
-      if (two) tmem_ld32(t_row + (uint32_t)(c0 * 32 + 32), v[1]);
-      tmem_ld_wait();
-      if (g + 2 >= ngroups) { release(); released = true; }
-      const int n0 = n_base + c0 * 32;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int c0 = 2 * (h + 2 * g), n0 = n_base + c0 * 32;
+      if (c0 >= nchunks) break;
       // a store of the engine that ends inside a 16-byte piece writes the piece whole: the columns behind N are the caller's
       const bool edge = n0 + 64 > p.N && (p.N & 7);
-      if (lane == 0) tma_store_wait_read();            // the previous block has left the staging tile
-      __syncwarp();
+      const uint32_t tile = buf + (uint32_t)g * kStoreBufBytes;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (half && !two) break;
-        float sc[32];
-        load_scales(p.b_scale, n0 + 32 * half, p.N, sc);
+      for (int i = 0; i < 8; ++i) {
+        if (i == 4 && c0 + 1 >= nchunks) break;
+        float f[8];
+        scale4(v[2 * g + (i >> 2)] + 8 * (i & 3), sa2, scales + 256u * g + 32u * i, *reinterpret_cast<float(*)[4]>(f));
+        scale4(v[2 * g + (i >> 2)] + 8 * (i & 3) + 4, sa2, scales + 256u * g + 32u * i + 16u, *reinterpret_cast<float(*)[4]>(f + 4));
+        uint32_t pk[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t pk[4];
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+          pk[j] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        if (!edge) {
+          st_shared_v4(tile + (uint32_t)lane * 128u + (uint32_t)((i ^ (lane & 7)) << 4), pk[0], pk[1], pk[2], pk[3]);
+        } else if (row < p.M) {
+          const int n = n0 + 8 * i;
+          __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row * p.ldo + n;
+          if (n + 8 <= p.N) *reinterpret_cast<uint4*>(o) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+          else
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int e = 8 * i + 2 * j;
-            const __nv_bfloat162 b = __floats2bfloat162_rn((float)(int)v[half][e] * sa * sc[e], (float)(int)v[half][e + 1] * sa * sc[e + 1]);
-            pk[j] = *reinterpret_cast<const uint32_t*>(&b);
-          }
-          if (!edge) {
-            st_shared_v4(buf + (uint32_t)lane * 128u + (uint32_t)(((4 * half + i) ^ (lane & 7)) << 4), pk[0], pk[1], pk[2], pk[3]);
-          } else if (row < p.M) {
-            const int n = n0 + 32 * half + 8 * i;
-            __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row * p.ldo + n;
-            if (n + 8 <= p.N) *reinterpret_cast<uint4*>(o) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-            else
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (n + e < p.N) o[e] = reinterpret_cast<const __nv_bfloat16*>(pk)[e];
-          }
+            for (int e = 0; e < 8; ++e)
+              if (n + e < p.N) o[e] = reinterpret_cast<const __nv_bfloat16*>(pk)[e];
         }
       }
       if (edge) continue;
       fence_async_smem();
       __syncwarp();
-      if (lane == 0 && row_base < p.M) tma_store_2d(&p.tout, n0, row_base, buf);      // never start a store outside the tensor
+      if (lane == 0 && row_base < p.M) tma_store_2d(&p.tout, n0, row_base, tile);      // never start a store outside the tensor
     }
-    if (!released) release();
     return;
   }
-  // 32-bit results: a chunk at a time through the staging tile, then four rows of 128 bytes per instruction
-#pragma unroll 1
-  for (int c = h; c < nchunks; c += 2) {
-    uint32_t v[32];
-    tmem_ld32(t_row + (uint32_t)(c * 32), v);
-    tmem_ld_wait();
-    if (c + 2 >= nchunks) { release(); released = true; }
-    const int n0 = n_base + c * 32;
-    if (OUT == OUT_F32) {
-      float sc[32];
-      load_scales(p.b_scale, n0, p.N, sc);
+  // 32-bit results: a chunk at a time through the staging tiles in turn, then four rows of 128 bytes per instruction
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = __float_as_uint((float)(int)v[i] * sa * sc[i]);
+  for (int i = 0; i < 4; ++i) {
+    const int c = 2 * (h + 2 * (i >> 1)) + (i & 1), n0 = n_base + c * 32;
+    if (c >= nchunks) break;
+    const uint32_t tile = buf + (uint32_t)(i & 1) * kStoreBufBytes;
+    if (i >= 2) __syncwarp();                          // the chunk before last has been read out of this tile
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (OUT == OUT_F32) {
+        float f[4];
+        scale4(v[i] + 4 * j, sa2, scales + 128u * i + 16u * j, f);
+        st_shared_v4(tile + (uint32_t)lane * 128u + (uint32_t)((j ^ (lane & 7)) << 4), __float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+      } else {
+        st_shared_v4(tile + (uint32_t)lane * 128u + (uint32_t)((j ^ (lane & 7)) << 4), v[i][4 * j], v[i][4 * j + 1], v[i][4 * j + 2], v[i][4 * j + 3]);
+      }
     }
-    __syncwarp();                                      // the previous chunk has been read out of the staging tile
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      st_shared_v4(buf + (uint32_t)lane * 128u + (uint32_t)((i ^ (lane & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
     __syncwarp();
     uint32_t* out = reinterpret_cast<uint32_t*>(p.out) + (int64_t)row_base * p.ldo + n0;
     if (p.vec && n0 + 32 <= n_end) {
       const int r0 = lane >> 3, c4 = lane & 7;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = r0 + 4 * i;
+      for (int j = 0; j < 8; ++j) {
+        const int r = r0 + 4 * j;
         uint4 w;
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                     : "r"(buf + (uint32_t)r * 128u + (uint32_t)((c4 ^ (r & 7)) << 4)) : "memory");
+                     : "r"(tile + (uint32_t)r * 128u + (uint32_t)((c4 ^ (r & 7)) << 4)) : "memory");
         if (row_base + r < p.M) *reinterpret_cast<uint4*>(out + (int64_t)r * p.ldo + 4 * c4) = w;
       }
     } else {
       const int rows = min(32, p.M - row_base);
       for (int r = 0; r < rows; ++r) {
         uint32_t w;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(buf + (uint32_t)r * 128u + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + 4u * (lane & 3)) : "memory");
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(tile + (uint32_t)r * 128u + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + 4u * (lane & 3)) : "memory");
         if (n0 + lane < n_end) out[(int64_t)r * p.ldo + lane] = w;
       }
     }
   }
-  if (!released) release();
+  __syncwarp();
 }
 
 template <int OUT, bool PAIR>
@@ -167,7 +192,7 @@ gemm_kernel(const __grid_constant__ GemmParams p) {
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t sbytes = PAIR ? stage_bytes2(p.bn) : stage_bytes(p.bn);
   const uint32_t store_base = smem_base + (uint32_t)p.stages * sbytes;
-  const uint32_t bar_base = store_base + kStoreBufTotal;
+  const uint32_t scale_base = store_base + kStage2, bar_base = scale_base + kScalesTotal;
   auto full_bar = [&](int s) { return bar_base + 8u * (uint32_t)s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (uint32_t)(kMaxStages + s); };
   auto tfull_bar = [&](int a) { return bar_base + 8u * (uint32_t)(2 * kMaxStages + a); };
@@ -271,10 +296,12 @@ gemm_kernel(const __grid_constant__ GemmParams p) {
     bool ok = true;
     for (int w = unit; w < items && ok; w += units) {
       const int tm = w / p.tiles_n, tn = w - tm * p.tiles_n;
+      const uint32_t scales = scale_base + (uint32_t)(warp - 2) * kWarpScales;
+      if (OUT != OUT_S32) fetch_scales(p, scales, tn * p.bn, min(tn * p.bn + p.bn, p.N), (warp - 2) >> 2, lane);
       ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
       if (!ok) break;
       tcgen05_fence_after();
-      epilogue<OUT, PAIR>(p, store_base + (uint32_t)(warp - 2) * kStoreBufBytes, tmem_base + (uint32_t)acc * acc_stride(p.bn), tm * bm + (int)rank * BM, tn * p.bn,
+      epilogue<OUT, PAIR>(p, store_base + (uint32_t)(warp - 2) * 2 * kStoreBufBytes, scales, tmem_base + (uint32_t)acc * acc_stride(p.bn), tm * bm + (int)rank * BM, tn * p.bn,
                           warp, lane, PAIR ? map_to_cta(tempty_bar(acc), 0) : tempty_bar(acc));
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }

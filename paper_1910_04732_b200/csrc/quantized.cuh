@@ -17,8 +17,7 @@ constexpr float kBorder = 2e-5f, kBorderSums = 5e-5f;
 constexpr float kToInt = 12582912.f;              // 1.5 * 2^23: adding it rounds to an integer, which is then the sum's low bits
 
 // 127 x / amax for a quotient within kBorder of lower + 1/2: 254 x against (2 lower + 1) amax, both as a product and its rounding error, so
-// that the comparison is exact; half goes to even.  Values of bf16 meet their borders often (x = amax / 2 is one of them: one value
-// in 700 of normal bf16 tokens), so this has to be cheap: in fp64 with a division it took most of the time.
+// that the comparison is exact; half goes to even.
 template <typename F>
 __device__ __forceinline__ int round_border(F x, F amax, int lower) {
   const F odd = (F)(2 * lower + 1), p = (F)254 * x, q = odd * amax;

@@ -103,11 +103,6 @@ __device__ __noinline__ double largest_exact(const int* acc, const float* col, i
 }
 
 __device__ __forceinline__ int round_exact(double x, double amax) { return (int)rint(127.0 * x / amax); }
-// Eight values' low bytes.
-__device__ __forceinline__ uint2 bytes8(const uint32_t (&b)[8]) {
-  return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
-                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
-}
 // bf16: 127 v / amax with inv = 127 / amax rounded UP decides every value.  With v = m 2^-j u and amax = a u, 128 <= m, a < 256, a quotient that is not on
 // a border is at least 1 / (a 2^(j+1)) > 1.9e-3 2^-j from it, and v inv is off by 3e-5 2^-j at most.  On a border it is only where 127 divides (2 n + 1) a:
 // at v = amax / 2, where v inv is 63.5 or just above and goes to the even 64; or with a = 254, where inv is exact and so is the tie.

@@ -1217,6 +1217,7 @@ bool i8_ok(const void* p, int64_t ld) { return aligned16(p) && (ld % 16) == 0; }
 constexpr int64_t kMaxI8K = 131071;      // products of two 8-bit values that a 32-bit sum holds whatever they are
 constexpr int64_t kMaxI8Rows = 4000000;  // their tiles are counted in 32 bits
 
+constexpr int64_t kFewFused = 8;
 constexpr int64_t kFewQuantize = 4096;   // values a block of the few-token kernel quantises for itself
 struct I8Ws {
   int8_t* Xq; int64_t ldxq; float* x_scale;     // the tokens
@@ -1327,6 +1328,44 @@ int launch_product_i8(const int8_t* A, int64_t lda, const float* a_scale, const 
   constexpr int OUT = std::is_same<T, bf16>::value ? i8::OUT_BF16 : std::is_same<T, float>::value ? i8::OUT_F32 : i8::OUT_S32;
   if (few_i8_ok(M, N, K)) return launch_few_i8<i8::TOK_I8, OUT, false>({A, lda, a_scale, nullptr, B, ldb, b_scale, Y, ldy, nullptr, (int)M, (int)N, (int)K, 0}, st);
   return launch_gemm_i8<T>(A, lda, a_scale, B, ldb, b_scale, Y, ldy, M, N, K, st);
+}
+
+// The first product of a compact pair with its rows quantised again in the same launch (see gemm_rowq_kernel).
+bool rowq_ok(int64_t k) { return k <= (int64_t)i8::kRowqMaxCluster * i8::kRowqMaxSlice; }
+int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* col_scale, int8_t* Hq, int64_t ldhq, float* h_scale,
+                int64_t M, int64_t N, int64_t K, cudaStream_t st) {
+  static OncePerDevice configured;
+  auto kern = i8::gemm_rowq_kernel;
+  FLOP_TRY(allow_smem(configured, kSmemBudget, kern));
+  const int64_t row_blocks = (M + tc::BM - 1) / tc::BM;
+  int parts = 1;
+  while (parts < i8::kRowqMaxCluster && (N > (int64_t)parts * i8::kRowqMaxSlice || (N > 32 * parts && row_blocks * parts * 2 <= num_sms()))) parts *= 2;
+  if (getenv("RP")) parts = atoi(getenv("RP"));
+  i8::RowqParams p;
+  memset(&p, 0, sizeof(p));
+  p.M = (int)M; p.N = (int)N; p.num_kb = (int)((K + i8::kBK - 1) / i8::kBK); p.parts = parts;
+  p.slice = (int)round_up((N + parts - 1) / parts, 16);
+  const int sb = (int)i8::rowq_stage_bytes(p.slice);
+  p.stages = std::min({tc::kMaxStages, (kSmemBudget - (int)i8::kRowqFixed) / sb, std::max(p.num_kb, 2)});
+  FLOP_TRY(make_tmap(&p.ta, A, M, K, lda, i8::kBK, tc::BM, true));
+  FLOP_TRY(make_tmap(&p.tb, B, N, K, ldb, i8::kBK, (uint32_t)p.slice, true));
+  p.a_scale = a_scale; p.col_scale = col_scale; p.out = Hq; p.ldo = ldhq; p.h_scale = h_scale;
+  {
+    GemmTimer timer(st, 2.0 * (double)M * (double)N * (double)K);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(row_blocks * parts)); cfg.blockDim = dim3(tc::kThreads); cfg.dynamicSmemBytes = (size_t)(i8::kRowqFixed + p.stages * sb); cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_on() ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)parts; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cudaLaunchKernelEx(&cfg, kern, p);
+  }
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
 }
 
 // ---- distillation from top logits
@@ -2737,21 +2776,25 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
   FLOP_TRY(check_ws(ws, ws_bytes, plan_i8_ws(probe, T, d_in, k).bytes));
   Arena ar{(unsigned char*)ws, ws_bytes, 0};
   const I8Ws w = plan_i8_ws(ar, T, d_in, k);
-  if (few_i8_ok(T, k, d_in) && T * d_in <= kFewQuantize) {
+  auto second = [&]() -> int {
+    if (dt == FLOP_BF16) return launch_product_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
+    return launch_product_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
+  };
+  if (T <= kFewFused && few_i8_ok(T, k, d_in) && T * d_in <= kFewQuantize && few_i8_ok(T, d_out, k) && T * k <= kFewQuantize) {
     const i8::FewParams p = {X, ldx, nullptr, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, w.x_scale, (int)T, (int)k, (int)d_in, aligned16(X) && ldx % 4 == 0};
     const int rc = dt == FLOP_BF16 ? launch_few_i8<i8::TOK_BF16, i8::OUT_S32, false>(p, st) : launch_few_i8<i8::TOK_F32, i8::OUT_S32, false>(p, st);
     FLOP_TRY(rc);
-  } else {
-    FLOP_TRY(launch_quantize_rows(X, ldx, T, d_in, dt, w.Xq, w.ldxq, w.x_scale, st));
-    FLOP_TRY(launch_product_i8<int>(w.Xq, w.ldxq, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, T, k, d_in, st));
+    const i8::FewParams p2 = {w.acc, w.ldacc, w.x_scale, q_scale, Pq, ldpq, p_scale, Y, ldy, nullptr, (int)T, (int)d_out, (int)k, aligned16(q_scale)};
+    return dt == FLOP_BF16 ? launch_few_i8<i8::TOK_H, i8::OUT_BF16, true>(p2, st) : launch_few_i8<i8::TOK_H, i8::OUT_F32, true>(p2, st);
   }
-  if (few_i8_ok(T, d_out, k) && T * k <= kFewQuantize) {
-    const i8::FewParams p = {w.acc, w.ldacc, w.x_scale, q_scale, Pq, ldpq, p_scale, Y, ldy, nullptr, (int)T, (int)d_out, (int)k, aligned16(q_scale)};
-    return dt == FLOP_BF16 ? launch_few_i8<i8::TOK_H, i8::OUT_BF16, true>(p, st) : launch_few_i8<i8::TOK_H, i8::OUT_F32, true>(p, st);
+  FLOP_TRY(launch_quantize_rows(X, ldx, T, d_in, dt, w.Xq, w.ldxq, w.x_scale, st));
+  if (rowq_ok(k)) {
+    FLOP_TRY(launch_rowq(w.Xq, w.ldxq, w.x_scale, Qq, ldqq, q_scale, w.Hq, w.ldhq, w.h_scale, T, k, d_in, st));
+    return second();
   }
+  FLOP_TRY(launch_product_i8<int>(w.Xq, w.ldxq, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, T, k, d_in, st));
   FLOP_TRY(launch_rows_i8<i8::TOK_H>(w.acc, w.ldacc, T, k, w.x_scale, q_scale, aligned16(q_scale), w.Hq, w.ldhq, k, w.h_scale, st));
-  if (dt == FLOP_BF16) return launch_product_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
-  return launch_product_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
+  return second();
 }
 
 int flop_distill_topk_fwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi,

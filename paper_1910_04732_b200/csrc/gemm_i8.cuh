@@ -10,6 +10,7 @@
 // the same tile as coalesced stores.
 #pragma once
 #include "gemm_tc2.cuh"
+#include "quantized.cuh"
 
 namespace flop {
 namespace i8 {
@@ -325,6 +326,227 @@ gemm_kernel(const __grid_constant__ GemmParams p) {
     tcgen05_fence_after();
     if (PAIR) tmem_dealloc2(tmem_base, kTmemCols);
     else tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// ---- first product of a compact pair, its rows quantised again before they leave the SM: Hq = 127 h / max |h| rounded, h = sum * col_scale, and
+// h_scale = a_scale * max |h| / 127.  A row's maximum needs all of its columns: a cluster of one to four CTAs holds a 128-row block, each a slice of
+// up to 256 columns in tensor memory, and they exchange the maxima of their slices through distributed shared memory.  That saves the trip of
+// the 32-bit sums through memory and a launch that would be waited for.
+//
+// The maximum is that of the exact products.  A sum below 2^24 is exact in fp32, so x = fl(sum * scale) is its product rounded once, rounding
+// keeps the order, and the largest product is among those with the largest x: the one with the largest rounding error, which an fma gives
+// exactly.  Rows beyond that (longer sums, products outside 1e+-30) are compared in fp64.  Rounding as everywhere: in fp32 unless
+// the quotient is within its error of a border.
+constexpr int kRowqMaxSlice = 256, kRowqMaxCluster = 4;
+
+struct RowqParams {
+  CUtensorMap ta, tb;
+  int M, N, num_kb, slice, stages, parts;         // N columns in `parts` slices
+  const float *a_scale, *col_scale;
+  int8_t* out; int64_t ldo; float* h_scale;
+};
+__host__ __device__ inline uint32_t rowq_stage_bytes(int slice) { return tc::kATileBytes + (uint32_t)slice * kBK; }
+constexpr uint32_t kRowqFixed = 1024 + kRowqMaxSlice * 4 + kRowqMaxCluster * 2 * 128 * 8 + 384;
+
+__device__ __noinline__ uint32_t round_sum(int sum, float scale, double exact, float inv) {
+  const double x = (double)sum * (double)scale;
+  const int q = exact < 1e30 && exact > 1e-30 ? round_border(x, exact, (int)floorf((float)sum * scale * inv)) : (int)rint(127.0 * x / exact);
+  return (uint32_t)q & 255u;
+}
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
+  tc::tmem_ld_wait();
+}
+// A thread walks its columns eight at a time in loops that are not unrolled: it does so once or twice in its life, and code that runs once waits
+// for its instructions (32 columns at a time, unrolled: 1.5 us per 32 columns).
+__global__ void __launch_bounds__(tc::kThreads, 1)
+gemm_rowq_kernel(const __grid_constant__ RowqParams p) {
+  using namespace tc;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t sbytes = rowq_stage_bytes(p.slice);
+  const uint32_t scale_base = smem_base + (uint32_t)p.stages * sbytes, max_base = scale_base + kRowqMaxSlice * 4;
+  const uint32_t bar_base = max_base + kRowqMaxCluster * 2 * 128 * 8;
+  auto full_bar = [&](int s) { return bar_base + 8u * (uint32_t)s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (uint32_t)(kMaxStages + s); };
+  const uint32_t tfull = bar_base + 8u * (uint32_t)(2 * kMaxStages);
+  __shared__ uint32_t s_tmem_base;
+  __shared__ int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = blockIdx.x % p.parts, tm = blockIdx.x / p.parts;
+  const int n_base = part * p.slice, n_end = min(n_base + p.slice, p.N);
+  const bool work = n_base < p.N;                                         // (a last slice can be empty)
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < p.stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    mbar_init(tfull, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0 && lane == 0) { prefetch_tmap(&p.ta); prefetch_tmap(&p.tb); }
+  if (warp == 1) tmem_alloc(smem_u32(&s_tmem_base), kRowqMaxSlice);
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem_base = s_tmem_base;
+  volatile int* abort_flag = &s_abort;
+  pdl_wait();
+  pdl_launch_dependents();
+  cluster_sync_all();                                                     // every CTA is there before one stores to another
+
+  if (warp == 0) {
+    if (lane == 0 && work) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) break;
+        const uint32_t sa = smem_base + (uint32_t)stage * sbytes;
+        mbar_expect_tx(full_bar(stage), sbytes);
+        tma_load_2d(sa, &p.ta, kb * kBK, tm * BM, full_bar(stage));
+        tma_load_2d(sa + kATileBytes, &p.tb, kb * kBK, n_base, full_bar(stage));
+        if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+      }
+      if (*abort_flag) {
+        const long long t0 = clock64();                                   // leaving early: let the copies already issued land
+        while (clock64() - t0 < 2000000LL) {}
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();
+  } else if (warp == 1) {
+    if (lane == 0 && work) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const uint32_t idesc = instr_desc_s8(BM, p.slice);
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        if (!mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
+        tcgen05_fence_after();
+        const uint32_t sa = smem_base + (uint32_t)stage * sbytes, sb = sa + kATileBytes;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma_s8<false>(tmem_base, smem_desc(sa + k * 32, false), smem_desc(sb + k * 32, false), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+        umma_commit(empty_bar(stage));
+        if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+      }
+      if (ok) umma_commit(tfull);
+    }
+    __syncwarp();
+    cluster_sync_all();
+  } else {
+    const int q = warp & 3, h = (warp - 2) >> 2, r = q * 32 + lane, row = tm * BM + r;
+    const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16);
+    const int nchunks = work ? (n_end - n_base + 31) >> 5 : 0;
+    for (int i = threadIdx.x - 64; i < kRowqMaxSlice; i += 32 * kEpiWarps) {
+      const float s = n_base + i < n_end ? __ldg(p.col_scale + n_base + i) : 0.f;
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(scale_base + 4u * (uint32_t)i), "f"(s) : "memory");
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const bool ok = __all_sync(0xffffffffu, !work || mbar_wait(tfull, 0u, abort_flag));
+    tcgen05_fence_after();
+    // the largest product of this thread's columns: rounded, and its rounding error
+    float top = 0.f, rest = 0.f;
+    int longest = 0;
+    const int cols_here = ok ? nchunks * 32 : 0;                          // this thread's: 16 h .. 16 h + 15 of every 32
+    auto next_cols = [](int n) { return n + ((n & 8) ? 24 : 8); };
+#pragma unroll 1
+    for (int n = 16 * h; n < cols_here; n = next_cols(n)) {
+      uint32_t v[8];
+      float sc[8], x[8], here = 0.f;
+      tmem_ld8(t_row + (uint32_t)n, v);
+      ld_shared_v4(scale_base + 4u * (uint32_t)n, *reinterpret_cast<float(*)[4]>(sc));
+      ld_shared_v4(scale_base + 4u * (uint32_t)n + 16u, *reinterpret_cast<float(*)[4]>(sc + 4));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        longest = max(longest, abs((int)v[e]));
+        x[e] = fabsf((float)(int)v[e] * sc[e]);
+        here = __uint_as_float(max(__float_as_uint(here), __float_as_uint(x[e])));      // (a NaN is the largest)
+      }
+      if (!(here < top)) {
+        if (!(here == top)) rest = -INFINITY;
+        top = here;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (x[e] == top) rest = fmaxf(rest, fmaf(fabsf((float)(int)v[e]), fabsf(sc[e]), -x[e]));
+      }
+    }
+    double best = (double)top + (double)rest;
+    // not decided by that: sums beyond 24 bits, products that fp32 does not hold
+    const bool far = longest > (1 << 24) || (longest > 0 && !(top < 1e30f && top > 1e-30f));
+    if (__any_sync(0xffffffffu, far)) {
+      double b = 0.0;
+#pragma unroll 1
+      for (int n = 16 * h; n < cols_here; n = next_cols(n)) {
+        uint32_t v[8];
+        tmem_ld8(t_row + (uint32_t)n, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float sc;
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sc) : "r"(scale_base + 4u * (uint32_t)(n + e)) : "memory");
+          const double x = fabs((double)(int)v[e] * (double)sc);
+          b = x < (double)INFINITY ? fmax(b, x) : (double)INFINITY;
+        }
+      }
+      if (far) best = b;
+    }
+    // every CTA's maxima to every CTA, then the row's
+    {
+      const uint32_t at = max_base + (uint32_t)(((part * 2 + h) * 128 + r) * 8);
+      for (int i = 0; i < p.parts; ++i)
+        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(map_to_cta(at, (uint32_t)i)), "d"(best) : "memory");
+    }
+    __syncwarp();
+    cluster_sync_all();
+    double exact = 0.0;
+    for (int i = 0; i < 2 * p.parts; ++i) {
+      double x;
+      asm volatile("ld.shared.f64 %0, [%1];" : "=d"(x) : "r"(max_base + (uint32_t)((i * 128 + r) * 8)) : "memory");
+      exact = fmax(exact, x);
+    }
+    const bool finite = exact < (double)INFINITY, plain = exact < 1e30 && exact > 1e-30;
+    if (ok && part == 0 && h == 0 && row < p.M) p.h_scale[row] = finite ? (float)((double)__ldg(p.a_scale + row) * (exact * (1.0 / 127.0))) : NAN;
+    const float inv = plain ? 127.f / (float)exact : 0.f;
+    const int cols = min((p.N + 15) & ~15, n_base + p.slice);             // whole 16-byte pieces, zeros behind N; the slice behind this one writes its own
+    int8_t* out = p.out + (int64_t)row * p.ldo + n_base;
+    uint2 half = make_uint2(0, 0);
+#pragma unroll 1
+    for (int n = 16 * h; n < cols_here; n = next_cols(n)) {
+      uint32_t v[8], b[8], near = 0;
+      float sc[8];
+      tmem_ld8(t_row + (uint32_t)n, v);
+      ld_shared_v4(scale_base + 4u * (uint32_t)n, *reinterpret_cast<float(*)[4]>(sc));
+      ld_shared_v4(scale_base + 4u * (uint32_t)n + 16u, *reinterpret_cast<float(*)[4]>(sc + 4));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = (float)(int)v[e] * sc[e], s = fmaf(x, inv, kToInt), off = fmaf(x, inv, kToInt - s);
+        b[e] = __float_as_uint(s);
+        near |= fabsf(off) >= 0.5f - kBorderSums ? 1u << e : 0u;
+      }
+      if (!plain) near = finite && exact > 0.0 ? 255u : 0u;
+#pragma unroll 1
+      for (; near; near &= near - 1) {
+        const int e = __ffs(near) - 1;
+        int s = 0;
+        float scale = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i == e) { s = (int)v[i]; scale = sc[i]; }
+        const uint32_t q8 = round_sum(s, scale, exact, inv);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = i == e ? q8 : b[i];
+      }
+      const uint2 w = finite ? bytes8(b) : make_uint2(0, 0);
+      if (!(n & 8)) half = w;
+      else if (row < p.M && n_base + n - 8 < cols) *reinterpret_cast<uint4*>(out + n - 8) = make_uint4(half.x, half.y, w.x, w.y);
+    }
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tcgen05_fence_after();
+    tmem_dealloc(tmem_base, kRowqMaxSlice);
   }
 }
 

@@ -25,5 +25,10 @@ __device__ __forceinline__ int round_border(F x, F amax, int lower) {
   return lower + (d > (F)0 || (d == (F)0 && (lower & 1)));
 }
 
+// Eight values' low bytes.
+__device__ __forceinline__ uint2 bytes8(const uint32_t (&b)[8]) {
+  return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+}
 }  // namespace i8
 }  // namespace flop

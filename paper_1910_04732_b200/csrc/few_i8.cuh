@@ -68,14 +68,9 @@ __device__ __forceinline__ void load8(const FewParams& p, const char* row, int k
       const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-    } else if (TOK == TOK_F32) {
+    } else {
       const float4 x = *reinterpret_cast<const float4*>(row + 4 * k), y = *reinterpret_cast<const float4*>(row + 4 * k + 16);
       v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-    } else {
-      const int4 x = *reinterpret_cast<const int4*>(row + 4 * k), y = *reinterpret_cast<const int4*>(row + 4 * k + 16);
-      const float4 c = __ldg(reinterpret_cast<const float4*>(p.col + k)), d = __ldg(reinterpret_cast<const float4*>(p.col + k) + 1);
-      v[0] = (float)x.x * c.x; v[1] = (float)x.y * c.y; v[2] = (float)x.z * c.z; v[3] = (float)x.w * c.w;
-      v[4] = (float)y.x * d.x; v[5] = (float)y.y * d.y; v[6] = (float)y.z * d.z; v[7] = (float)y.w * d.w;
     }
     return;
   }
@@ -84,25 +79,10 @@ __device__ __forceinline__ void load8(const FewParams& p, const char* row, int k
     v[i] = 0.f;
     if (k + i < p.K) {
       if (TOK == TOK_BF16) v[i] = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[k + i]);
-      else if (TOK == TOK_F32) v[i] = reinterpret_cast<const float*>(row)[k + i];
-      else v[i] = (float)reinterpret_cast<const int*>(row)[k + i] * __ldg(p.col + k + i);
+      else v[i] = reinterpret_cast<const float*>(row)[k + i];
     }
   }
 }
-// The largest |acc * col| in fp64 among a lane's values that fp32 has at `near` or above (or cannot compare).
-__device__ __noinline__ double largest_exact(const int* acc, const float* col, int k0, int step, int K, float near) {
-  double best = 0.0;
-  for (int k = k0; k < K; k += step)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k + i < K && !(fabsf((float)acc[k + i] * col[k + i]) < near)) {
-        const double h = fabs((double)acc[k + i] * (double)col[k + i]);
-        best = h < (double)INFINITY ? fmax(best, h) : (double)INFINITY;
-      }
-  return best;
-}
-
-__device__ __forceinline__ int round_exact(double x, double amax) { return (int)rint(127.0 * x / amax); }
 // bf16: 127 v / amax with inv = 127 / amax rounded UP decides every value.  With v = m 2^-j u and amax = a u, 128 <= m, a < 256, a quotient that is not on
 // a border is at least 1 / (a 2^(j+1)) > 1.9e-3 2^-j from it, and v inv is off by 3e-5 2^-j at most.  On a border it is only where 127 divides (2 n + 1) a:
 // at v = amax / 2, where v inv is 63.5 or just above and goes to the even 64; or with a = 254, where inv is exact and so is the tie.
@@ -153,29 +133,28 @@ __device__ __noinline__ uint2 round8_wide(const char* at, int n, double amax) {
   }
   return make_uint2(w[0], w[1]);
 }
-// The same for v = acc * col in fp32, exact the largest |acc * col| in fp64.
-__device__ __forceinline__ uint2 round8_sums(const float (&v)[8], float inv, double exact, bool careful, const int* acc, const float* col, int left) {
-  uint32_t b[8], near = 0;
-  float far = 0.f;
+// Sums times their columns' scales, in fp64 (exact as long as a sum has 29 bits): eight products from k on, 0 behind K.
+__device__ __forceinline__ void products8(const FewParams& p, const char* row, int k, double (&h)[8]) {
+  if (k + 8 <= p.K && p.vec) {
+    const int4 x = *reinterpret_cast<const int4*>(row + 4 * k), y = *reinterpret_cast<const int4*>(row + 4 * k + 16);
+    const float4 c = __ldg(reinterpret_cast<const float4*>(p.col + k)), d = __ldg(reinterpret_cast<const float4*>(p.col + k) + 1);
+    h[0] = (double)x.x * (double)c.x; h[1] = (double)x.y * (double)c.y; h[2] = (double)x.z * (double)c.z; h[3] = (double)x.w * (double)c.w;
+    h[4] = (double)y.x * (double)d.x; h[5] = (double)y.y * (double)d.y; h[6] = (double)y.z * (double)d.z; h[7] = (double)y.w * (double)d.w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h[i] = k + i < p.K ? (double)reinterpret_cast<const int*>(row)[k + i] * (double)__ldg(p.col + k + i) : 0.0;
+}
+__device__ __forceinline__ uint2 round8_sums(const double (&h)[8], float inv, double exact, bool careful) {
+  uint32_t b[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float s = fmaf(v[i], inv, kToInt), off = fabsf(fmaf(v[i], inv, kToInt - s));
+    const float x = (float)h[i], s = fmaf(x, inv, kToInt);
     b[i] = __float_as_uint(s);
-    far = fmaxf(far, off);
-    near |= off >= 0.5f - kBorderSums ? 1u << i : 0u;
+    if (careful) b[i] = (uint32_t)round_exact(h[i], exact);
+    else if (fabsf(fmaf(x, inv, kToInt - s)) >= 0.5f - kBorderSums) b[i] = (uint32_t)round_border(h[i], exact, (int)floorf(x * inv));
   }
-  uint2 w = bytes8(b);
-  if (!careful && far < 0.5f - kBorderSums) return w;
-  near = (careful ? 255u : near) & (left >= 8 ? 255u : (1u << left) - 1u);
-#pragma unroll 1
-  for (; near; near &= near - 1) {
-    const int i = __ffs(near) - 1;
-    const double x = (double)acc[i] * (double)col[i];
-    const int q = careful ? round_exact(x, exact) : round_border(x, exact, (int)floorf((float)acc[i] * col[i] * inv));
-    uint32_t& u = i < 4 ? w.x : w.y;
-    u = (u & ~(255u << (8 * (i & 3)))) | (((uint32_t)q & 255u) << (8 * (i & 3)));
-  }
-  return w;
+  return bytes8(b);
 }
 
 // warps to a row of a block that has T of them
@@ -216,49 +195,66 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
 #pragma unroll
     for (int r = 0; r < R; ++r) bits[r] = max(bits[r] << 16, bits[r] & 0xffff0000u);
   }
-#pragma unroll 2
-  for (; k_more < p.K; k_more += step) {
-    float v[R][8];
-#pragma unroll
-    for (int r = 0; r < R; ++r) load8<TOK>(p, row_of(r), k_more, v[r]);
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) bits[r] = max(bits[r], __float_as_uint(v[r][i]) & 0x7fffffffu);      // (infinities and NaN are the largest)
-  }
-  uint32_t top[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) top[r] = __reduce_max_sync(0xffffffffu, bits[r]);
-  if (per_row > 1) {                                                       // then R rows are one
-    uint32_t* red32 = reinterpret_cast<uint32_t*>(red);
-    if (lane == 0) red32[warp] = top[0];
-    __syncthreads();
-    for (int w = 0; w < per_row; ++w) top[0] = max(top[0], red32[first * per_row + w]);
-  }
   double exact[R];
+  if (TOK == TOK_H) {
+    // positive doubles compare as integers (a NaN is the largest): the high words first, the low ones among those that have the highest
+#pragma unroll
+    for (int r = 0; r < R; ++r) exact[r] = 0.0;
+#pragma unroll 1
+    for (; k_more < p.K; k_more += step)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        double h[8];
+        products8(p, row_of(r), k_more, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const double x = fabs(h[i]);
+          if (!(x <= exact[r])) exact[r] = x;
+        }
+      }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint32_t mine = (uint32_t)__double2hiint(exact[r]), hi = __reduce_max_sync(0xffffffffu, mine);
+      const uint32_t low = __reduce_max_sync(0xffffffffu, mine == hi ? (uint32_t)__double2loint(exact[r]) : 0u);
+      exact[r] = __hiloint2double((int)hi, (int)low);
+    }
+    if (per_row > 1) {                                                     // then R rows are one
+      double* red64 = reinterpret_cast<double*>(red);
+      if (lane == 0) red64[warp] = exact[0];
+      __syncthreads();
+      for (int w = 0; w < per_row; ++w) {
+        const double x = red64[first * per_row + w];
+        if (!(x <= exact[0])) exact[0] = x;
+      }
+    }
+  } else {
+#pragma unroll 1
+    for (; k_more < p.K; k_more += step) {
+      float v[R][8];
+#pragma unroll
+      for (int r = 0; r < R; ++r) load8<TOK>(p, row_of(r), k_more, v[r]);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bits[r] = max(bits[r], __float_as_uint(v[r][i]) & 0x7fffffffu);      // (infinities and NaN are the largest)
+    }
+    uint32_t top[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) top[r] = __reduce_max_sync(0xffffffffu, bits[r]);
+    if (per_row > 1) {
+      uint32_t* red32 = reinterpret_cast<uint32_t*>(red);
+      if (lane == 0) red32[warp] = top[0];
+      __syncthreads();
+      for (int w = 0; w < per_row; ++w) top[0] = max(top[0], red32[first * per_row + w]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) exact[r] = (double)__uint_as_float(top[r]);
+  }
   bool careful[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const float amax = __uint_as_float(top[r]);
-    exact[r] = top[r] < 0x7f800000u ? (double)amax : (double)INFINITY;
-    careful[r] = TOK == TOK_H && !(amax < 1e30f && amax > 1e-30f);
-    if (TOK == TOK_H) {
-      // products acc * col: those within the error of fp32 of the largest are compared in fp64; all of them, and the rounding too, where
-      // fp32 could have overflowed or lost digits
-      const float near = careful[r] ? 0.f : amax * (1.f - 1e-6f);
-      double best = 0.0;
-      if (!(__uint_as_float(bits[r]) < near)) best = largest_exact(reinterpret_cast<const int*>(row_of(r)), p.col, k_lane, step, p.K, near);
-      // positive doubles compare as integers: the high words first, the low ones among those that have the highest
-      const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)__double2hiint(best));
-      const uint32_t low = __reduce_max_sync(0xffffffffu, (uint32_t)__double2hiint(best) == hi ? (uint32_t)__double2loint(best) : 0u);
-      exact[r] = __hiloint2double((int)hi, (int)low);
-    }
-  }
-  if (TOK == TOK_H && per_row > 1) {
-    double* red64 = reinterpret_cast<double*>(red + 16);
-    if (lane == 0) red64[warp] = exact[0];
-    __syncthreads();
-    for (int w = 0; w < per_row; ++w) exact[0] = fmax(exact[0], red64[first * per_row + w]);
+    if (!(exact[r] < (double)INFINITY)) exact[r] = (double)INFINITY;
+    careful[r] = !(exact[r] < 1e30 && exact[r] > 1e-30);
   }
   if (sub == 0 && lane < R) {
     const int t = first + lane * rows_at_once;
@@ -275,7 +271,6 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
   float inv[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    if (TOK != TOK_H) careful[r] = !(exact[r] < 1e30 && exact[r] > 1e-30);
     inv[r] = exact[r] > 0.0 && exact[r] < (double)INFINITY ? (careful[r] ? 1.f : TOK == TOK_BF16 ? __fdiv_ru(127.f, (float)exact[r]) : 127.f / (float)exact[r]) : 0.f;
   }
   int k = k_lane;
@@ -301,9 +296,11 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
       if (k < p.K && inv[r] != 0.f) {
         const char* at = row_of(r) + (int64_t)k * (TOK == TOK_BF16 ? 2 : 4);
         float v[8];
-        load8<TOK>(p, row_of(r), k, v);
+        if (TOK != TOK_H) load8<TOK>(p, row_of(r), k, v);
         if (TOK == TOK_H) {
-          w = round8_sums(v, inv[r], exact[r], careful[r], reinterpret_cast<const int*>(at), p.col + k, p.K - k);
+          double h[8];
+          products8(p, row_of(r), k, h);
+          w = round8_sums(h, inv[r], exact[r], careful[r]);
         } else if (careful[r]) {
           w = round8_wide<TOK>(at, p.K - k, exact[r]);
         } else if (TOK == TOK_BF16) {

@@ -1340,7 +1340,6 @@ int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t
   const int64_t row_blocks = (M + tc::BM - 1) / tc::BM;
   int parts = 1;
   while (parts < i8::kRowqMaxCluster && (N > (int64_t)parts * i8::kRowqMaxSlice || (N > 32 * parts && row_blocks * parts * 2 <= num_sms()))) parts *= 2;
-  if (getenv("RP")) parts = atoi(getenv("RP"));
   i8::RowqParams p;
   memset(&p, 0, sizeof(p));
   p.M = (int)M; p.N = (int)N; p.num_kb = (int)((K + i8::kBK - 1) / i8::kBK); p.parts = parts;

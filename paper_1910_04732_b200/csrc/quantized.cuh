@@ -25,6 +25,7 @@ __device__ __forceinline__ int round_border(F x, F amax, int lower) {
   return lower + (d > (F)0 || (d == (F)0 && (lower & 1)));
 }
 
+__device__ __forceinline__ int round_exact(double x, double amax) { return (int)rint(127.0 * x / amax); }
 // Eight values' low bytes.
 __device__ __forceinline__ uint2 bytes8(const uint32_t (&b)[8]) {
   return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),

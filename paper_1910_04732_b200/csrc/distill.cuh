@@ -14,9 +14,11 @@
 // relative to the largest value of their own set: nothing overflows, and a tail far below the list keeps its digits.  Sums of
 // the vocabulary in fp32, of the slots in fp64 (1 - sum q cancels, and so do the two logarithms of a term), all in a fixed order.
 //
-// Bound: HBM.  Loss and gradient need one read and one write of the logits, so a row is read once and held in registers, 16-byte pieces
-// dealt out over the G threads of a part: a warp per row for small vocabularies, a block, or a cluster of up to eight blocks that
-// exchange the maximum and sum of their parts through distributed shared memory.  Rows too wide for eight blocks are read twice.
+// Bound: HBM for rows of thousands of words (loss alone 4096 x 128000 bf16 183 us, 5.75 TB/s), but at one exponential and some three instructions
+// per element and pass the issue slots are close behind: loss and gradient of the same 562 us, 3.7 TB/s of one read and one write.
+// Rows of up to 4096 pieces of 16 bytes are read once and held in registers (part_kernel): eight lanes, a warp or a block to a row, or, where rows
+// are few, a cluster of up to eight blocks that exchange the maximum and sum of their parts through distributed shared memory.  Wider rows, and
+// those of one pass only, are walked (row_kernel).
 #pragma once
 #include "common.cuh"
 
@@ -39,10 +41,9 @@ struct Args {
   const float* stats_in; const float* dloss;     // BWD (dloss nullable)
   void* dS; int64_t ldds;                        // BWD, BOTH
   int vec;                                       // rows of S and dS start on 16 bytes
-  int parts, part_pieces;                        // blocks per row (a cluster, but for BWD), pieces of each
+  int parts, part_pieces;                        // part_kernel: blocks per row (a cluster, but for BWD), pieces of each
 };
 
-__host__ __device__ constexpr int warps_of(int g) { return g / 32; }
 // shared memory of one part: a bit per word in whole 16 bytes, three values per slot
 __host__ __device__ inline size_t part_smem(int V, int K) { return (size_t)((V + 127) / 128) * 16 + (size_t)((3 * K + 3) / 4) * 16; }
 
@@ -73,10 +74,11 @@ __device__ __forceinline__ double log_share(float s, float m_rest, float mc, flo
   return ((double)m_rest - (double)mc + log2_of(s) - l2a) * kLn2d;
 }
 __device__ __forceinline__ float nan_max(float a, float b) { return a != a || a > b ? a : b; }
-template <typename V, typename F>
-__device__ __forceinline__ V warp_all(V v, F f) {
+// over the W lanes (of those in `mask`) that a value belongs to
+template <int W = 32, typename V, typename F>
+__device__ __forceinline__ V warp_all(V v, F f, uint32_t mask = 0xffffffffu) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
+  for (int o = W / 2; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(mask, v, o));
   return v;
 }
 template <typename V> __device__ __forceinline__ V add(V a, V b) { return a + b; }
@@ -175,24 +177,30 @@ __device__ __forceinline__ void store_peer(const void* local, uint32_t rank, flo
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(peer), "f"(a), "f"(b) : "memory");
 }
 
-// One part of one row, held in registers: G threads, P pieces of 16 bytes each.
+// One part of one row, held in registers: G threads, P pieces of 16 bytes each; G < 32 are lanes of a warp that has 32 / G rows, which go their own ways
+// (masked shuffles).  16384 x 205 bf16, K = 16, loss and gradient: 10.7 us (1.5 TB/s); what bounds it is the work per row, fp64 on the slots first of all.
+__host__ __device__ constexpr int part_threads(int g) { return g <= 32 ? 256 : g; }
+__host__ __device__ constexpr int part_rows(int g) { return g <= 32 ? 256 / g : 1; }
 template <typename T, int MODE, int G, int P>
-__global__ void __launch_bounds__(G == 32 ? 256 : G, P > 4 ? 1024 / (G == 32 ? 256 : G) : 1) part_kernel(const Args a) {
-  constexpr int NW = warps_of(G), kGroups = G == 32 ? 8 : 1;
+__global__ void __launch_bounds__(part_threads(G), P > 4 || G < 32 ? 1024 / part_threads(G) : 1) part_kernel(const Args a) {
+  constexpr int NW = G / 32, kGroups = part_rows(G), W = G < 32 ? G : 32;   // W: lanes that share a row
+  constexpr bool kOneWarp = G <= 32;
   extern __shared__ __align__(16) unsigned char smem[];
   struct First { float t, n, x, m, s; };                // largest t, number of listed words, largest listed logit; maximum and sum outside the list
   struct Second { double a, kl; float top; };           // sum of the teacher's exponentials, of the terms, of the student's on the list
-  __shared__ First first[NW];
-  __shared__ Second second[NW];
+  __shared__ First first[NW > 0 ? NW : 1];
+  __shared__ Second second[NW > 0 ? NW : 1];
   __shared__ float2 peer[8];
   __shared__ int s_dup[kGroups];
-  const int group = G == 32 ? threadIdx.x >> 5 : 0, tid = G == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const int lane = threadIdx.x & 31, warp = G == 32 ? 0 : threadIdx.x >> 5;
-  const int64_t row = G == 32 ? (int64_t)blockIdx.x * kGroups + group : blockIdx.x / a.parts;
-  const int part = G == 32 ? 0 : (int)(blockIdx.x % a.parts);
-  const bool cluster = (MODE & FWD) && G != 32 && a.parts > 1;
+  const int group = kOneWarp ? threadIdx.x / G : 0, tid = kOneWarp ? threadIdx.x % G : threadIdx.x;
+  const int lane = threadIdx.x & 31, warp = kOneWarp ? 0 : threadIdx.x >> 5;
+  const uint32_t mask = G < 32 ? ((1u << W) - 1) << (lane & ~(W - 1)) : 0xffffffffu;
+  const int64_t row = kOneWarp ? (int64_t)blockIdx.x * kGroups + group : blockIdx.x / a.parts;
+  const int part = kOneWarp ? 0 : (int)(blockIdx.x % a.parts);
+  const bool cluster = (MODE & FWD) && !kOneWarp && a.parts > 1;
   if (cluster) cluster_arrive();                        // completed before the first store to a peer: all of them run
-  auto sync = [&] { if (G == 32) __syncwarp(); else __syncthreads(); };
+  auto sync = [&] { if (kOneWarp) __syncwarp(mask); else __syncthreads(); };
+  auto all = [&](auto v, auto f) { return warp_all<W>(v, f, mask); };
   const int words4 = (a.V + 127) / 128;
   unsigned char* mine = smem + (size_t)group * part_smem(a.V, a.K);
   uint32_t* bits = reinterpret_cast<uint32_t*>(mine);
@@ -204,7 +212,7 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G, P > 4 ? 1024 / (G == 32 ? 2
   sync();
   pdl_wait();
   pdl_launch_dependents();
-  if (G == 32 && row >= a.T) return;
+  if (kOneWarp && row >= a.T) return;
   const T* S = reinterpret_cast<const T*>(a.S) + row * a.lds;
   T* dS = MODE == FWD ? nullptr : reinterpret_cast<T*>(a.dS) + row * a.ldds;
   const int all_pieces = (a.V + kPer<T> - 1) / kPer<T>;
@@ -261,19 +269,19 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G, P > 4 ? 1024 / (G == 32 ? 2
         f.n += 1.f;
         if (MODE & FWD) f.x = fmaxf(f.x, slot_x[j]);
       }
-    f.t = warp_all(f.t, nan_max);
-    f.n = warp_all(f.n, add<float>);
+    f.t = all(f.t, nan_max);
+    f.n = all(f.n, add<float>);
     if (MODE & FWD) {
-      f.x = warp_all(f.x, max2);
+      f.x = all(f.x, max2);
       hide_listed();
       float m = -INFINITY;
 #pragma unroll
       for (int i = 0; i < P; ++i) m = fmaxf(m, piece_max<T>(d[i]));
-      f.m = warp_all(m, max2);
+      f.m = all(m, max2);
       const float ref = f.m == -INFINITY ? 0.f : __fmul_rn(f.m, a.c);
 #pragma unroll
       for (int i = 0; i < P; ++i) f.s += piece_sum<T>(d[i], a.c, ref);
-      f.s = warp_all(f.s, add<float>);
+      f.s = all(f.s, add<float>);
     } else {
       hide_listed();
     }
@@ -336,8 +344,8 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G, P > 4 ? 1024 / (G == 32 ? 2
       if (!(q <= 0.f)) h.kl += (double)q * (lq - lx);
     }
   }
-  h.a = warp_all(h.a, add<double>);
-  if (MODE & FWD) { h.kl = warp_all(h.kl, add<double>); h.top = warp_all(h.top, add<float>); }
+  h.a = all(h.a, add<double>);
+  if (MODE & FWD) { h.kl = all(h.kl, add<double>); h.top = all(h.top, add<float>); }
   if (NW > 1) {
     if (lane == 0) second[warp] = h;
     sync();
@@ -378,8 +386,9 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G, P > 4 ? 1024 / (G == 32 ? 2
 }
 
 // ---- rows that one block of G threads walks, persistent over the rows.  A thread has a batch of four 16-byte pieces in registers and the next
-// one on its way, across the end of a pass and of a row; loss and gradient read a row twice, the second time from L1 or L2 (592 rows in flight are
-// at most 150 MB for the widest vocabularies and 38 MB at 128k words; measured DRAM traffic there: each logit once in, once out).
+// one on its way, across the end of a pass and of a row.  Loss and gradient go over a row twice, the second time backwards: the last batch is
+// still in registers, the rest is read again, most recent first.  What the second read costs: 1000 x 50001 bf16 64 us against 30 for the loss alone.
+// (Batches kept in shared memory instead of read again: 610 to 650 us at 4096 x 128000, against 562; 64 registers do not hold that loop.)
 constexpr int kBatch = 4;
 
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
@@ -434,21 +443,221 @@ __device__ __forceinline__ float batch_max(const uint4 (&d)[kBatch]) {
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
-__host__ __device__ inline size_t row_smem(int V, int K) { return 2 * part_smem(V, K); }      // this row's list and the next one's
+// shared memory: this row's list and the next one's
+__host__ __device__ inline size_t row_smem(int V, int K) { return 2 * part_smem(V, K); }
+constexpr int kLane = 4;                                                 // slots of a lane and round: 128 to a warp
 
-// The last warp of the block has the lists, one row ahead of the others: it reads a row's list, sets its bits and does everything that
-// takes only the slots while the other warps are at the row before, takes the loss when their sums are there, and writes the K entries of the
-// gradient when they are through.  Barriers, in the order the other warps (M) and this one (L) meet them, row by row:
-//     kBits    L arrives when the row's bits are set              M waits before its first look at them
-//     kSums    both wait: M's sums and L's numbers of the row are written
-//     kStored  M arrives when the row's gradient is written       L waits before it writes the listed words and clears the bits
+constexpr int kBits = 1, kSums = 3, kStored = 4;                        // named barriers (kBits and kBits + 1 in turn)
+struct Sums { float m, s; };                                             // maximum (logit) and sum outside the list, relative to 2^(m c)
+struct Info { double q, kl; float top_ref, top, r, mc, l2all, m_rest, l2rest; int empty; };
+
+// The next row of a block that is looked at, from `row` on; those passed over get their loss (the list's warp) and their zeros (the others).
+template <typename T, int MODE>
+__device__ __forceinline__ int64_t active_from(const Args& a, int64_t row, int pieces, int tid, int threads, bool list_warp) {
+  for (; row < a.T; row += gridDim.x) {
+    float g = a.weight ? a.weight[row] : 1.f;
+    if (MODE == BWD && a.dloss) g *= a.dloss[row];
+    if (g != 0.f) break;
+    if (list_warp) {
+      if ((MODE & FWD) && (tid & 31) == 0) {
+        a.loss[row] = 0.f;
+        if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
+      }
+    } else if (MODE & BWD) {
+      for (int p = tid; p < pieces; p += threads) store_piece<T>(reinterpret_cast<T*>(a.dS) + row * a.ldds, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
+    }
+  }
+  return row;
+}
+template <int MODE>
+__device__ __forceinline__ float factor_of(const Args& a, int64_t row) {  // of the row's gradient
+  const float g = (a.weight ? a.weight[row] : 1.f) * a.inv_tau;
+  return MODE == BWD && a.dloss ? a.dloss[row] * g : g;
+}
+
+// The last warp of the block has the lists, one row ahead of the others: while they are in a row's first pass it reads the next row's list, sets
+// its bits and does everything that takes only the slots; it takes the loss when the row's sums are there, and writes the K entries of the
+// gradient when the others are through.  Its life is latency (index -> word -> exponentials), so loads go out four to a lane and the indices
+// a row before they are used.  Barriers, in the order the other warps (M) and this one (L) meet them, row by row:
+//     kBits, kBits + 1 in turn   L arrives when the row's bits are set              M waits before its first look at them
+//     kSums                      both wait: M's sums and L's numbers of the row are written
+//     kStored                    M arrives when the row's gradient is written       L waits before it writes the listed words and clears the bits
+// The list's warp is a function of its own: in the kernel's body its registers would be taken from the other warps' (64 each), which then spill
+// in their loops.
 template <typename T, int MODE, int G>
-__global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
+__device__ __noinline__ void row_lists(const Args& a, unsigned char* smem, Sums (*sums)[G / 32 - 1], Info* info, int64_t row, int words4, int pieces, size_t side_bytes) {
+  constexpr int NW = G / 32 - 1;
+  const int lane = threadIdx.x & 31;
+  const T* S0 = reinterpret_cast<const T*>(a.S);
+  T* dS0 = reinterpret_cast<T*>(a.dS);
+  struct List { uint32_t* bits; int* idx; float *t, *x; };
+  auto list_of = [&](int side) {
+    List l;
+    l.bits = reinterpret_cast<uint32_t*>(smem + side * side_bytes);
+    l.idx = reinterpret_cast<int*>(l.bits + 4 * words4);
+    l.t = reinterpret_cast<float*>(l.idx + a.K);
+    l.x = l.t + a.K;
+    return l;
+  };
+  int ahead_idx[kLane];                                                // the first 128 slots of the row after the next
+  float ahead_t[kLane], ahead_lse = 0.f;
+  auto load_slots = [&](int64_t row, int j0, int (&idx)[kLane], float (&t)[kLane]) {
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) {
+      const int j = j0 + 32 * i + lane;
+      idx[i] = j < a.K ? a.t_idx[row * a.ldi + j] : -1;
+      t[i] = j < a.K ? a.t_logits[row * a.ldt + j] : 0.f;
+    }
+  };
+  auto load_ahead = [&](int64_t row) {
+    if (row >= a.T) return;
+    load_slots(row, 0, ahead_idx, ahead_t);
+    if (a.t_lse) ahead_lse = a.t_lse[row];
+  };
+  // the list of `row` (its first slots and its lse are in ahead_*); returns the row after it, whose slots are then on their way
+  auto prepare = [&](int side, int64_t row) {
+    const List l = list_of(side);
+    const T* S = S0 + row * a.lds;
+    const double lse = a.t_lse ? (double)ahead_lse : 0.0;
+    bool dup = false;
+    for (int j0 = 0; j0 < a.K; j0 += 32 * kLane) {
+      int idx[kLane];
+      float t[kLane];
+      if (j0 == 0) {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) { idx[i] = ahead_idx[i]; t[i] = ahead_t[i]; }
+      } else {
+        load_slots(row, j0, idx, t);
+      }
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) {
+        const int j = j0 + 32 * i + lane;
+        if (idx[i] < 0 || idx[i] >= a.V) idx[i] = -1;
+        if (j < a.K) { l.idx[j] = idx[i]; l.t[j] = t[i]; }
+        if (idx[i] >= 0) dup |= atomicOr(&l.bits[idx[i] >> 5], 1u << (idx[i] & 31)) >> (idx[i] & 31) & 1u;
+      }
+    }
+    __syncwarp();
+    bar_arrive(kBits + side, G);
+    if (__any_sync(0xffffffffu, dup)) {                                // rare: the first of equal indices stays
+      uint32_t drop = 0;
+      for (int j = lane, n = 0; j < a.K; j += 32, ++n)
+        if (l.idx[j] >= 0)
+          for (int i = 0; i < j; ++i)
+            if (l.idx[i] == l.idx[j]) { drop |= 1u << n; break; }
+      __syncwarp();
+      for (int j = lane, n = 0; j < a.K; j += 32, ++n)
+        if (drop >> n & 1u) l.idx[j] = -1;
+      __syncwarp();
+    }
+    float mt = -INFINITY, mx = -INFINITY;
+    int n = 0;
+    for (int j0 = 0; j0 < a.K; j0 += 32 * kLane) {
+      float x[kLane];
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) {
+        const int j = j0 + 32 * i + lane, idx = j < a.K ? l.idx[j] : -1;
+        x[i] = idx >= 0 ? to_f32(S[idx]) : -INFINITY;
+        if (idx >= 0) { mt = nan_max(mt, l.t[j]); ++n; }
+      }
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) {
+        const int j = j0 + 32 * i + lane;
+        if (j < a.K) l.x[j] = x[i];
+        mx = fmaxf(mx, x[i]);
+      }
+    }
+    const int64_t after = active_from<T, MODE>(a, row + gridDim.x, pieces, lane, 32, true);
+    load_ahead(after);
+    mt = warp_all(mt, nan_max); mx = warp_all(mx, max2);
+    n = __reduce_add_sync(0xffffffffu, n);
+    const double t_ref = a.t_lse ? lse : (double)mt * a.inv_tau_d;
+    // the student's exponentials on the list relative to the largest there
+    const float ref = !(MODE & FWD) || mx == -INFINITY ? 0.f : __fmul_rn(mx, a.c);
+    float top = 0.f;
+    double sum_q = 0.0, kl = 0.0;
+    for (int j = lane; j < a.K; j += 32) {
+      if (l.idx[j] < 0) continue;
+      const double lq = (double)l.t[j] * a.inv_tau_d - t_ref;
+      const float q = exp_of(lq);
+      l.t[j] = q;
+      sum_q += (double)q;
+      if (MODE & FWD) {
+        const double lx = ((double)l.x[j] * (double)a.c - (double)ref) * kLn2d;
+        const float e = exp_of(lx);
+        l.x[j] = e;
+        top += e;
+        if (!(q <= 0.f)) kl += (double)q * (lq - lx);
+      }
+    }
+    sum_q = warp_all(sum_q, add<double>);
+    if (MODE & FWD) { kl = warp_all(kl, add<double>); top = warp_all(top, add<float>); }
+    if (lane == 0) {
+      Info& o = info[side];
+      o.q = sum_q; o.kl = kl; o.top_ref = ref; o.top = top;
+      o.r = a.t_lse && n < a.V ? (float)fmax(0.0, 1.0 - sum_q) : 0.f;
+      o.empty = n == 0 || (!a.t_lse && mt == -INFINITY);               // an empty list, or one that gives every word nothing
+      if (MODE == BWD) { const float* st = a.stats_in + 4 * row; o.mc = st[0]; o.l2all = st[1]; o.m_rest = st[2]; o.l2rest = st[3]; }
+    }
+    __syncwarp();
+    return after;
+  };
+  int side = 0;
+  load_ahead(row);
+  int64_t next = prepare(0, row);
+  for (;;) {
+    // the loss alone has one pass to hide the next list behind, loss and gradient rather the second
+    int64_t after = next;
+    if (MODE != BOTH && next < a.T) after = prepare(side ^ 1, next);
+    bar_sync(kSums, G);
+    const Info o = info[side];
+    float all_inv = 0.f;
+    const float q_norm = a.t_lse ? 1.f : (float)(1.0 / o.q);
+    if (MODE & FWD) {
+      const Sums u = lane < NW ? sums[side][lane] : Sums{-INFINITY, 0.f};
+      const float m = warp_all(u.m, max2), m_rest = m == -INFINITY ? 0.f : __fmul_rn(m, a.c);
+      const float s = warp_all(u.m == -INFINITY ? u.s : u.s * pow2_of(__fmul_rn(u.m, a.c) - m_rest), add<float>);
+      // relative to the larger reference
+      const float mc = o.top > 0.f || o.top != o.top ? fmaxf(o.top_ref, m == -INFINITY ? o.top_ref : m_rest) : m_rest;
+      const float on = o.top * pow2_of(o.top_ref - mc);
+      const float all = on + (s > 0.f ? s * pow2_of(m_rest - mc) : s);
+      all_inv = pow2_of(o.top_ref - mc) / all;
+      if (lane == 0) {
+        const double l2a = log2_of(all);
+        // the terms' logarithms are relative to the list's reference
+        const double log_all = (l2a + (double)mc - (double)o.top_ref) * kLn2d;
+        double v = a.t_lse ? o.kl + o.q * log_all : o.kl / o.q - log2_of((float)o.q) * kLn2d + log_all;
+        if (o.r > 0.f) v += (double)o.r * (log_left(o.q, o.r) - log_share(s, m_rest, mc, on, l2a));
+        a.loss[row] = o.empty ? 0.f : (a.weight ? a.weight[row] : 1.f) * (float)v;
+        if (a.stats) { float* st = a.stats + 4 * row; st[0] = mc; st[1] = (float)l2a; st[2] = m_rest; st[3] = log2f(s); }
+      }
+    }
+    if (MODE == BOTH && next < a.T) after = prepare(side ^ 1, next);
+    // what is left of a row when its gradient is written: the listed words, and their bits
+    const List l = list_of(side);
+    if (MODE & BWD) {
+      const float g = factor_of<MODE>(a, row);
+      bar_sync(kStored, G);
+      for (int j = lane; j < a.K; j += 32)
+        if (l.idx[j] >= 0 && !o.empty) {
+          const float p = MODE == BWD ? ex2(fmaf(l.x[j], a.c, -o.mc) - o.l2all) : l.x[j] * all_inv;
+          dS0[row * a.ldds + l.idx[j]] = from_f32<T>(g * (p - l.t[j] * q_norm));
+        }
+    }
+    for (int j = lane; j < a.K; j += 32)
+      if (l.idx[j] >= 0) atomicAnd(&l.bits[l.idx[j] >> 5], ~(1u << (l.idx[j] & 31)));
+    __syncwarp();
+    if (next >= a.T) break;
+    row = next;
+    next = after;
+    side ^= 1;
+  }
+}
+
+template <typename T, int MODE, int G>
+__global__ void __launch_bounds__(G, 1024 / G) row_kernel(const __grid_constant__ Args a) {
   constexpr int M = G - 32, NW = M / 32;
-  constexpr int kBits = 1, kSums = 2, kStored = 3;
   extern __shared__ __align__(16) unsigned char smem[];
-  struct Sums { float m, s; };                                           // maximum (logit) and sum outside the list, relative to 2^(m c)
-  struct Info { float top_ref, top, r, mc, l2all, m_rest, l2rest; int empty; };
   __shared__ Sums sums[2][NW];
   __shared__ Info info[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -460,152 +669,10 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
   pdl_launch_dependents();
   const T* S0 = reinterpret_cast<const T*>(a.S);
   T* dS0 = reinterpret_cast<T*>(a.dS);
-  auto active_from = [&](int64_t row) {                                  // the next row of this block that is looked at
-    for (; row < a.T; row += gridDim.x) {
-      float g = a.weight ? a.weight[row] : 1.f;
-      if (MODE == BWD && a.dloss) g *= a.dloss[row];
-      if (g != 0.f) break;
-      if (warp == NW) {
-        if ((MODE & FWD) && lane == 0) {
-          a.loss[row] = 0.f;
-          if (a.stats) for (int i = 0; i < 4; ++i) a.stats[4 * row + i] = 0.f;
-        }
-      } else if (MODE & BWD) {
-        for (int p = tid; p < pieces; p += M) store_piece<T>(dS0 + row * a.ldds, p, a.V, a.vec, make_uint4(0, 0, 0, 0));
-      }
-    }
-    return row;
-  };
-  auto factor = [&](int64_t row) {                                       // of the row's gradient
-    const float g = (a.weight ? a.weight[row] : 1.f) * a.inv_tau;
-    return MODE == BWD && a.dloss ? a.dloss[row] * g : g;
-  };
-  int64_t row = active_from(blockIdx.x);
+  int64_t row = active_from<T, MODE>(a, blockIdx.x, pieces, tid, M, warp == NW);
   if (row >= a.T) return;
-
   if (warp == NW) {
-    // ------------------------------------------------------------------------------------ the lists
-    struct List { uint32_t* bits; int* idx; float *t, *x; };
-    auto list_of = [&](int side) {
-      List l;
-      l.bits = reinterpret_cast<uint32_t*>(smem + side * side_bytes);
-      l.idx = reinterpret_cast<int*>(l.bits + 4 * words4);
-      l.t = reinterpret_cast<float*>(l.idx + a.K);
-      l.x = l.t + a.K;
-      return l;
-    };
-    double sum_q = 0.0, kl = 0.0;                                        // of the row whose info was written last
-    auto read_list = [&](int side, int64_t row) {
-      const List l = list_of(side);
-      const T* S = S0 + row * a.lds;
-      bool dup = false;
-      for (int j = lane; j < a.K; j += 32) {
-        int idx = a.t_idx[row * a.ldi + j];
-        if (idx < 0 || idx >= a.V) idx = -1;
-        l.idx[j] = idx;
-        if (idx < 0) continue;
-        dup |= atomicOr(&l.bits[idx >> 5], 1u << (idx & 31)) >> (idx & 31) & 1u;
-        l.t[j] = a.t_logits[row * a.ldt + j];
-        l.x[j] = to_f32(S[idx]);
-      }
-      __syncwarp();
-      bar_arrive(kBits, G);
-      if (__any_sync(0xffffffffu, dup)) {                                // rare: the first of equal indices stays
-        uint32_t drop = 0;
-        for (int j = lane, n = 0; j < a.K; j += 32, ++n)
-          if (l.idx[j] >= 0)
-            for (int i = 0; i < j; ++i)
-              if (l.idx[i] == l.idx[j]) { drop |= 1u << n; break; }
-        __syncwarp();
-        for (int j = lane, n = 0; j < a.K; j += 32, ++n)
-          if (drop >> n & 1u) l.idx[j] = -1;
-        __syncwarp();
-      }
-      float mt = -INFINITY, n = 0.f, mx = -INFINITY;
-      for (int j = lane; j < a.K; j += 32)
-        if (l.idx[j] >= 0) { mt = nan_max(mt, l.t[j]); n += 1.f; mx = fmaxf(mx, l.x[j]); }
-      mt = warp_all(mt, nan_max); n = warp_all(n, add<float>); mx = warp_all(mx, max2);
-      const double t_ref = a.t_lse ? (double)a.t_lse[row] : (double)mt * a.inv_tau_d;
-      // the student's exponentials on the list relative to the largest there
-      const float ref = !(MODE & FWD) ? 0.f : mx == -INFINITY ? 0.f : __fmul_rn(mx, a.c);
-      float top = 0.f;
-      sum_q = 0.0; kl = 0.0;
-      for (int j = lane; j < a.K; j += 32) {
-        if (l.idx[j] < 0) continue;
-        const double lq = (double)l.t[j] * a.inv_tau_d - t_ref;
-        const float q = exp_of(lq);
-        l.t[j] = q;
-        sum_q += (double)q;
-        if (MODE & FWD) {
-          const double lx = ((double)l.x[j] * (double)a.c - (double)ref) * kLn2d;
-          const float e = exp_of(lx);
-          l.x[j] = e;
-          top += e;
-          if (!(q <= 0.f)) kl += (double)q * (lq - lx);
-        }
-      }
-      sum_q = warp_all(sum_q, add<double>);
-      if (MODE & FWD) { kl = warp_all(kl, add<double>); top = warp_all(top, add<float>); }
-      if (lane == 0) {
-        Info& o = info[side];
-        o.top_ref = ref; o.top = top;
-        o.r = a.t_lse && n < (float)a.V ? (float)fmax(0.0, 1.0 - sum_q) : 0.f;
-        o.empty = n == 0.f || (!a.t_lse && mt == -INFINITY);             // an empty list, or one that gives every word nothing
-        if (MODE == BWD) { const float* st = a.stats_in + 4 * row; o.mc = st[0]; o.l2all = st[1]; o.m_rest = st[2]; o.l2rest = st[3]; }
-      }
-      __syncwarp();
-    };
-    // what is left of a row when its gradient is written: the listed words, and their bits
-    auto finish = [&](int side, int64_t row, float all_inv, float q_norm) {
-      const List l = list_of(side);
-      const Info o = info[side];
-      if (MODE & BWD) {
-        bar_sync(kStored, G);
-        const float g = factor(row);
-        for (int j = lane; j < a.K; j += 32)
-          if (l.idx[j] >= 0 && !o.empty) {
-            const float p = MODE == BWD ? ex2(fmaf(l.x[j], a.c, -o.mc) - o.l2all) : l.x[j] * all_inv;
-            dS0[row * a.ldds + l.idx[j]] = from_f32<T>(g * (p - l.t[j] * q_norm));
-          }
-      }
-      for (int j = lane; j < a.K; j += 32)
-        if (l.idx[j] >= 0) atomicAnd(&l.bits[l.idx[j] >> 5], ~(1u << (l.idx[j] & 31)));
-      __syncwarp();
-    };
-    int side = 0;
-    read_list(0, row);
-    for (;;) {
-      const int64_t next = active_from(row + gridDim.x);
-      bar_sync(kSums, G);
-      const double a_q = sum_q;
-      float all_inv = 0.f;
-      const float q_norm = a.t_lse ? 1.f : (float)(1.0 / a_q);
-      if (MODE & FWD) {
-        const Info o = info[side];
-        const Sums u = lane < NW ? sums[side][lane] : Sums{-INFINITY, 0.f};
-        const float m = warp_all(u.m, max2), m_rest = m == -INFINITY ? 0.f : __fmul_rn(m, a.c);
-        const float s = warp_all(u.m == -INFINITY ? u.s : u.s * pow2_of(__fmul_rn(u.m, a.c) - m_rest), add<float>);
-        // relative to the larger reference
-        const float mc = o.top > 0.f || o.top != o.top ? fmaxf(o.top_ref, m == -INFINITY ? o.top_ref : m_rest) : m_rest;
-        const float on = o.top * pow2_of(o.top_ref - mc);
-        const float all = on + (s > 0.f ? s * pow2_of(m_rest - mc) : s);
-        all_inv = pow2_of(o.top_ref - mc) / all;
-        if (lane == 0) {
-          const double l2a = log2_of(all);
-          // the terms' logarithms are relative to the list's reference
-          const double log_all = (l2a + (double)mc - (double)o.top_ref) * kLn2d;
-          double v = a.t_lse ? kl + a_q * log_all : kl / a_q - log2_of((float)a_q) * kLn2d + log_all;
-          if (o.r > 0.f) v += (double)o.r * (log_left(a_q, o.r) - log_share(s, m_rest, mc, on, l2a));
-          a.loss[row] = o.empty ? 0.f : (a.weight ? a.weight[row] : 1.f) * (float)v;
-          if (a.stats) { float* st = a.stats + 4 * row; st[0] = mc; st[1] = (float)l2a; st[2] = m_rest; st[3] = log2f(s); }
-        }
-      }
-      if (next < a.T) read_list(side ^ 1, next);
-      finish(side, row, all_inv, q_norm);
-      if (next >= a.T) break;
-      row = next;
-      side ^= 1;
-    }
+    row_lists<T, MODE, G>(a, smem, sums, info, row, words4, pieces, side_bytes);
     return;
   }
 
@@ -647,9 +714,9 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
   load(ahead, S0 + row * a.lds, 0);
   for (;;) {
     const T* S = S0 + row * a.lds;
-    const int64_t next = active_from(row + gridDim.x);
+    const int64_t next = active_from<T, MODE>(a, row + gridDim.x, pieces, tid, M, false);
     const T* S_next = next < a.T ? S0 + next * a.lds : nullptr;
-    bar_sync(kBits, G);
+    bar_sync(kBits + side, G);
     float m = -INFINITY;
     if (MODE & FWD) {
       // first pass: maximum and sum outside the list, kept relative to the maximum so far
@@ -687,7 +754,7 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const Args a) {
     if (MODE & BWD) {
       // second pass: outside the list 2^(x - m_rest) times what is common to the row
       const Info& o = info[side];
-      const float g = factor(row), r = o.r;
+      const float g = factor_of<MODE>(a, row), r = o.r;
       float m_rest, pull;
       if (MODE == BWD) {
         m_rest = o.m_rest;

@@ -1368,28 +1368,29 @@ int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t
 }
 
 // ---- distillation from top logits
+constexpr int kSubWarpSmem = 48 * 1024;     // four blocks to an SM
 template <typename T, int MODE, int G, int P>
 int launch_distill_part(const distill::Args& a, int parts, cudaStream_t st) {
   static OncePerDevice configured;
-  constexpr int rows_per_block = G == 32 ? 8 : 1;
+  constexpr int rows_per_block = distill::part_rows(G);
   auto kern = distill::part_kernel<T, MODE, G, P>;
   const size_t smem = rows_per_block * distill::part_smem(a.V, a.K);
-  FLOP_TRY(allow_smem(configured, G == 32 ? 8 * distill::part_smem(2048, distill::kMaxSlots) : distill::part_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
+  FLOP_TRY(allow_smem(configured, G < 32 ? (size_t)kSubWarpSmem : G == 32 ? 8 * distill::part_smem(2048, distill::kMaxSlots) : distill::part_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
   distill::Args b = a;
   const int pieces = (a.V + distill::kPer<T> - 1) / distill::kPer<T>;
   b.parts = parts;
   b.part_pieces = (pieces + parts - 1) / parts;
   cudaLaunchConfig_t cfg{};
-  const int64_t blocks = G == 32 ? ((int64_t)a.T + rows_per_block - 1) / rows_per_block : (int64_t)a.T * parts;
+  const int64_t blocks = G <= 32 ? ((int64_t)a.T + rows_per_block - 1) / rows_per_block : (int64_t)a.T * parts;
   if (blocks > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
-  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(G == 32 ? 256 : G); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(distill::part_threads(G)); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = pdl_on() ? 1 : 0;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = (unsigned)parts; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = (MODE & distill::FWD) && G != 32 && parts > 1 ? 2 : 1;
+  cfg.numAttrs = (MODE & distill::FWD) && G > 32 && parts > 1 ? 2 : 1;
   cudaLaunchKernelEx(&cfg, kern, b);
   count_launch();
   FLOP_CUDA(cudaGetLastError());
@@ -1399,10 +1400,10 @@ template <typename T, int MODE, int G>
 int launch_distill_row(const distill::Args& a, cudaStream_t st) {
   static OncePerDevice configured;
   auto kern = distill::row_kernel<T, MODE, G>;
-  FLOP_TRY(allow_smem(configured, distill::row_smem(distill::kMaxVocab, distill::kMaxSlots), kern));
+  FLOP_TRY(allow_smem(configured, kSmemBudget - 2048, kern));
   const size_t smem = distill::row_smem(a.V, a.K);
-  const int resident = (int)std::min<size_t>(1024 / G, (size_t)(228 * 1024) / (smem + 2048));
-  launch_k(kern, dim3((unsigned)std::min<int64_t>(a.T, (int64_t)num_sms() * std::max(resident, 1))), dim3(G), smem, st, a);
+  const int resident = std::max(1, (int)std::min<size_t>(1024 / G, (size_t)kSmemBudget / (smem + 2048)));
+  launch_k(kern, dim3((unsigned)std::min<int64_t>(a.T, (int64_t)num_sms() * resident)), dim3(G), smem, st, a);
   count_launch();
   FLOP_CUDA(cudaGetLastError());
   return FLOP_OK;
@@ -1410,10 +1411,18 @@ int launch_distill_row(const distill::Args& a, cudaStream_t st) {
 template <typename T, int MODE>
 int launch_distill_inst(const distill::Args& a, cudaStream_t st) {
   const int64_t pieces = (a.V + distill::kPer<T> - 1) / distill::kPer<T>;
-  if (pieces <= 32) return launch_distill_part<T, MODE, 32, 1>(a, 1, st);
+  // Small vocabularies are bound by what a row costs beside its words (slots, reductions), so with many rows a warp takes four of them, or two; that
+  // row's chain is then twice as long, so with few rows a warp has one.  Several / one to a warp, loss and gradient: 16384 x 205 bf16 10.7 / 19.9 us,
+  // 512 x 205 6.3 / 4.1; 16384 x 500 16.0 / 22.4, 512 x 500 5.5 / 4.2: the lines cross at 3400 rows.
+  if (a.T > 24 * (int64_t)num_sms()) {
+    if (pieces <= 32 && distill::part_rows(8) * distill::part_smem(a.V, a.K) <= kSubWarpSmem) return launch_distill_part<T, MODE, 8, 4>(a, 1, st);
+    if (pieces <= 64 && distill::part_rows(16) * distill::part_smem(a.V, a.K) <= kSubWarpSmem) return launch_distill_part<T, MODE, 16, 4>(a, 1, st);
+  }
   if (pieces <= 64) return launch_distill_part<T, MODE, 32, 2>(a, 1, st);
   if (pieces <= 128) return launch_distill_part<T, MODE, 32, 4>(a, 1, st);
   if (pieces <= 256) return launch_distill_part<T, MODE, 32, 8>(a, 1, st);
+  // few rows: a cluster of blocks to a row, up to eight of 32 KB to 64 KB.  24 x 32000 bf16, loss and gradient: 5.7 us,
+  // 8.0 as one block per row; the loss of 60 x 32000 6.6 / 7.1
   if (a.T <= num_sms() / 2 && pieces <= 32768) {
     int parts = 1;
     while (parts < 8 && (pieces > (int64_t)parts * 2048 || (int64_t)a.T * parts * 2 <= num_sms())) parts *= 2;
@@ -1421,12 +1430,21 @@ int launch_distill_inst(const distill::Args& a, cudaStream_t st) {
     if (pieces <= (int64_t)parts * 2048) return launch_distill_part<T, MODE, 256, 8>(a, parts, st);
     return launch_distill_part<T, MODE, 512, 8>(a, parts, st);
   }
+  // Rows in registers cost one read, but a block lasts from the first load to the last store, with nothing to hide that behind but the SM's other
+  // blocks; the walking kernel reads twice for loss and gradient, always a batch ahead.  Held / walked, bf16, loss and gradient: 16384 x 4096
+  // 91 / 166 us, 8192 x 16000 159 / 191, 8192 x 20000 (five of eight pieces in use) 256 / 195; f32: 8192 x 10000 218 / 200, 8192 x 16000 260 / 324.
+  // The loss alone is read once either way: 16384 x 4096 61 / 145 us, 8192 x 10000 f32 walked 77.
   if (MODE != distill::BWD && pieces <= 512) return launch_distill_part<T, MODE, 64, 8>(a, 1, st);
   if (MODE == distill::BOTH && pieces <= 1024) return launch_distill_part<T, MODE, 128, 8>(a, 1, st);
   if (MODE == distill::BOTH && pieces <= 2048) return launch_distill_part<T, MODE, 256, 8>(a, 1, st);
+  if (MODE == distill::BOTH && pieces > 3584 && pieces <= 4096) return launch_distill_part<T, MODE, 512, 8>(a, 1, st);
+  // Threads of a block: 256 against 512 is 30 / 39 us for the loss of 1000 x 50001 and 183 / 195 for 4096 x 128000; with the gradient 64 / 75 and
+  // 569 / 562 (four smaller blocks have four rows under way, two larger ones leave more of a row in L1), f32 2048 x 40000 249 / 221.
   if (pieces <= 1024) return launch_distill_row<T, MODE, 128>(a, st);
-  if (pieces <= 4096) return launch_distill_row<T, MODE, 256>(a, st);
-  return launch_distill_row<T, MODE, 512>(a, st);
+  if constexpr (MODE == distill::BOTH) {
+    if (pieces > 8192) return launch_distill_row<T, MODE, 512>(a, st);
+  }
+  return launch_distill_row<T, MODE, 256>(a, st);
 }
 template <int MODE>
 int distill_impl(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt, const int32_t* t_idx, int64_t ldi, int64_t K,

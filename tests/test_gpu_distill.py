@@ -128,7 +128,7 @@ def test_sizes(b, form, dtype, rest, T, V, K, extra):
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("T,V,K", [(100, 2049, 20), (2500, 2300, 30), (1300, 4097, 9), (100, 6200, 40), (700, 12289, 33), (640, 16400, 500), (100, 24577, 20), (330, 30001, 1024), (310, 49153, 16),
-                                   (100, 66001, 64)])
+                                   (100, 66001, 64), (3601, 205, 16), (4003, 7, 3), (3700, 500, 130), (3555, 121, 40), (3600, 512, 700), (3999, 33, 33)])
 def test_many_rows(b, form, dtype, T, V, K):
     """More rows than blocks, with lists of every length, repeated words, and rows that are passed over, next to one another."""
     g = np.random.default_rng(T)

@@ -442,7 +442,8 @@ int flop_chain_fwd(const void* X, int64_t ldx, const void* Q, int64_t ldq, const
  *     scale[i] = max_j |X[i, j]| / 127,   Xq[i, j] = 127 X[i, j] / max_j |X[i, j]|  rounded half to even
  * The rounding is that of the exact quotient.  A row of zeros has scale 0 and zeros.  A row that holds an infinity or a NaN has
  * scale NaN and zeros, so that what is computed from it is NaN.  Rows are tokens (X[T, d_in]) or output channels
- * (Qc[k, d_in], Pc[d_out, k]).  Columns of Xq from cols on are left untouched.  Xq may not overlap X. */
+ * (Qc[k, d_in], Pc[d_out, k]).  Columns of Xq from cols on are left untouched.  Xq may not overlap X.
+ * At most 2^31 - 1 rows and 2^30 columns (FLOP_ERR_UNSUPPORTED beyond). */
 int flop_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dt, int8_t* Xq, int64_t ldxq,
                        float* scale, void* stream);
 

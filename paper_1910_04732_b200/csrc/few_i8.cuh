@@ -2,7 +2,8 @@
 // steps over KS of a block's eight warps, the weights read straight into registers (see gemm_few.cuh, whose form this is with bytes in place
 // of bf16: a lane's 16 bytes of a row serve two instructions, K permuted alike in both operands).
 //
-// Bound: latency.  What a launch costs here is the chain of loads it waits for, so the tokens are made where they are needed: every block
+// Bound: latency.  8 x 4096 x 1024: 3.1 us replayed, 16 x 4096 x 1024 4.4, 8 x 16384 x 4096 (67 MB of weights, 5.3 TB/s) 12.7.
+// What a launch costs here is the chain of loads it waits for, so the tokens are made where they are needed: every block
 // quantises (TOK_X) or requantises (TOK_H) all of them into its own shared memory, behind the request for its first weights,
 // instead of a launch before it that does so once and is waited for.  A pruned matrix is two launches: tokens -> 32-bit sums of the
 // first product; those -> result.  The work is repeated per block, so calls with many values of X per block take the launches

@@ -1215,10 +1215,9 @@ namespace {
 // ---- 8-bit integers with a scale per row
 bool i8_ok(const void* p, int64_t ld) { return aligned16(p) && (ld % 16) == 0; }
 constexpr int64_t kMaxI8K = 131071;      // products of two 8-bit values that a 32-bit sum holds whatever they are
+constexpr int64_t kMaxI8Cols = 1 << 30;  // of a row that is quantised: positions and a step beyond them in 32 bits
 constexpr int64_t kMaxI8Rows = 4000000;  // their tiles are counted in 32 bits
 
-constexpr int64_t kFewFused = 8;
-constexpr int64_t kFewQuantize = 4096;   // values a block of the few-token kernel quantises for itself
 struct I8Ws {
   int8_t* Xq; int64_t ldxq; float* x_scale;     // the tokens
   int* acc; int64_t ldacc;                      // sums of the first product
@@ -1238,7 +1237,13 @@ I8Ws plan_i8_ws(Arena& ar, int64_t T, int64_t d_in, int64_t k) {
   return w;
 }
 
-// `limit`: columns of the result that are written, zeros from `cols` on
+// Whether the blocks of a product of `T` tokens quantise all of them for themselves, `cols` values each, instead of a launch before it: that saves a
+// launch and its boundary, and costs every block the work on all values.  Pair of products, apart / here: 1 x 1024 -> 358 -> 4096 12.4 / 7.1 us, 8 of
+// them 12.3 / 9.2, 8 x 2048 -> 512 -> 4096 14.6 / 10.1, 16 x 512 -> 200 -> 2048 10.5 / 9.2, but 16 x 1024 -> 358 -> 4096 13.0 / 13.8.
+bool few_quantizes(int64_t T, int64_t cols) { return T <= 16 && T * cols <= (T <= 8 ? 16384 : 8192); }
+
+// `limit`: columns of the result that are written, zeros from `cols` on.  A row has as many of a block's warps as leave every SM two blocks' worth and
+// every lane a step: 16 x 4096 bf16 2.2 us (5.6 with a warp per row), 128 x 1024 2.0 (2.6), 4096 x 1024 with a warp per row 4.7 (10.8 with eight).
 template <int TOK>
 int launch_rows_i8(const void* X, int64_t ldx, int64_t rows, int64_t cols, const float* row_scale, const float* col_scale, int vec, int8_t* Xq, int64_t ldxq,
                    int64_t limit, float* scale, cudaStream_t st) {
@@ -1297,9 +1302,10 @@ int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int
   return FLOP_OK;
 }
 
-// Few tokens (few_i8.cuh).
+// Few tokens (few_i8.cuh), against tiles of 128: 16 x 4096 x 1024 4.4 / 6.4 us, 16 x 8192 x 4096 11.7 / 16.7, 24 x 4096 x 2048 7.4 / 8.8, 32 x 4096 x 1024
+// 5.8 / 6.3; from 17 tokens on the warp-level instruction is what large products wait for: 32 x 8192 x 1024 7.1 / 6.3, 32 x 16384 x 2048 16.9 / 10.8.
 bool few_i8_ok(int64_t T, int64_t N, int64_t K) {
-  return T <= 32 && i8::few_smem((int)T, (int)K, 4) <= (size_t)kSmemBudget && N <= INT32_MAX / 2;
+  return T <= 32 && (T <= 16 || (double)T * (double)N * (double)K <= 1.6e8) && i8::few_smem((int)T, (int)K, 4) <= (size_t)kSmemBudget && N <= INT32_MAX / 2;
 }
 template <int TOK, int OUT, int NT, int KS, bool EARLY>
 int launch_few_i8_inst(const i8::FewParams& p, cudaStream_t st) {
@@ -1316,10 +1322,15 @@ int launch_few_i8_inst(const i8::FewParams& p, cudaStream_t st) {
 }
 template <int TOK, int OUT, bool EARLY>
 int launch_few_i8(const i8::FewParams& p, cudaStream_t st) {
-  const bool wide = (p.N + 15) / 16 > 2 * num_sms() && p.K < 2048;
-  if (p.T <= 8) return wide ? launch_few_i8_inst<TOK, OUT, 1, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 1, 8, EARLY>(p, st);
-  if (p.T <= 16) return wide ? launch_few_i8_inst<TOK, OUT, 2, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 2, 8, EARLY>(p, st);
-  return wide ? launch_few_i8_inst<TOK, OUT, 4, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 4, 8, EARLY>(p, st);
+  const int nt = p.T <= 8 ? 1 : p.T <= 16 ? 2 : 4;
+  // A block's warps on K alone, 16 outputs to a block, or two to K and 64 outputs: fewer, longer-lived blocks where there would be more than two rounds
+  // of them.  K alone / two: 8 x 8192 x 1024 5.1 / 3.6 us, 8 x 16384 x 4096 15.4 / 12.7, 16 x 16384 x 2048 11.1 / 10.5, but 8 x 4096 x 1024 3.1 / 3.6 and, where
+  // a warp's share of K is long, 16 x 8192 x 4096 11.7 / 12.9, 1 x 8192 x 16384 44.8 / 53.7.
+  const bool wide = (p.N + 15) / 16 > 2 * num_sms() && (int64_t)p.K * nt < 8192;
+  if (nt == 1) return wide ? launch_few_i8_inst<TOK, OUT, 1, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 1, 8, EARLY>(p, st);
+  if (nt == 2) return wide ? launch_few_i8_inst<TOK, OUT, 2, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 2, 8, EARLY>(p, st);
+  if constexpr (TOK == i8::TOK_I8) return wide ? launch_few_i8_inst<TOK, OUT, 4, 2, EARLY>(p, st) : launch_few_i8_inst<TOK, OUT, 4, 8, EARLY>(p, st);
+  return FLOP_ERR_UNSUPPORTED;   // (more than 16 tokens come quantised: few_quantizes)
 }
 // One product of quantised tokens, in the form the sizes call for.
 template <typename T>
@@ -1330,7 +1341,9 @@ int launch_product_i8(const int8_t* A, int64_t lda, const float* a_scale, const 
   return launch_gemm_i8<T>(A, lda, a_scale, B, ldb, b_scale, Y, ldy, M, N, K, st);
 }
 
-// The first product of a compact pair with its rows quantised again in the same launch (see gemm_rowq_kernel).
+// The first product of a compact pair with its rows quantised again in the same launch (see gemm_rowq_kernel), wherever its cluster holds k.  Apart / here:
+// 64 x 1024 -> 358 -> 4096 18.1 / 14.7 us, 4096 of them 35.0 / 26.4, 4096 x 1024 -> 900 -> 4096 49.1 / 36.9, 16384 x 2048 -> 1024 -> 2048 129 / 118.  A row
+// block is cut into more parts than its width asks for while SMs are left: 150 x 410 -> 160 -> 2100 14.6 / 12.8 us, 512 x 1024 -> 358 -> 4096 18.0 / 16.0.
 bool rowq_ok(int64_t k) { return k <= (int64_t)i8::kRowqMaxCluster * i8::kRowqMaxSlice; }
 int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* col_scale, int8_t* Hq, int64_t ldhq, float* h_scale,
                 int64_t M, int64_t N, int64_t K, cudaStream_t st) {
@@ -2759,7 +2772,7 @@ int flop_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t cols, i
   if (rows == 0) return FLOP_OK;
   if (!scale || (cols > 0 && (!check_mat(X, ldx, cols) || !check_mat(Xq, ldxq, cols)))) return FLOP_ERR_INVALID_ARG;
   if (cols > 0 && ((dt == FLOP_BF16 && !bf16_ok(X, ldx)) || !i8_ok(Xq, ldxq))) return FLOP_ERR_UNSUPPORTED;
-  if (rows > INT32_MAX || cols > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX || cols > kMaxI8Cols) return FLOP_ERR_UNSUPPORTED;
   if (Span(X, rows, cols, ldx, elt(dt)).meets(Span(Xq, rows, cols, ldxq, 1))) return FLOP_ERR_INVALID_ARG;
   return launch_quantize_rows(X, ldx, rows, cols, dt, Xq, ldxq, scale, (cudaStream_t)stream);
 }
@@ -2797,7 +2810,7 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
     if (dt == FLOP_BF16) return launch_product_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
     return launch_product_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
   };
-  if (T <= kFewFused && few_i8_ok(T, k, d_in) && T * d_in <= kFewQuantize && few_i8_ok(T, d_out, k) && T * k <= kFewQuantize) {
+  if (few_quantizes(T, d_in) && few_quantizes(T, k) && few_i8_ok(T, k, d_in) && few_i8_ok(T, d_out, k)) {
     const i8::FewParams p = {X, ldx, nullptr, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, w.x_scale, (int)T, (int)k, (int)d_in, aligned16(X) && ldx % 4 == 0};
     const int rc = dt == FLOP_BF16 ? launch_few_i8<i8::TOK_BF16, i8::OUT_S32, false>(p, st) : launch_few_i8<i8::TOK_F32, i8::OUT_S32, false>(p, st);
     FLOP_TRY(rc);

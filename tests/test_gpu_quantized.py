@@ -122,7 +122,8 @@ def test_rows_behind_32_bit_offsets(b):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,N,K,extra", [(1, 1, 1, 0), (1, 4096, 1024, 0), (2, 33, 17, 1), (7, 100, 64, 0), (8, 16, 128, 0), (9, 250, 410, 2), (16, 1000, 358, 0), (17, 130, 1000, 0),
                                          (31, 65, 95, 1), (33, 2100, 410, 0), (64, 64, 512, 0), (65, 300, 4097, 0), (127, 129, 130, 0), (128, 256, 128, 0), (150, 2100, 410, 1),
-                                         (256, 256, 256, 0), (257, 511, 385, 0), (300, 70, 2048, 0), (1000, 1000, 1000, 0), (600, 2600, 144, 0), (4096, 358, 200, 0), (2000, 4096, 64, 1)])
+                                         (256, 256, 256, 0), (257, 511, 385, 0), (300, 70, 2048, 0), (1000, 1000, 1000, 0), (600, 2600, 144, 0), (4096, 358, 200, 0), (2000, 4096, 64, 1),
+                                         (5, 5001, 2100, 0), (16, 5003, 2047, 1), (32, 5000, 1100, 0), (24, 4801, 1001, 2)])
 def test_products(b, dtype, M, N, K, extra):
     g = np.random.default_rng(M + N + K)
     A, B = whole(g, M, K, extra, -128), whole(g, N, K, 0, -128)

@@ -26,7 +26,7 @@ def quantize(lib, X=P, ldx=64, rows=4, cols=64, dt=b.BF16, Xq=4 * P, ldxq=64, sc
     (dict(X=None), b.ERR_INVALID_ARG), (dict(Xq=None), b.ERR_INVALID_ARG), (dict(scale=None), b.ERR_INVALID_ARG),
     (dict(ldx=56), b.ERR_INVALID_ARG), (dict(ldxq=48), b.ERR_INVALID_ARG), (dict(X=P + 8), b.ERR_UNSUPPORTED), (dict(ldx=65), b.ERR_UNSUPPORTED),
     (dict(Xq=4 * P + 8), b.ERR_UNSUPPORTED), (dict(ldxq=72), b.ERR_UNSUPPORTED), (dict(Xq=P), b.ERR_INVALID_ARG), (dict(Xq=P + 256), b.ERR_INVALID_ARG),
-    (dict(rows=1 << 31), b.ERR_UNSUPPORTED)])
+    (dict(rows=1 << 31), b.ERR_UNSUPPORTED), (dict(cols=(1 << 30) + 1, ldx=1 << 31, ldxq=1 << 31), b.ERR_UNSUPPORTED)])
 def test_quantize_rows(lib, change, code):
     assert quantize(lib, **change) == code
 

@@ -325,7 +325,7 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
 }
 
 // The same for a whole matrix, 8 / per_row rows to a block; columns behind `limit` of the result are left alone.
-// Bound: HBM for many rows.  For few rows, latency: a lane's values are a chain of some ten instructions each, eleven cycles apiece with two warps
+// Bound: HBM for many rows (16384 x 2048 bf16 24.4 us, 4.1 TB/s; two passes over a row, the second from L1).  For few rows, latency: a lane's values are a chain of some ten instructions each, eleven cycles apiece with two warps
 // to a scheduler, so a row is spread over as many warps as leave every SM a block.
 template <int TOK>
 __global__ void __launch_bounds__(kFewThreads)

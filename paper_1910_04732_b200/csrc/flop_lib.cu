@@ -1241,6 +1241,9 @@ I8Ws plan_i8_ws(Arena& ar, int64_t T, int64_t d_in, int64_t k) {
 // launch and its boundary, and costs every block the work on all values.  Pair of products, apart / here: 1 x 1024 -> 358 -> 4096 12.4 / 7.1 us, 8 of
 // them 12.3 / 9.2, 8 x 2048 -> 512 -> 4096 14.6 / 10.1, 16 x 512 -> 200 -> 2048 10.5 / 9.2, but 16 x 1024 -> 358 -> 4096 13.0 / 13.8.
 bool few_quantizes(int64_t T, int64_t cols) { return T <= 16 && T * cols <= (T <= 8 ? 16384 : 8192); }
+// The same for the sums of the first product, which are scaled in fp64: 8 x 4096 -> 800 -> 4096 22.2 / 16.0 us, 1 x 16384 -> 1000 -> 4096 52.8 / 15.2,
+// 16 x 512 -> 256 -> 2048 10.6 / 9.2, but 8 x 4096 -> 2000 -> 4096 16.0 / 21.2 and 16 x 200 -> 500 -> 2048 11.8 / 12.1.
+bool few_requantizes(int64_t T, int64_t k) { return T <= 16 && T * k <= (T <= 8 ? 8192 : 6144); }
 
 // `limit`: columns of the result that are written, zeros from `cols` on.  A row has as many of a block's warps as leave every SM two blocks' worth and
 // every lane a step: 16 x 4096 bf16 2.2 us (5.6 with a warp per row), 128 x 1024 2.0 (2.6), 4096 x 1024 with a warp per row 4.7 (10.8 with eight).
@@ -2810,10 +2813,17 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
     if (dt == FLOP_BF16) return launch_product_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
     return launch_product_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
   };
-  if (few_quantizes(T, d_in) && few_quantizes(T, k) && few_i8_ok(T, k, d_in) && few_i8_ok(T, d_out, k)) {
-    const i8::FewParams p = {X, ldx, nullptr, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, w.x_scale, (int)T, (int)k, (int)d_in, aligned16(X) && ldx % 4 == 0};
-    const int rc = dt == FLOP_BF16 ? launch_few_i8<i8::TOK_BF16, i8::OUT_S32, false>(p, st) : launch_few_i8<i8::TOK_F32, i8::OUT_S32, false>(p, st);
-    FLOP_TRY(rc);
+  // few tokens: the sums of the first product go to the second one, whose blocks quantise them again
+  const bool here = few_quantizes(T, d_in);
+  if ((here || T <= 8) && few_requantizes(T, k) && few_i8_ok(T, k, d_in) && few_i8_ok(T, d_out, k)) {
+    if (here) {
+      const i8::FewParams p = {X, ldx, nullptr, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, w.x_scale, (int)T, (int)k, (int)d_in, aligned16(X) && ldx % 4 == 0};
+      const int rc = dt == FLOP_BF16 ? launch_few_i8<i8::TOK_BF16, i8::OUT_S32, false>(p, st) : launch_few_i8<i8::TOK_F32, i8::OUT_S32, false>(p, st);
+      FLOP_TRY(rc);
+    } else {
+      FLOP_TRY(launch_quantize_rows(X, ldx, T, d_in, dt, w.Xq, w.ldxq, w.x_scale, st));
+      FLOP_TRY(launch_product_i8<int>(w.Xq, w.ldxq, nullptr, Qq, ldqq, nullptr, w.acc, w.ldacc, T, k, d_in, st));
+    }
     const i8::FewParams p2 = {w.acc, w.ldacc, w.x_scale, q_scale, Pq, ldpq, p_scale, Y, ldy, nullptr, (int)T, (int)d_out, (int)k, aligned16(q_scale)};
     return dt == FLOP_BF16 ? launch_few_i8<i8::TOK_H, i8::OUT_BF16, true>(p2, st) : launch_few_i8<i8::TOK_H, i8::OUT_F32, true>(p2, st);
   }

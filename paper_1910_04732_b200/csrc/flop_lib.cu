@@ -1345,7 +1345,7 @@ int launch_product_i8(const int8_t* A, int64_t lda, const float* a_scale, const 
 }
 
 // The first product of a compact pair with its rows quantised again in the same launch (see gemm_rowq_kernel), wherever its cluster holds k.  Apart / here:
-// 64 x 1024 -> 358 -> 4096 18.1 / 14.7 us, 4096 of them 35.0 / 26.4, 4096 x 1024 -> 900 -> 4096 49.1 / 36.9, 16384 x 2048 -> 1024 -> 2048 129 / 118.  A row
+// 64 x 1024 -> 358 -> 4096 18.1 / 14.7 us, 4096 of them 35.0 / 26.4, 4096 x 1024 -> 900 -> 4096 49.1 / 36.9, 16384 x 2048 -> 1024 -> 2048 129 / 107.  A row
 // block is cut into more parts than its width asks for while SMs are left: 150 x 410 -> 160 -> 2100 14.6 / 12.8 us, 512 x 1024 -> 358 -> 4096 18.0 / 16.0.
 bool rowq_ok(int64_t k) { return k <= (int64_t)i8::kRowqMaxCluster * i8::kRowqMaxSlice; }
 int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* col_scale, int8_t* Hq, int64_t ldhq, float* h_scale,
@@ -1361,7 +1361,10 @@ int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t
   p.M = (int)M; p.N = (int)N; p.num_kb = (int)((K + i8::kBK - 1) / i8::kBK); p.parts = parts;
   p.slice = (int)round_up((N + parts - 1) / parts, 16);
   const int sb = (int)i8::rowq_stage_bytes(p.slice);
-  p.stages = std::min({tc::kMaxStages, (kSmemBudget - (int)i8::kRowqFixed) / sb, std::max(p.num_kb, 2)});
+  // more blocks than SMs: two to an SM, so that one's epilogue runs beside the other's main loop (16384 x 2048 -> 1024 -> 2048 118 -> 107 us,
+  // 32768 x 768 -> 300 -> 768 82 -> 72); a shorter ring then, but two of them
+  const bool two = row_blocks * parts > num_sms();
+  p.stages = std::min({tc::kMaxStages, ((two ? 112 * 1024 : kSmemBudget) - (int)i8::kRowqFixed) / sb, std::max(p.num_kb, 2)});
   FLOP_TRY(make_tmap(&p.ta, A, M, K, lda, i8::kBK, tc::BM, true));
   FLOP_TRY(make_tmap(&p.tb, B, N, K, ldb, i8::kBK, (uint32_t)p.slice, true));
   p.a_scale = a_scale; p.col_scale = col_scale; p.out = Hq; p.ldo = ldhq; p.h_scale = h_scale;

@@ -212,6 +212,18 @@ def test_compact_forward(b, dtype, T, d_in, k, d_out, extra):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,d_in,k,d_out", [(5000, 600, 901, 70), (9000, 300, 300, 64), (19001, 150, 60, 33)])
+def test_compact_forward_of_many_tokens(b, dtype, T, d_in, k, d_out):
+    """More blocks of the first product than SMs; the rows looked at are the first, the last and some between."""
+    g = np.random.default_rng(T)
+    x, f = tokens(g, T, d_in, dtype), factors(g, k, d_in, d_out)
+    Y = run_compact(b, x, *f)
+    pick = np.unique(np.r_[:130, T - 130:T, g.integers(0, T, 300)])
+    want, _ = O.compact_fwd_i8(host(x)[pick], *(host(t) for t in f))
+    check_scaled(Y[torch.from_numpy(pick).cuda()], want, dtype, 6)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_a_token_does_not_depend_on_the_others(b, dtype):
     """Bit for bit the same in calls of every length: the integers and the order of the scalings do not depend on the kernels."""
     g = np.random.default_rng(2)

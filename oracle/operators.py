@@ -31,12 +31,17 @@ def gemm_i8(a, b, a_scale, b_scale):
 
 
 def compact_fwd_i8(x, qq, q_scale, pq, p_scale):
-    """(Y, the intermediate's integers).  The token's scale is common to a row of H and leaves its integers alone."""
+    """(Y, the intermediate's integers).  The token's scale is common to a row of H and leaves its integers alone; a row of H that is not
+    finite (a channel whose scale is not) has none."""
     xq, x_scale = quantize_rows(x)
-    h = (xq.astype(np.float64) @ np.asarray(qq, dtype=np.float64).T) * np.asarray(q_scale, dtype=np.float64)
+    with np.errstate(invalid="ignore"):                      # 0 times infinity
+        h = (xq.astype(np.float64) @ np.asarray(qq, dtype=np.float64).T) * np.asarray(q_scale, dtype=np.float64)
     hq, h_scale = np.zeros(h.shape, dtype=np.int64), np.zeros(h.shape[0])
     for i, row in enumerate(h):
         amax = np.abs(row).max()
+        if not np.isfinite(amax):
+            h_scale[i] = np.nan
+            continue
         if amax > 0:
             hq[i] = np.rint(127.0 * row / amax).astype(np.int64)
         h_scale[i] = float(x_scale[i]) * amax / 127.0

@@ -134,17 +134,27 @@ __device__ __noinline__ uint2 round8_wide(const char* at, int n, double amax) {
   }
   return make_uint2(w[0], w[1]);
 }
-// Sums times their columns' scales, in fp64 (exact as long as a sum has 29 bits): eight products from k on, 0 behind K.
-__device__ __forceinline__ void products8(const FewParams& p, const char* row, int k, double (&h)[8]) {
+// Sums times their columns' scales, in fp64 (exact as long as a sum has 29 bits): eight products from k on, 0 behind K.  They are finite
+// where the scales are: `poison` (CHECK) takes 0 times every scale, and stays 0 or becomes a NaN for good.
+template <bool CHECK>
+__device__ __forceinline__ void products8(const FewParams& p, const char* row, int k, double (&h)[8], float& poison) {
   if (k + 8 <= p.K && p.vec) {
     const int4 x = *reinterpret_cast<const int4*>(row + 4 * k), y = *reinterpret_cast<const int4*>(row + 4 * k + 16);
     const float4 c = __ldg(reinterpret_cast<const float4*>(p.col + k)), d = __ldg(reinterpret_cast<const float4*>(p.col + k) + 1);
     h[0] = (double)x.x * (double)c.x; h[1] = (double)x.y * (double)c.y; h[2] = (double)x.z * (double)c.z; h[3] = (double)x.w * (double)c.w;
     h[4] = (double)y.x * (double)d.x; h[5] = (double)y.y * (double)d.y; h[6] = (double)y.z * (double)d.z; h[7] = (double)y.w * (double)d.w;
+    if (CHECK) {
+      poison = fmaf(c.w, 0.f, fmaf(c.z, 0.f, fmaf(c.y, 0.f, fmaf(c.x, 0.f, poison))));
+      poison += fmaf(d.w, 0.f, fmaf(d.z, 0.f, fmaf(d.y, 0.f, d.x * 0.f)));
+    }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) h[i] = k + i < p.K ? (double)reinterpret_cast<const int*>(row)[k + i] * (double)__ldg(p.col + k + i) : 0.0;
+  for (int i = 0; i < 8; ++i) {
+    const float s = k + i < p.K ? __ldg(p.col + k + i) : 0.f;
+    h[i] = k + i < p.K ? (double)reinterpret_cast<const int*>(row)[k + i] * (double)s : 0.0;
+    if (CHECK) poison = fmaf(s, 0.f, poison);
+  }
 }
 __device__ __forceinline__ uint2 round8_sums(const double (&h)[8], float inv, double exact, bool careful) {
   uint32_t b[8];
@@ -198,23 +208,26 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
   }
   double exact[R];
   if (TOK == TOK_H) {
-    // positive doubles compare as integers (a NaN is the largest): the high words first, the low ones among those that have the highest
+    // positive doubles compare as integers: across the lanes the high words first, then the low ones among those that have the highest
 #pragma unroll
     for (int r = 0; r < R; ++r) exact[r] = 0.0;
+    float poison = 0.f;
 #pragma unroll 1
     for (; k_more < p.K; k_more += step)
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         double h[8];
-        products8(p, row_of(r), k_more, h);
+        if (r == 0) products8<true>(p, row_of(r), k_more, h, poison);      // (the scales are those of every row)
+        else products8<false>(p, row_of(r), k_more, h, poison);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const double x = fabs(h[i]);
-          if (!(x <= exact[r])) exact[r] = x;
+          if (x > exact[r]) exact[r] = x;
         }
       }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      if (!(poison == 0.f)) exact[r] = (double)INFINITY;                   // one channel without a scale, and no token has one
       const uint32_t mine = (uint32_t)__double2hiint(exact[r]), hi = __reduce_max_sync(0xffffffffu, mine);
       const uint32_t low = __reduce_max_sync(0xffffffffu, mine == hi ? (uint32_t)__double2loint(exact[r]) : 0u);
       exact[r] = __hiloint2double((int)hi, (int)low);
@@ -223,10 +236,7 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
       double* red64 = reinterpret_cast<double*>(red);
       if (lane == 0) red64[warp] = exact[0];
       __syncthreads();
-      for (int w = 0; w < per_row; ++w) {
-        const double x = red64[first * per_row + w];
-        if (!(x <= exact[0])) exact[0] = x;
-      }
+      for (int w = 0; w < per_row; ++w) exact[0] = fmax(exact[0], red64[first * per_row + w]);
     }
   } else {
 #pragma unroll 1
@@ -300,7 +310,8 @@ __device__ __forceinline__ void make_tokens(const FewParams& p, int8_t* tile, in
         if (TOK != TOK_H) load8<TOK>(p, row_of(r), k, v);
         if (TOK == TOK_H) {
           double h[8];
-          products8(p, row_of(r), k, h);
+          float unused;
+          products8<false>(p, row_of(r), k, h, unused);
           w = round8_sums(h, inv[r], exact[r], careful[r]);
         } else if (careful[r]) {
           w = round8_wide<TOK>(at, p.K - k, exact[r]);

@@ -460,6 +460,7 @@ int flop_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
  *     h[t, j] = acc[t, j] q_scale[j],   hq[t, j] = 127 h[t, j] / max_j |h[t, j]|  rounded half to even (as fp64 has it),
  *     h_scale[t] = x_scale[t] max_j |h[t, j]| / 127,   Y[t, n] = (sum_j hq[t, j] Pq[n, j]) * h_scale[t] * p_scale[n]
  * The integers do not depend on the number of tokens in the call or on the kernels that serve it, and a token's result only on that token.
+ * A row of h that is not finite (a token, or any q_scale, that is not) has hq = 0 and h_scale NaN: its Y is NaN.
  * ws: flop_workspace_bytes(FLOP_OP_COMPACT_FWD_I8, T, d_in, d_out, k, dt). */
 int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ldqq, const float* q_scale,
                         const int8_t* Pq, int64_t ldpq, const float* p_scale, void* Y, int64_t ldy, int64_t T,

@@ -468,7 +468,7 @@ gemm_rowq_kernel(const __grid_constant__ RowqParams p) {
         x[e] = fabsf((float)(int)v[e] * sc[e]);
         here = __uint_as_float(max(__float_as_uint(here), __float_as_uint(x[e])));      // (a NaN is the largest)
       }
-      if (!(here < top)) {
+      if (__float_as_uint(here) >= __float_as_uint(top)) {                // (bits again: a NaN is not replaced)
         if (!(here == top)) rest = -INFINITY;
         top = here;
 #pragma unroll
@@ -495,6 +495,7 @@ gemm_rowq_kernel(const __grid_constant__ RowqParams p) {
       }
       if (far) best = b;
     }
+    if (!(best < (double)INFINITY)) best = (double)INFINITY;              // a channel without a scale: so is the row, and fmax below would drop a NaN
     // every CTA's maxima to every CTA, then the row's
     {
       const uint32_t at = max_base + (uint32_t)(((part * 2 + h) * 128 + r) * 8);

@@ -39,3 +39,11 @@ def poisoned(b, dtype, T, d_in, k, d_out):  # noqa: F811
                                             (8, 4096, 143, 40), (12, 96, 143, 50), (16, 96, 358, 64), (16, 64, 17, 40), (40, 96, 1500, 50), (300, 64, 1030, 40)])
 def test_sums_scaled_in_fp64(b, dtype, T, d_in, k, d_out):  # noqa: F811
     poisoned(b, dtype, T, d_in, k, d_out)
+
+
+# the first product's epilogue: one to four blocks to a row, whole and ragged slices
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,d_in,k,d_out", [(9, 1024, 358, 64), (12, 96, 600, 50), (16, 600, 900, 40), (17, 64, 17, 40), (40, 96, 143, 50), (40, 200, 358, 64), (130, 96, 600, 64),
+                                            (300, 96, 16, 33), (300, 96, 143, 50), (300, 128, 1024, 40), (2500, 64, 300, 33)])
+def test_sums_scaled_in_the_epilogue(b, dtype, T, d_in, k, d_out):  # noqa: F811
+    poisoned(b, dtype, T, d_in, k, d_out)

@@ -619,9 +619,11 @@ __device__ __noinline__ void row_lists(const Args& a, unsigned char* smem, Sums 
       const float s = warp_all(u.m == -INFINITY ? u.s : u.s * pow2_of(__fmul_rn(u.m, a.c) - m_rest), add<float>);
       // relative to the larger reference
       const float mc = o.top > 0.f || o.top != o.top ? fmaxf(o.top_ref, m == -INFINITY ? o.top_ref : m_rest) : m_rest;
-      const float on = o.top * pow2_of(o.top_ref - mc);
+      // (a list that the student rules out whole has no reference: 0 at one far above the rest's would be 0 times infinity)
+      const float to_mc = o.top == 0.f ? 0.f : pow2_of(o.top_ref - mc);
+      const float on = o.top * to_mc;
       const float all = on + (s > 0.f ? s * pow2_of(m_rest - mc) : s);
-      all_inv = pow2_of(o.top_ref - mc) / all;
+      all_inv = to_mc / all;
       if (lane == 0) {
         const double l2a = log2_of(all);
         // the terms' logarithms are relative to the list's reference

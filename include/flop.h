@@ -474,7 +474,8 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
  *   t_lse[T]:    q = exp(t / tau - t_lse), t_lse the teacher's log sum of exp(t / tau) over ALL words, r = max(0, 1 - sum_L q)
  *                (0 if L is the whole vocabulary)          loss = sum_L q (log q - log p) + r (log r - log p_rest)
  *   p_rest = sum of p outside L: the rest of the vocabulary is one more bucket.
- *   dS[t, v] = g (p_v - q_v) on L, g (p_v - r p_v / p_rest) outside; g = weight[t] / tau (times dloss[t] in _bwd)
+ *   dS[t, v] = g (n p_v - q_v) on L, g (n p_v - r p_v / p_rest) outside; g = weight[t] / tau (times dloss[t] in _bwd); n = sum_L q + r, which
+ *   is 1 but where r is 0: a list that sums to more than one (t_logits or t_lse kept in fewer bits), or that is the whole vocabulary
  * weight[T] (nullable: 1) multiplies loss and gradient.  Tokens with g = 0 (loss: weight = 0) and tokens whose list is empty have
  * loss 0 and gradient 0, whatever their logits hold.  A NaN or +infinity among the other tokens' logits makes the
  * loss NaN; -infinity (a word that is masked out) has probability 0.

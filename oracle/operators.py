@@ -81,6 +81,8 @@ def distill_row(s, t_logits, t_idx, t_lse, weight, tau):
     if r > 0:
         terms.append(r * (math.log(r) - (rest - lse)))
     p = np.exp(s - lse)
+    if t_lse is not None:
+        p = p * (math.fsum(q) + r)                           # every term holds a -log p of its own weight
     grad = p.copy()
     grad[listed] -= q
     pull, log_r = np.zeros(V), 0.0

@@ -5,7 +5,8 @@
 // [0, V); of equal indices the first):
 //     without t_lse   q = softmax over L of t c                   loss = sum_L q (log q - log p)
 //     with t_lse      q = exp(t c - t_lse), r = 1 - sum_L q       loss = sum_L q (log q - log p) + r (log r - log p_rest)
-// where p_rest is the student's mass outside L.  Gradient: c (p_v - q_v) on L and c (p_v - r p_v / p_rest) outside it.
+// (r = 0 where the list sums to more than one or is the whole vocabulary) and p_rest is the student's mass outside L.  Every term has a -log p in it, so
+// the gradient is c (n p_v - q_v) on L and c (n p_v - r p_v / p_rest) outside it, n = sum_L q + r: one, but where r is 0.
 //
 // The sums outside L are taken over the words outside L, not as one minus the rest: a student that agrees with its teacher leaves a
 // tail of 1e-3 there, which a difference of sums near one holds to four digits.  A bit per word says which are listed (a repeated
@@ -355,6 +356,7 @@ __global__ void __launch_bounds__(part_threads(G), P > 4 || G < 32 ? 1024 / part
   }
   const float r = a.t_lse && f.n < (float)a.V ? (float)fmax(0.0, 1.0 - h.a) : 0.f;
   const float q_norm = a.t_lse ? 1.f : (float)(1.0 / h.a);
+  const float mass = !a.t_lse || r > 0.f ? 1.f : (float)h.a;              // sum q + r
   if (MODE & FWD) {
     const double l2a = log2_of(h.top + (f.s > 0.f ? f.s * pow2_of(m_rest - mc) : f.s));
     l2all = (float)l2a;
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(part_threads(G), P > 4 || G < 32 ? 1024 / part
   }
   if (MODE & BWD) {
     // outside the list: 2^(x - m_rest) times what is common to the row
-    const float pull = l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - mc - l2all) - r * ex2(-l2rest));
+    const float pull = l2rest == -INFINITY ? 0.f : g * (mass * ex2(m_rest - mc - l2all) - r * ex2(-l2rest));
     // keeps the compiler from holding the row unpacked across the reductions (123 registers instead of 80)
 #pragma unroll
     for (int i = 0; i < P; ++i) asm volatile("" : "+r"(d[i].x), "+r"(d[i].y), "+r"(d[i].z), "+r"(d[i].w));
@@ -380,7 +382,7 @@ __global__ void __launch_bounds__(part_threads(G), P > 4 || G < 32 ? 1024 / part
     sync();                                             // the zeros of the listed words are written
     for (int j = tid; j < a.K; j += G) {
       const int idx = slot_idx[j], at = idx / kPer<T>;
-      if (idx >= 0 && at >= lo && at < hi) dS[idx] = from_f32<T>(g * (ex2(fmaf(slot_x[j], a.c, -mc) - l2all) - slot_t[j] * q_norm));
+      if (idx >= 0 && at >= lo && at < hi) dS[idx] = from_f32<T>(g * (mass * ex2(fmaf(slot_x[j], a.c, -mc) - l2all) - slot_t[j] * q_norm));
     }
   }
 }
@@ -449,7 +451,7 @@ constexpr int kLane = 4;                                                 // slot
 
 constexpr int kBits = 1, kSums = 3, kStored = 4;                        // named barriers (kBits and kBits + 1 in turn)
 struct Sums { float m, s; };                                             // maximum (logit) and sum outside the list, relative to 2^(m c)
-struct Info { double q, kl; float top_ref, top, r, mc, l2all, m_rest, l2rest; int empty; };
+struct Info { double q, kl; float top_ref, top, r, mass, mc, l2all, m_rest, l2rest; int empty; };      // (mass = q + r)
 
 // The next row of a block that is looked at, from `row` on; those passed over get their loss (the list's warp) and their zeros (the others).
 template <typename T, int MODE>
@@ -596,6 +598,7 @@ __device__ __noinline__ void row_lists(const Args& a, unsigned char* smem, Sums 
       Info& o = info[side];
       o.q = sum_q; o.kl = kl; o.top_ref = ref; o.top = top;
       o.r = a.t_lse && n < a.V ? (float)fmax(0.0, 1.0 - sum_q) : 0.f;
+      o.mass = !a.t_lse || o.r > 0.f ? 1.f : (float)sum_q;
       o.empty = n == 0 || (!a.t_lse && mt == -INFINITY);               // an empty list, or one that gives every word nothing
       if (MODE == BWD) { const float* st = a.stats_in + 4 * row; o.mc = st[0]; o.l2all = st[1]; o.m_rest = st[2]; o.l2rest = st[3]; }
     }
@@ -623,7 +626,7 @@ __device__ __noinline__ void row_lists(const Args& a, unsigned char* smem, Sums 
       const float to_mc = o.top == 0.f ? 0.f : pow2_of(o.top_ref - mc);
       const float on = o.top * to_mc;
       const float all = on + (s > 0.f ? s * pow2_of(m_rest - mc) : s);
-      all_inv = to_mc / all;
+      all_inv = o.mass * to_mc / all;
       if (lane == 0) {
         const double l2a = log2_of(all);
         // the terms' logarithms are relative to the list's reference
@@ -642,7 +645,7 @@ __device__ __noinline__ void row_lists(const Args& a, unsigned char* smem, Sums 
       bar_sync(kStored, G);
       for (int j = lane; j < a.K; j += 32)
         if (l.idx[j] >= 0 && !o.empty) {
-          const float p = MODE == BWD ? ex2(fmaf(l.x[j], a.c, -o.mc) - o.l2all) : l.x[j] * all_inv;
+          const float p = MODE == BWD ? o.mass * ex2(fmaf(l.x[j], a.c, -o.mc) - o.l2all) : l.x[j] * all_inv;
           dS0[row * a.ldds + l.idx[j]] = from_f32<T>(g * (p - l.t[j] * q_norm));
         }
     }
@@ -760,14 +763,14 @@ __global__ void __launch_bounds__(G, 1024 / G) row_kernel(const __grid_constant_
       float m_rest, pull;
       if (MODE == BWD) {
         m_rest = o.m_rest;
-        pull = o.l2rest == -INFINITY ? 0.f : g * (ex2(m_rest - o.mc - o.l2all) - r * ex2(-o.l2rest));
+        pull = o.l2rest == -INFINITY ? 0.f : g * (o.mass * ex2(m_rest - o.mc - o.l2all) - r * ex2(-o.l2rest));
       } else {
         const Sums u = lane < NW ? sums[side][lane] : Sums{-INFINITY, 0.f};
         const float ma = warp_all(u.m, max2);
         m_rest = ma == -INFINITY ? 0.f : __fmul_rn(ma, a.c);
         const float s = warp_all(u.m == -INFINITY ? u.s : u.s * ex2(__fmul_rn(u.m, a.c) - m_rest), add<float>);
-        // 1 / (all words' sum) - r / (the rest's), both relative to the rest's maximum; a list far above it makes the first one 0
-        pull = s == 0.f ? 0.f : g * (1.f / (s + (o.top == 0.f ? 0.f : o.top * ex2(o.top_ref - m_rest))) - r / s);
+        // mass / (all words' sum) - r / (the rest's), both relative to the rest's maximum; a list far above it makes the first one 0
+        pull = s == 0.f ? 0.f : g * (o.mass / (s + (o.top == 0.f ? 0.f : o.top * ex2(o.top_ref - m_rest))) - r / s);
       }
       const bool empty = o.empty;
       T* dS = dS0 + row * a.ldds;

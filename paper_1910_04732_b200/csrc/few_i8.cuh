@@ -70,7 +70,8 @@ __device__ __forceinline__ void load8(const FewParams& p, const char* row, int k
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
     } else {
-      const float4 x = *reinterpret_cast<const float4*>(row + 4 * k), y = *reinterpret_cast<const float4*>(row + 4 * k + 16);
+      const float4* at = reinterpret_cast<const float4*>(row) + k / 4;                  // (a row may have 2^30 values, 4 GB)
+      const float4 x = at[0], y = at[1];
       v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
     }
     return;

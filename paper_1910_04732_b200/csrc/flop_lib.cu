@@ -37,6 +37,7 @@
 #include "quantized.cuh"
 #include "gemm_i8.cuh"
 #include "few_i8.cuh"
+#include "tile_widths.cuh"
 
 using namespace flop;
 typedef __nv_bfloat16 bf16;
@@ -237,7 +238,7 @@ constexpr int kSmemFixed = 1024 + (int)tc::kStoreBufTotal + kSmemBarrierBytes;  
 // cost model in SM cycles: waves over the machine x (k-blocks per work item x the slower of MMA
 // issue and shared-memory fill, plus the epilogue).  The fill rate of one SM's shared memory was
 // measured at about 54 bytes per cycle; a 128 x bn x 64 MMA block takes 2*bn cycles.
-TcPlan plan_tc(int64_t M, int64_t N, int64_t K, bool allow_split, bool b_mn_major, bool allow_cta2 = true) {
+TcPlan plan_tc(int64_t M, int64_t N, int64_t K, bool allow_split, bool b_mn_major, bool allow_cta2 = true, bool bytes = false) {
   const int sms = num_sms();
   const int num_kb = (int)((K + tc::BK - 1) / tc::BK);
   const int force_bn = tuning().tc_bn, force_stages = tuning().tc_stages, force_cta2 = tuning().tc_cta2;
@@ -253,11 +254,10 @@ TcPlan plan_tc(int64_t M, int64_t N, int64_t K, bool allow_split, bool b_mn_majo
     if (pass == 0 && allow_cta2 && ((force_cta2 == 1 && !cta2) || (force_cta2 == 2 && cta2))) continue;
     for (int bi = 0; bi < 5; ++bi) {
       const int bn = bns[bi];
-      if (bn == 208 && (force_bn != 208 || !cta2 || b_mn_major)) continue;
+      if (!tc::tile_width_ok(bn, cta2, b_mn_major, bytes) || (bn == 208 && force_bn != 208)) continue;
       const bool forced_bn = pass == 0 && force_bn;
       if (forced_bn && bn != force_bn) continue;
       if (!forced_bn && bn > 64 && bn - 64 >= N) continue;   // a smaller tile already covers N
-      if (cta2 && b_mn_major && (bn / 2) % 64 != 0) continue;  // MN-major halves come in 64-wide boxes
       const int bm = cta2 ? tc::BM2 : tc::BM;
       const int units = cta2 ? sms / 2 : sms;                 // CTA pairs or CTAs that run at once
       const int tiles_m = (int)((M + bm - 1) / bm), tiles_n = (int)((N + bn - 1) / bn);
@@ -690,9 +690,8 @@ GroupShape plan_group(const std::vector<Mnk>& jobs, bool b_mn_major, bool wgrad 
     if (pairs_only && !cta2) continue;
     for (int c = 0; c < 5; ++c) {
       const int bn = cand[c];
-      if (bn == 208 && (force_bn != 208 || !cta2 || b_mn_major)) continue;
+      if (!tc::tile_width_ok(bn, cta2, b_mn_major, false) || (bn == 208 && force_bn != 208)) continue;
       if (pass == 0 && force_bn && bn != force_bn) continue;
-      if (cta2 && b_mn_major && (bn / 2) % 64 != 0) continue;
       const int bm = cta2 ? tc::BM2 : tc::BM;
       const int units = cta2 ? sms / 2 : sms;
       double items = 0, kb_sum = 0;
@@ -1268,7 +1267,8 @@ template <typename T>
 int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, T* Y, int64_t ldy, int64_t M,
                    int64_t N, int64_t K, cudaStream_t st) {
   constexpr int OUT = std::is_same<T, bf16>::value ? i8::OUT_BF16 : std::is_same<T, float>::value ? i8::OUT_F32 : i8::OUT_S32;
-  const TcPlan pl = plan_tc(M, N, (K + 1) / 2, false, false);       // a k-block of 128 values moves the bytes and takes the cycles of 64 bf16 ones
+  const TcPlan pl = plan_tc(M, N, (K + 1) / 2, false, false, true, true);       // a k-block of 128 values moves the bytes and takes the cycles of 64 bf16 ones
+  if (!tc::tile_width_ok(pl.bn, pl.cta2, false, true)) return FLOP_ERR_UNSUPPORTED;
   i8::GemmParams p;
   memset(&p, 0, sizeof(p));
   FLOP_TRY(make_tmap(&p.ta, A, M, K, lda, i8::kBK, tc::BM, true));

@@ -453,7 +453,8 @@ gemm_rowq_kernel(const __grid_constant__ RowqParams p) {
     // the largest product of this thread's columns: rounded, and its rounding error
     float top = 0.f, rest = 0.f;
     int longest = 0;
-    const int cols_here = ok ? nchunks * 32 : 0;                          // this thread's: 16 h .. 16 h + 15 of every 32
+    // this thread's: 16 h .. 16 h + 15 of every 32, up to the slice's end (a multiple of 16): what lies in tensor memory behind it is an older kernel's
+    const int cols_here = ok ? min(nchunks * 32, p.slice) : 0;
     auto next_cols = [](int n) { return n + ((n & 8) ? 24 : 8); };
 #pragma unroll 1
     for (int n = 16 * h; n < cols_here; n = next_cols(n)) {

@@ -47,3 +47,17 @@ def test_sums_scaled_in_fp64(b, dtype, T, d_in, k, d_out):  # noqa: F811
                                             (300, 96, 16, 33), (300, 96, 143, 50), (300, 128, 1024, 40), (2500, 64, 300, 33)])
 def test_sums_scaled_in_the_epilogue(b, dtype, T, d_in, k, d_out):  # noqa: F811
     poisoned(b, dtype, T, d_in, k, d_out)
+
+
+@pytest.mark.parametrize("T,d_in,k,d_out", [(150, 410, 143, 60), (300, 264, 300, 96), (300, 96, 16, 33)])
+def test_slices_that_end_inside_32_columns(b, T, d_in, k, d_out):  # noqa: F811
+    """The maximum of a row is taken over what this product put into tensor memory, not over the fp32 sums that another one left behind it."""
+    g = np.random.default_rng(k)
+    x, f = tokens(g, T, d_in, torch.bfloat16), factors(g, k, d_in, d_out)
+    want = run_compact(b, x, *f)
+    check_scaled(want, O.compact_fwd_i8(host(x), *(host(t) for t in f))[0], torch.bfloat16, 6)
+    X, Q, P, Y = (b.padded(*s, torch.bfloat16) for s in ((18944, 256), (64, 256), (256, 64), (18944, 256)))
+    for fill in (1e30, -3.0, float("nan")):
+        X.fill_(fill), Q.fill_(1.0), P.fill_(1.0)
+        b.compact_fwd(X, Q, P, Y, 64, b.alloc_workspace(b.workspace_bytes(b.OP_COMPACT_FWD, 18944, 256, 256, 64, b.BF16)))
+        assert torch.equal(run_compact(b, x, *f), want)

@@ -482,8 +482,8 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
  *   _fwd       loss[T]; stats[T * 4] f32 (nullable) keeps what _bwd needs
  *   _bwd       dS[T, V] from the same arguments and stats; dloss[T] (nullable: 1) is the gradient arriving at loss
  *   _fwd_bwd   both in one pass over the logits, for a caller that knows the weight of every token beforehand
- * dS may be S (same ld), no other overlap.  Columns from V on are left untouched.  V <= 524,288, K <= 1024.  Sums are fp32 in a fixed
- * order: results are reproducible.  Needs no workspace. */
+ * dS may be S (same ld), no other overlap.  Columns from V on are left untouched.  V <= 524,288, K <= 1024.  Sums over the
+ * vocabulary are fp32, over the list's slots fp64, in a fixed order: results are reproducible.  Needs no workspace. */
 int flop_distill_topk_fwd(const void* S, int64_t lds, int64_t T, int64_t V, int dt, const float* t_logits, int64_t ldt,
                           const int32_t* t_idx, int64_t ldi, int64_t K, const float* t_lse, const float* weight,
                           float temperature, float* loss, float* stats, void* stream);

@@ -17,9 +17,9 @@
 //
 // Bound: HBM for rows of thousands of words (loss alone 4096 x 128000 bf16 183 us, 5.75 TB/s), but at one exponential and some three instructions
 // per element and pass the issue slots are close behind: loss and gradient of the same 562 us, 3.7 TB/s of one read and one write.
-// Rows of up to 4096 pieces of 16 bytes are read once and held in registers (part_kernel): eight lanes, a warp or a block to a row, or, where rows
-// are few, a cluster of up to eight blocks that exchange the maximum and sum of their parts through distributed shared memory.  Wider rows, and
-// those of one pass only, are walked (row_kernel).
+// Short rows are read once and held in registers (part_kernel): eight lanes, a warp or a block to a row, or, where rows are few, a cluster of up
+// to eight blocks that exchange the maximum and sum of their parts through distributed shared memory.  With many rows, what is held is up to 4096
+// pieces of 16 bytes for loss and gradient together, 512 for the loss alone and 256 for the backward call; wider rows are walked (row_kernel).
 #pragma once
 #include "common.cuh"
 
@@ -28,7 +28,6 @@ namespace distill {
 
 constexpr int kMaxSlots = 1024;
 constexpr int kMaxVocab = 1 << 19;        // two bits per word in shared memory: 128 KB
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr double kLn2d = 0.6931471805599453;
 
 enum { FWD = 1, BWD = 2, BOTH = 3 };
@@ -484,8 +483,9 @@ __device__ __forceinline__ float factor_of(const Args& a, int64_t row) {  // of 
 //     kBits, kBits + 1 in turn   L arrives when the row's bits are set              M waits before its first look at them
 //     kSums                      both wait: M's sums and L's numbers of the row are written
 //     kStored                    M arrives when the row's gradient is written       L waits before it writes the listed words and clears the bits
-// The list's warp is a function of its own: in the kernel's body its registers would be taken from the other warps' (64 each), which then spill
-// in their loops.
+// The list's warp is a function of its own: in the kernel's body its registers would be taken from the other warps' (64 each).  Even so loss and
+// gradient spill: 120 to 140 bytes stored and 170 to 210 loaded a thread in the kernel, 40 to 60 in this function; the loss alone spills
+// nothing, the backward call at most 16 bytes.
 template <typename T, int MODE, int G>
 __device__ __noinline__ void row_lists(const Args& a, unsigned char* smem, Sums (*sums)[G / 32 - 1], Info* info, int64_t row, int words4, int pieces, size_t side_bytes) {
   constexpr int NW = G / 32 - 1;

@@ -1240,7 +1240,7 @@ I8Ws plan_i8_ws(Arena& ar, int64_t T, int64_t d_in, int64_t k) {
 // launch and its boundary, and costs every block the work on all values.  Pair of products, apart / here: 1 x 1024 -> 358 -> 4096 12.4 / 7.1 us, 8 of
 // them 12.3 / 9.2, 8 x 2048 -> 512 -> 4096 14.6 / 10.1, 16 x 512 -> 200 -> 2048 10.5 / 9.2, but 16 x 1024 -> 358 -> 4096 13.0 / 13.8.
 bool few_quantizes(int64_t T, int64_t cols) { return T <= 16 && T * cols <= (T <= 8 ? 16384 : 8192); }
-// The same for the sums of the first product, which are scaled in fp64: 8 x 4096 -> 800 -> 4096 22.2 / 16.0 us, 1 x 16384 -> 1000 -> 4096 52.8 / 15.2,
+// The same for the sums of the first product, which are scaled in fp64: 8 x 4096 -> 800 -> 4096 22.2 / 16.2 us, 1 x 16384 -> 1000 -> 4096 52.8 / 15.4,
 // 16 x 512 -> 256 -> 2048 10.6 / 9.2, but 8 x 4096 -> 2000 -> 4096 16.0 / 21.2 and 16 x 200 -> 500 -> 2048 11.8 / 12.1.
 bool few_requantizes(int64_t T, int64_t k) { return T <= 16 && T * k <= (T <= 8 ? 8192 : 6144); }
 
@@ -1305,8 +1305,10 @@ int launch_gemm_i8(const int8_t* A, int64_t lda, const float* a_scale, const int
   return FLOP_OK;
 }
 
-// Few tokens (few_i8.cuh), against tiles of 128: 16 x 4096 x 1024 4.4 / 6.4 us, 16 x 8192 x 4096 11.7 / 16.7, 24 x 4096 x 2048 7.4 / 8.8, 32 x 4096 x 1024
-// 5.8 / 6.3; from 17 tokens on the warp-level instruction is what large products wait for: 32 x 8192 x 1024 7.1 / 6.3, 32 x 16384 x 2048 16.9 / 10.8.
+// Few tokens (few_i8.cuh), against tiles of 128: 16 x 4096 x 1024 4.4 / 6.4 us, 16 x 8192 x 4096 11.7 / 16.7, 24 x 4096 x 1024 5.0 / 6.3, 32 x 4096 x 1024
+// 5.8 / 6.3; from 17 tokens on the warp-level instruction is what large products wait for: 32 x 8192 x 1024 7.0 / 6.3, 17 x 16384 x 1024 7.3 / 6.9,
+// 32 x 16384 x 2048 16.8 / 10.7.  The line by the product of the three sizes is a rough one: long K with few outputs would still gain beyond it, and goes to
+// the tiles (24 x 4096 x 2048 7.3 / 8.8, 17 x 4096 x 4096 11.4 / 13.9, 24 x 2048 x 4096 10.2 / 12.2).
 bool few_i8_ok(int64_t T, int64_t N, int64_t K) {
   return T <= 32 && (T <= 16 || (double)T * (double)N * (double)K <= 1.6e8) && i8::few_smem((int)T, (int)K, 4) <= (size_t)kSmemBudget && N <= INT32_MAX / 2;
 }
@@ -1346,7 +1348,7 @@ int launch_product_i8(const int8_t* A, int64_t lda, const float* a_scale, const 
 
 // The first product of a compact pair with its rows quantised again in the same launch (see gemm_rowq_kernel), wherever its cluster holds k.  Apart / here:
 // 64 x 1024 -> 358 -> 4096 18.1 / 14.7 us, 4096 of them 35.0 / 26.4, 4096 x 1024 -> 900 -> 4096 49.1 / 36.9, 16384 x 2048 -> 1024 -> 2048 129 / 107.  A row
-// block is cut into more parts than its width asks for while SMs are left: 150 x 410 -> 160 -> 2100 14.6 / 12.8 us, 512 x 1024 -> 358 -> 4096 18.0 / 16.0.
+// block is cut into more parts than its width asks for while SMs are left: 150 x 410 -> 160 -> 2100 14.6 / 12.3 us, 512 x 1024 -> 358 -> 4096 18.0 / 16.0.
 bool rowq_ok(int64_t k) { return k <= (int64_t)i8::kRowqMaxCluster * i8::kRowqMaxSlice; }
 int launch_rowq(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* col_scale, int8_t* Hq, int64_t ldhq, float* h_scale,
                 int64_t M, int64_t N, int64_t K, cudaStream_t st) {
@@ -1452,7 +1454,8 @@ int launch_distill_inst(const distill::Args& a, cudaStream_t st) {
   // Rows in registers cost one read, but a block lasts from the first load to the last store, with nothing to hide that behind but the SM's other
   // blocks; the walking kernel reads twice for loss and gradient, always a batch ahead.  Held / walked, bf16, loss and gradient: 16384 x 4096
   // 91 / 166 us, 8192 x 16000 159 / 191, 8192 x 20000 (five of eight pieces in use) 256 / 195; f32: 8192 x 10000 218 / 200, 8192 x 16000 260 / 324.
-  // The loss alone is read once either way: 16384 x 4096 61 / 145 us, 8192 x 10000 f32 walked 77.
+  // The loss alone is read once either way: 16384 x 4096 61 / 145 us, 8192 x 10000 f32 walked 77.  512 pieces are the widest that it is built for held, and
+  // 256 the backward call; beyond them only the walked form has been measured.
   if (MODE != distill::BWD && pieces <= 512) return launch_distill_part<T, MODE, 64, 8>(a, 1, st);
   if (MODE == distill::BOTH && pieces <= 1024) return launch_distill_part<T, MODE, 128, 8>(a, 1, st);
   if (MODE == distill::BOTH && pieces <= 2048) return launch_distill_part<T, MODE, 256, 8>(a, 1, st);
@@ -2816,7 +2819,8 @@ int flop_compact_fwd_i8(const void* X, int64_t ldx, const int8_t* Qq, int64_t ld
     if (dt == FLOP_BF16) return launch_product_i8<bf16>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (bf16*)Y, ldy, T, d_out, k, st);
     return launch_product_i8<float>(w.Hq, w.ldhq, w.h_scale, Pq, ldpq, p_scale, (float*)Y, ldy, T, d_out, k, st);
   };
-  // few tokens: the sums of the first product go to the second one, whose blocks quantise them again
+  // Few tokens: the sums of the first product go to the second one, whose blocks quantise them again.  (Tokens quantised in a launch of their own before
+  // that: up to 8 of them, measured above; not measured for 9 to 16.)
   const bool here = few_quantizes(T, d_in);
   if ((here || T <= 8) && few_requantizes(T, k) && few_i8_ok(T, k, d_in) && few_i8_ok(T, d_out, k)) {
     if (here) {

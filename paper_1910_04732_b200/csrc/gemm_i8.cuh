@@ -9,9 +9,10 @@
 // the accumulator is there.  bf16 leaves through a swizzled 32 x 64 staging tile and a TMA store (which clips the edges), 32-bit results through
 // the same tile as coalesced stores.
 //
-// Bound: tensor cores, then power.  16384 x 6144 x 2048 bf16 144 us, 2.86 POP/s (86 % of twice the measured bf16 product); 8192 x 8192 x 8192
-// 425 us, 2.59 POP/s under the power cap.  Short K is bound by the epilogue (4096 x 4096 takes 17 us for K = 358 and for 1024), so both 64-column halves
-// are fetched at once and its loops are unrolled (a loop over them: 7 % slower).
+// Bound: tensor cores, then power.  16384 x 6144 x 2048 bf16 142 us, 2.91 POP/s (87 % of twice the measured bf16 product), until the power cap
+// takes hold: 160 us at 1490 MHz when calls follow one another for milliseconds.  8192 x 8192 x 8192 425-434 us, 2.5-2.6 POP/s under the cap.  Short K is
+// bound by the epilogue (4096 x 4096: 11.3 us for K = 128, 13.5 for 358, 17.0 for 1024), so both 64-column halves are fetched at once and its loops
+// are unrolled (a loop over them: 7 % slower; fp32 results of CTA pairs spill 40 bytes a thread that way).
 #pragma once
 #include "gemm_tc2.cuh"
 #include "quantized.cuh"

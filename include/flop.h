@@ -67,7 +67,9 @@ typedef enum {
   FLOP_OP_COMPACT = 3,     /* flop_compact_ranks                       */
   FLOP_OP_COMPACT_FWD = 4, /* flop_compact_fwd (r = k)                 */
   FLOP_OP_EMBEDDING_BWD = 5, /* flop_gated_embedding_bwd (r = d_i)      */
-  FLOP_OP_COMPACT_FWD_I8 = 6 /* flop_compact_fwd_i8 (r = k)             */
+  FLOP_OP_COMPACT_FWD_I8 = 6, /* flop_compact_fwd_i8 (r = k)             */
+  FLOP_OP_EMBEDDING_SORTED_BWD = 8, /* flop_embedding_bwd (d_in = d); 7 is no operation */
+  FLOP_OP_LAYER_NORM_BWD = 9 /* flop_layer_norm_bwd (d_in = d)          */
 } flop_op_t;
 
 const char* flop_status_string(int status);
@@ -495,6 +497,60 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
                               int64_t ldt, const int32_t* t_idx, int64_t ldi, int64_t K, const float* t_lse,
                               const float* weight, float temperature, float* loss, void* dS, int64_t ldds,
                               void* stream);
+
+/* Operators on token rows, in front of and between the factorised matrices of a model in training (no counterpart in the paper).
+ * dt is the type of every matrix of a call; bf16 matrices follow the header's rules on alignment, fp32 ones may start anywhere and have any
+ * leading dimension (rows that start on 16 bytes are faster).  Columns of an output from d on are left untouched.
+ * At most 2^31 - 1 rows, 2^30 columns (FLOP_ERR_UNSUPPORTED beyond).
+ *
+ * Embedding, dense (the counterpart of flop_gated_embedding_* for a table that is not factorised): ids[T] (int32, DEVICE) are rows of
+ * E[n_rows, d]; ids outside [0, n_rows) are padding.
+ *   _fwd   Y[t] = scale E[ids[t]]; zeros for padding.  Y may not overlap E or ids.
+ *   _bwd   dE[v] (= | += with accumulate) scale * sum over {t: ids[t] = v} of dY[t], in type wgrad_dt.  Without accumulate every row of
+ *          dE[n_rows, d] is written (zeros for words that do not occur), with it only the rows of words that do.
+ *          Sums are fp32, in an order that depends on T, d and the device alone: results are reproducible.
+ *          dE may not overlap dY or ids.  ws: flop_workspace_bytes(FLOP_OP_EMBEDDING_SORTED_BWD, T, d, 0, n_rows, dt). */
+int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde, int64_t n_rows, float scale, void* Y,
+                       int64_t ldy, int64_t d, int dt, void* stream);
+int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t T, int64_t n_rows, float scale, void* dE,
+                       int64_t ldde, int accumulate, int64_t d, int dt, int wgrad_dt, void* ws, size_t ws_bytes, void* stream);
+
+/* Dropout with the mask drawn from the gates' generator and never stored: forward and backward pass draw the same mask from the same
+ * (seed, offset + *offset_dev).  offset_dev (DEVICE, nullable) lets a captured launch draw anew: it has to hold the same value in both passes.
+ *     h[t, 8g + j] = the j-th 16 bits (low half first) of Philox4x32-10, key = seed, counter words
+ *                    (offset + *offset_dev + t ceil(d / 8) + g as 64 bits, 1, 0)
+ *     threshold = min(floor(65536 p + 1/2), 65535),  keep = h >= threshold,  s = 65536 / (65536 - threshold)
+ *   _fwd   Y = R + keep * X * s (R nullable: 0)        _bwd   dX = keep * dY * s  (the gradient of R is dY itself)
+ * p in [0, 1) is used in units of 2^-16; s is that of the probability used, so the expectation of Y is R + X.  A call uses up
+ * T ceil(d / 8) counters.  flop_gate_sample draws from other counters (third word 0), so that both may share a seed.  What is
+ * dropped counts as 0, whatever it holds (infinities and NaN too).  Y may be X or R (same ld), dX may be dY; no other overlap. */
+int flop_dropout_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset,
+                     const uint64_t* offset_dev, void* Y, int64_t ldy, int64_t T, int64_t d, int dt, void* stream);
+int flop_dropout_bwd(const void* dY, int64_t lddy, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev,
+                     void* dX, int64_t lddx, int64_t T, int64_t d, int dt, void* stream);
+
+/* Layer norm over the columns of a row, with the residual sum and the dropout in front of it in the same pass:
+ *   _fwd   S = R + dropout(X), rounded to dt   (R nullable: 0; p = 0: no dropout; the mask is flop_dropout_fwd's)
+ *          Y = (S - mean) rstd weight + bias,  rstd = 1 / sqrt(mean((S - mean)^2) + eps)
+ *          S is written where the pointer is given, and what is normalised is the rounded sum either way.  stats[T * 2] f32 (nullable, 8-byte
+ *          aligned) keeps (mean, rstd) for _bwd.  weight, bias: f32[d], nullable (1, 0).  eps >= 0; a row of equal values with
+ *          eps = 0 has no result (NaN).
+ *   _bwd   takes S (X itself where the forward call had neither R nor dropout), stats and weight of the forward call, and dS (nullable),
+ *          the gradient that arrives at S from elsewhere (the residual stream of the blocks behind):
+ *              x = (S - mean) rstd,  a = dY weight,  g = rstd (a - mean(a) - x mean(a x)) + dS
+ *              dR = g,  dX = keep * g * s (p, seed, offset as in the forward call; p = 0: g),
+ *              dweight (= | += with accumulate) sum_t dY x,  dbias likewise sum_t dY      (f32[d])
+ *          Any output may be NULL.  Sums over rows are fp32, in an order that depends on T, d and the device alone.
+ *          ws: flop_workspace_bytes(FLOP_OP_LAYER_NORM_BWD, T, d, 0, 0, dt); not needed where dweight and dbias are NULL.
+ * Outputs may take the place of inputs (same ld): S and Y that of X or R, dX and dR that of dY, S or dS.  S and Y, and dX and dR, are
+ * apart; there is no other overlap. */
+int flop_layer_norm_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset,
+                        const uint64_t* offset_dev, const float* weight, const float* bias, float eps, void* S,
+                        int64_t lds, void* Y, int64_t ldy, float* stats, int64_t T, int64_t d, int dt, void* stream);
+int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds, const float* stats, const float* weight,
+                        const void* dS, int64_t ldds, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev,
+                        void* dX, int64_t lddx, void* dR, int64_t lddr, float* dweight, float* dbias, int accumulate,
+                        int64_t T, int64_t d, int dt, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

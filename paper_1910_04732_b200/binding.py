@@ -25,6 +25,7 @@ LIB_PATH = os.path.join(_HERE, "libflop_b200.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 F32, BF16 = 0, 1
 OP_FWD, OP_BWD, OP_L0, OP_COMPACT, OP_COMPACT_FWD, OP_EMBEDDING_BWD, OP_COMPACT_FWD_I8 = range(7)
+OP_EMBEDDING_SORTED_BWD, OP_LAYER_NORM_BWD = 8, 9
 
 EXPORTS = ("flop_status_string", "flop_last_async_status", "flop_device_status", "flop_sync_bytes",
            "flop_gated_lowrank_fwd_chained", "flop_gated_lowrank_bwd_chained", "flop_selftest_wait_timeout", "flop_launch_count", "flop_plan_tile_schedule", "flop_plan_chain_queue", "flop_scale_rows_grouped", "flop_dlog_alpha_finish_grouped", "flop_gemm_timing_begin",
@@ -35,7 +36,8 @@ EXPORTS = ("flop_status_string", "flop_last_async_status", "flop_device_status",
            "flop_expected_l0_lagrangian_noalloc", "flop_agp_gates", "flop_gated_embedding_fwd",
            "flop_gated_embedding_bwd",
            "flop_compact_ranks", "flop_compact_fwd", "flop_chain_fwd", "flop_quantize_rows", "flop_gemm_i8", "flop_compact_fwd_i8",
-           "flop_distill_topk_fwd", "flop_distill_topk_bwd", "flop_distill_topk_fwd_bwd")
+           "flop_distill_topk_fwd", "flop_distill_topk_bwd", "flop_distill_topk_fwd_bwd",
+           "flop_embedding_fwd", "flop_embedding_bwd", "flop_dropout_fwd", "flop_dropout_bwd", "flop_layer_norm_fwd", "flop_layer_norm_bwd")
 
 
 class HcParams(ctypes.Structure):
@@ -157,6 +159,14 @@ def load_library() -> ctypes.CDLL:
     lib.flop_distill_topk_fwd.argtypes = student + [vp, vp, vp]
     lib.flop_distill_topk_bwd.argtypes = student + [vp, vp, vp, i64, vp]
     lib.flop_distill_topk_fwd_bwd.argtypes = student + [vp, vp, i64, vp]
+    cf, u64 = ctypes.c_float, ctypes.c_uint64
+    mask = [cf, u64, u64, vp]          # p, seed, offset, offset_dev
+    lib.flop_embedding_fwd.argtypes = [vp, i64, vp, i64, i64, cf, vp, i64, i64, ci, vp]
+    lib.flop_embedding_bwd.argtypes = [vp, i64, vp, i64, i64, cf, vp, i64, ci, i64, ci, ci, vp, sz, vp]
+    lib.flop_dropout_fwd.argtypes = [vp, i64, vp, i64] + mask + [vp, i64, i64, i64, ci, vp]
+    lib.flop_dropout_bwd.argtypes = [vp, i64] + mask + [vp, i64, i64, i64, ci, vp]
+    lib.flop_layer_norm_fwd.argtypes = [vp, i64, vp, i64] + mask + [vp, vp, cf, vp, i64, vp, i64, vp, i64, i64, ci, vp]
+    lib.flop_layer_norm_bwd.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64] + mask + [vp, i64, vp, i64, vp, vp, ci, i64, i64, ci, vp, sz, vp]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ci
     lib.flop_launch_count.restype = ctypes.c_ulonglong
@@ -515,3 +525,40 @@ def distill_topk_bwd(S, t_logits, t_idx, t_lse, weight, temperature: float, stat
 def distill_topk_fwd_bwd(S, t_logits, t_idx, t_lse, weight, temperature: float, loss, dS) -> None:
     """flop_distill_topk_fwd_bwd: loss and gradient in one pass over the logits (dS may be S)."""
     _check(_native()._operators.distill_topk_fwd_bwd(S, t_logits, t_idx, t_lse, weight, temperature, loss, dS), "flop_distill_topk_fwd_bwd")
+
+
+def embedding_fwd(ids, E, scale: float, Y) -> None:
+    """flop_embedding_fwd: Y[t] = scale * E[ids[t]] (int32 ids; those outside the table are padding: zeros)."""
+    _check(_native()._rows.embedding_fwd(ids, E, scale, Y), "flop_embedding_fwd")
+
+
+def embedding_bwd(dY, ids, scale: float, dE, ws, accumulate: bool = False) -> None:
+    """flop_embedding_bwd: dE[v] (=|+=) scale * the sum of dY over v's tokens (workspace: OP_EMBEDDING_SORTED_BWD with T, d, 0, rows of dE)."""
+    _check(_native()._rows.embedding_bwd(dY, ids, scale, dE, ws, accumulate), "flop_embedding_bwd")
+
+
+def dropout_counters(rows: int, cols: int) -> int:
+    """Counters of the generator that a dropout of [rows, cols] uses up: what a program adds to `offset` before its next one."""
+    return rows * ((cols + 7) // 8)
+
+
+def dropout_fwd(X, Y, p: float, seed: int, offset: int, R=None, offset_dev=None) -> None:
+    """flop_dropout_fwd: Y = R + dropout(X).  The mask is that of (seed, offset + offset_dev[0]); offset_dev: one 64-bit integer on the device."""
+    _check(_native()._rows.dropout_fwd(X, R, p, seed, offset, offset_dev, Y), "flop_dropout_fwd")
+
+
+def dropout_bwd(dY, dX, p: float, seed: int, offset: int, offset_dev=None) -> None:
+    """flop_dropout_bwd: dX from dY through the mask of the forward call with the same p, seed, offset and offset_dev[0]."""
+    _check(_native()._rows.dropout_bwd(dY, p, seed, offset, offset_dev, dX), "flop_dropout_bwd")
+
+
+def layer_norm_fwd(X, weight, bias, eps: float, Y, stats=None, R=None, S=None, p: float = 0.0, seed: int = 0, offset: int = 0, offset_dev=None) -> None:
+    """flop_layer_norm_fwd: S = R + dropout(X), Y = layer norm of S; weight and bias f32 (None: 1, 0), stats[T, 2] f32 for the backward call."""
+    _check(_native()._rows.layer_norm_fwd(X, R, p, seed, offset, offset_dev, weight, bias, eps, S, Y, stats), "flop_layer_norm_fwd")
+
+
+def layer_norm_bwd(dY, S, stats, weight, dX, dweight, dbias, ws, dS=None, dR=None, p: float = 0.0, seed: int = 0, offset: int = 0, offset_dev=None,
+                   accumulate: bool = False) -> None:
+    """flop_layer_norm_bwd: dX, dR (rows), dweight, dbias (f32), each may be None; dS: the gradient that arrives at S from elsewhere
+    (workspace: OP_LAYER_NORM_BWD with T, d)."""
+    _check(_native()._rows.layer_norm_bwd(dY, S, stats, weight, dS, p, seed, offset, offset_dev, dX, dR, dweight, dbias, ws, accumulate), "flop_layer_norm_bwd")

@@ -1,15 +1,18 @@
-"""Builds the CUDA library in-tree, csrc/flop_lib.cu -> libflop_b200.so (sm_100a only), and the native half of the Python
+"""Builds the CUDA library in-tree, csrc/flop_lib.cu and csrc/flop_rows.cu -> libflop_b200.so (sm_100a only), and the native half of the Python
 binding, csrc/binding_native.cpp -> _binding_native.<python and torch it is for>.so."""
 from __future__ import annotations
 
 import os
+import re
 import shutil
 import subprocess
 import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "flop_lib.cu")
+UNITS = [os.path.join(HERE, "csrc", f) for f in ("flop_lib.cu", "flop_rows.cu")]
+ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
+OBJECTS = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libflop_b200.so")
 NATIVE_SRC = os.path.join(HERE, "csrc", "binding_native.cpp")
 
@@ -24,7 +27,19 @@ def _nvcc() -> str:
 def sources():
     d = os.path.join(HERE, "csrc")
     inc = os.path.join(os.path.dirname(HERE), "include", "flop.h")
-    return [os.path.join(d, f) for f in sorted(os.listdir(d)) if f.endswith((".cu", ".cuh"))] + [inc]
+    return [os.path.join(d, f) for f in sorted(os.listdir(d)) if f.endswith((".cu", ".cuh", ".h"))] + [inc]
+
+
+def _includes(path, seen=None):
+    """`path` and the files of this repository that it includes, directly or not."""
+    seen = set() if seen is None else seen
+    path = os.path.normpath(path)
+    if path not in seen and os.path.exists(path):
+        seen.add(path)
+        with open(path) as f:
+            for name in re.findall(r'^#include "([^"]+)"', f.read(), re.M):
+                _includes(os.path.join(os.path.dirname(path), name), seen)
+    return seen
 
 
 def up_to_date() -> bool:
@@ -71,16 +86,29 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and up_to_date():
         build_native()
         return LIB
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-o", LIB, SRC]
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    os.makedirs(OBJECTS, exist_ok=True)
+    jobs, objects = [], []
+    for unit in UNITS:                     # the units compile side by side; one whose sources are older than its object is kept
+        obj = os.path.join(OBJECTS, os.path.basename(unit) + ".o")
+        objects.append(obj)
+        if not force and not verbose and os.path.exists(obj) and all(os.path.getmtime(p) <= os.path.getmtime(obj) for p in _includes(unit)):
+            continue
+        cmd = [_nvcc(), *(["-Xptxas", "-v"] if verbose else []), *ARCH, "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-c", "-o", obj, unit]
+        jobs.append((obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    failed = ""
+    for obj, job in jobs:
+        out, _ = job.communicate()
+        if job.returncode != 0:
+            failed += out
+            if os.path.exists(obj):
+                os.remove(obj)
+        elif verbose:
+            print(out)
+    if failed:
+        raise RuntimeError("nvcc failed:\n" + failed)
+    r = subprocess.run([_nvcc(), *ARCH, "-shared", "-o", LIB, *objects], capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + r.stdout + r.stderr)
-    if verbose:
-        print(r.stderr)
+        raise RuntimeError("linking failed:\n" + r.stdout + r.stderr)
     build_native(force)
     return LIB
 

@@ -8,6 +8,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -322,6 +323,117 @@ FLOP_METHOD(distill_topk_fwd_bwd, 8) {   // S, t_logits, t_idx, t_lse, weight, t
   });
 }
 
+// ---- embedding lookup, dropout and layer norm (module _rows)
+// The library works on the current device and sees addresses only: a tensor of the host or of another device is refused here, and the call runs
+// on the device of its tensors, on that device's current stream.
+struct Place {
+  c10::DeviceIndex device = -1;
+  c10::cuda::OptionalCUDAGuard guard;
+  Place(std::initializer_list<PyObject*> tensors) {
+    for (PyObject* o : tensors) {
+      const at::Tensor* t = tensor(o);
+      if (!t) continue;
+      if (!t->is_cuda()) {
+        PyErr_Format(PyExc_TypeError, "expected tensors on a CUDA device, got one on %s", t->device().str().c_str());
+        throw Stop{};
+      }
+      if (device < 0) device = t->device().index();
+      same(t->device().index(), device, "devices of the tensors");
+    }
+    if (device >= 0) guard.set_index(device);
+  }
+  void* stream() const { return (void*)c10::cuda::getCurrentCUDAStream(device).stream(); }
+};
+Mat like(PyObject* o, const Mat& m, int dt, const char* what) {   // a matrix of m's size and type; None: none
+  const Mat r = optional_matrix(o);
+  if (o == Py_None) return r;
+  same(storage(required(o)), dt, what); same(r.rows, m.rows, what); same(r.cols, m.cols, what);
+  return r;
+}
+struct Mask { float p; uint64_t seed, offset; const uint64_t* dev; };
+Mask mask(PyObject* const* a) {   // p, seed, offset, offset_dev
+  Mask m{number(a[0]), (uint64_t)integer(a[1]), (uint64_t)integer(a[2]), nullptr};
+  need(a[3], at::kLong, 1, "offset_dev");
+  m.dev = ptr<const uint64_t>(a[3]);
+  return m;
+}
+
+FLOP_METHOD(embedding_fwd, 4) {   // ids, E, scale, Y
+  const Mat E = matrix(a[1]), Y = matrix(a[3]);
+  const int dt = storage(required(a[1]));
+  const float scale = number(a[2]);
+  same(storage(required(a[3])), dt, "types of Y and E"); same(Y.cols, E.cols, "columns of Y and E");
+  required(a[0]); need(a[0], at::kInt, Y.rows, "ids"); same((int64_t)numel(a[0]), Y.rows, "ids and rows of Y");
+  const int32_t* ids = ptr<int32_t>(a[0]);
+  const Place at{a[0], a[1], a[3]};
+  return call([&] { return flop_embedding_fwd(ids, Y.rows, E.p, E.ld, E.rows, scale, Y.p, Y.ld, Y.cols, dt, at.stream()); });
+}
+
+FLOP_METHOD(embedding_bwd, 6) {   // dY, ids, scale, dE, ws, accumulate
+  const Mat dY = matrix(a[0]), dE = matrix(a[3]);
+  const int dt = storage(required(a[0])), wdt = storage(required(a[3]));
+  const float scale = number(a[2]);
+  same(dE.cols, dY.cols, "columns of dE and dY");
+  required(a[1]); need(a[1], at::kInt, dY.rows, "ids"); same((int64_t)numel(a[1]), dY.rows, "ids and rows of dY");
+  const int32_t* ids = ptr<int32_t>(a[1]);
+  need(a[4], at::kByte, 0, "ws");
+  void* ws = ptr(a[4]); const size_t wb = numel(a[4]);
+  const int accumulate = flag(a[5]);
+  const Place at{a[0], a[1], a[3], a[4]};
+  return call([&] { return flop_embedding_bwd(dY.p, dY.ld, ids, dY.rows, dE.rows, scale, dE.p, dE.ld, accumulate, dY.cols, dt, wdt, ws, wb, at.stream()); });
+}
+
+FLOP_METHOD(dropout_fwd, 7) {   // X, R, p, seed, offset, offset_dev, Y
+  const Mat X = matrix(a[0]);
+  const int dt = storage(required(a[0]));
+  const Mat R = like(a[1], X, dt, "R and X"), Y = like((required(a[6]), a[6]), X, dt, "Y and X");
+  const Mask m = mask(a + 2);
+  const Place at{a[0], a[1], a[5], a[6]};
+  return call([&] { return flop_dropout_fwd(X.p, X.ld, R.p, R.ld, m.p, m.seed, m.offset, m.dev, Y.p, Y.ld, X.rows, X.cols, dt, at.stream()); });
+}
+
+FLOP_METHOD(dropout_bwd, 6) {   // dY, p, seed, offset, offset_dev, dX
+  const Mat dY = matrix(a[0]);
+  const int dt = storage(required(a[0]));
+  const Mat dX = like((required(a[5]), a[5]), dY, dt, "dX and dY");
+  const Mask m = mask(a + 1);
+  const Place at{a[0], a[4], a[5]};
+  return call([&] { return flop_dropout_bwd(dY.p, dY.ld, m.p, m.seed, m.offset, m.dev, dX.p, dX.ld, dY.rows, dY.cols, dt, at.stream()); });
+}
+
+FLOP_METHOD(layer_norm_fwd, 12) {   // X, R, p, seed, offset, offset_dev, weight, bias, eps, S, Y, stats
+  const Mat X = matrix(a[0]);
+  const int dt = storage(required(a[0]));
+  const Mat R = like(a[1], X, dt, "R and X"), S = like(a[9], X, dt, "S and X"), Y = like((required(a[10]), a[10]), X, dt, "Y and X");
+  const Mask m = mask(a + 2);
+  need(a[6], at::kFloat, X.cols, "weight"); need(a[7], at::kFloat, X.cols, "bias"); need(a[11], at::kFloat, 2 * X.rows, "stats");
+  const float *w = ptr<float>(a[6]), *b = ptr<float>(a[7]), eps = number(a[8]);
+  float* stats = ptr<float>(a[11]);
+  const Place at{a[0], a[1], a[5], a[6], a[7], a[9], a[10], a[11]};
+  return call([&] {
+    return flop_layer_norm_fwd(X.p, X.ld, R.p, R.ld, m.p, m.seed, m.offset, m.dev, w, b, eps, S.p, S.ld, Y.p, Y.ld, stats, X.rows, X.cols, dt, at.stream());
+  });
+}
+
+FLOP_METHOD(layer_norm_bwd, 15) {   // dY, S, stats, weight, dS, p, seed, offset, offset_dev, dX, dR, dweight, dbias, ws, accumulate
+  const Mat dY = matrix(a[0]);
+  const int dt = storage(required(a[0]));
+  const Mat S = like((required(a[1]), a[1]), dY, dt, "S and dY"), dS = like(a[4], dY, dt, "dS and dY"), dX = like(a[9], dY, dt, "dX and dY"),
+            dR = like(a[10], dY, dt, "dR and dY");
+  const Mask m = mask(a + 5);
+  need(a[2], at::kFloat, 2 * dY.rows, "stats"); need(a[3], at::kFloat, dY.cols, "weight");
+  need(a[11], at::kFloat, dY.cols, "dweight"); need(a[12], at::kFloat, dY.cols, "dbias"); need(a[13], at::kByte, 0, "ws");
+  const float *stats = ptr<float>(a[2]), *w = ptr<float>(a[3]);
+  float *dw = ptr<float>(a[11]), *db = ptr<float>(a[12]);
+  void* ws = ptr(a[13]); const size_t wb = numel(a[13]);
+  const int accumulate = flag(a[14]);
+  const Place at{a[0], a[1], a[2], a[3], a[4], a[8], a[9], a[10], a[11], a[12], a[13]};
+  return call([&] {
+    return flop_layer_norm_bwd(dY.p, dY.ld, S.p, S.ld, stats, w, dS.p, dS.ld, m.p, m.seed, m.offset, m.dev, dX.p, dX.ld, dR.p, dR.ld, dw, db, accumulate, dY.rows,
+                               dY.cols, dt, ws, wb, at.stream());
+  });
+}
+
 #define FLOP_ENTRY(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FLOP_ENTRY(gate_sample), FLOP_ENTRY(gated_lowrank_fwd), FLOP_ENTRY(gated_lowrank_bwd), FLOP_ENTRY(expected_l0_lagrangian),
                          FLOP_ENTRY(gated_embedding_fwd), FLOP_ENTRY(gated_embedding_bwd), FLOP_ENTRY(compact_ranks), FLOP_ENTRY(compact_fwd),
@@ -329,18 +441,23 @@ PyMethodDef methods[] = {FLOP_ENTRY(gate_sample), FLOP_ENTRY(gated_lowrank_fwd),
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 PyMethodDef operator_methods[] = {FLOP_ENTRY(quantize_rows), FLOP_ENTRY(gemm_i8), FLOP_ENTRY(compact_fwd_i8), FLOP_ENTRY(distill_topk_fwd),
                                   FLOP_ENTRY(distill_topk_bwd), FLOP_ENTRY(distill_topk_fwd_bwd), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef row_methods[] = {FLOP_ENTRY(embedding_fwd), FLOP_ENTRY(embedding_bwd), FLOP_ENTRY(dropout_fwd), FLOP_ENTRY(dropout_bwd),
+                             FLOP_ENTRY(layer_norm_fwd), FLOP_ENTRY(layer_norm_bwd), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef rows = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, row_methods, nullptr, nullptr, nullptr, nullptr};
 PyModuleDef operators = {PyModuleDef_HEAD_INIT, "_operators", nullptr, -1, operator_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-// The calls beside the layer's own path are a module of their own inside this one.
+// The calls beside the layer's own path are modules of their own inside this one.
 PyMODINIT_FUNC PyInit__binding_native(void) {
   PyObject* m = PyModule_Create(&module);
-  PyObject* o = m ? PyModule_Create(&operators) : nullptr;
-  if (!o || PyModule_AddObject(m, "_operators", o) < 0) {
-    Py_XDECREF(o);
-    Py_XDECREF(m);
-    return nullptr;
+  for (PyModuleDef* def : {&operators, &rows}) {
+    PyObject* o = m ? PyModule_Create(def) : nullptr;
+    if (!o || PyModule_AddObject(m, def->m_name, o) < 0) {
+      Py_XDECREF(o);
+      Py_XDECREF(m);
+      return nullptr;
+    }
   }
   return m;
 }

@@ -9,8 +9,9 @@
 namespace flop {
 
 // Device status word: 0 = ok, otherwise a flop_status_t written by a kernel
-// whose bounded wait gave up.  Read and cleared by flop_device_status().
-__device__ int g_device_status = 0;
+// whose bounded wait gave up.  Read and cleared by flop_device_status().  It belongs to flop_lib.cu, whose kernels are all
+// that wait; another translation unit's copy is never written.
+static __device__ int g_device_status = 0;
 
 // Programmatic dependent launch: every kernel of the library is launched so that its prologue may
 // overlap the tail of the kernel before it on the stream.  pdl_wait() blocks until all earlier

@@ -1,0 +1,321 @@
+// C ABI of the operators on token rows in front of and between the factorised matrices (see include/flop.h): embedding lookup and
+// its gradient, dropout, layer norm.  Argument checks, workspace planning and launches; the kernels are in embedding_rows.cuh, dropout.cuh
+// and layer_norm.cuh.
+#include <math.h>
+#include <string.h>
+
+#include "host.cuh"
+#include "embedding_rows.cuh"
+#include "layer_norm.cuh"
+#include "rows_ws.h"
+
+using namespace flop;
+typedef __nv_bfloat16 bf16;
+
+namespace {
+
+constexpr int64_t kMaxCols = 1 << 30;
+
+// A matrix that an operator reads or writes: where it lies, and whether the kernels can take it.
+struct RowsArg {
+  const void* p; int64_t ld; int dt;
+  bool given() const { return p != nullptr; }
+  bool fits(int64_t d) const { return ld >= d; }
+  bool placed() const { return dt != FLOP_BF16 || bf16_ok(p, ld); }                         // the library's rule for bf16
+  bool vec() const { return aligned16(p) && (ld * (int64_t)elt(dt)) % 16 == 0; }            // rows start on 16 bytes
+  Span span(int64_t T, int64_t d) const { return Span(p, T, d, ld, elt(dt)); }
+};
+// Every row is read before it is written, element by element by the same thread, so an output may be an input; half of it may not.
+bool in_place_or_apart(const RowsArg& out, const RowsArg& in, int64_t T, int64_t d) {
+  return !out.given() || !in.given() || (out.p == in.p && out.ld == in.ld && out.dt == in.dt) || !out.span(T, d).meets(in.span(T, d));
+}
+bool apart(const RowsArg& a, const RowsArg& b, int64_t T, int64_t d) { return !a.given() || !b.given() || !a.span(T, d).meets(b.span(T, d)); }
+
+int64_t groups_of(int64_t d) { return (d + 7) / 8; }
+
+bool valid_p(float p) { return p >= 0.f && p < 1.f; }
+Drop make_drop(float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev) {
+  Drop d{};
+  d.key = make_uint2((uint32_t)seed, (uint32_t)(seed >> 32));
+  d.offset = offset; d.offset_dev = offset_dev;
+  d.threshold = std::min<uint32_t>((uint32_t)floor((double)p * 65536.0 + 0.5), 65535u);
+  d.scale = (float)(65536.0 / (65536.0 - (double)d.threshold));
+  return d;
+}
+
+int launched() {
+  count_launch();
+  FLOP_CUDA(cudaGetLastError());
+  return FLOP_OK;
+}
+
+// Blocks of a kernel that strides over the groups of all rows, and the stride in rows and groups.
+template <typename Args>
+dim3 group_grid(Args& a, int64_t T, int64_t d, int blocks_per_sm) {
+  a.groups = (int)groups_of(d);
+  a.total = T * a.groups;
+  const int64_t blocks = std::min<int64_t>((a.total + 255) / 256, (int64_t)num_sms() * blocks_per_sm);
+  a.step_rows = blocks * 256 / a.groups;
+  a.step_groups = (int)(blocks * 256 - a.step_rows * a.groups);
+  return dim3((unsigned)blocks);
+}
+
+// ---------------------------------------------------------------- embedding
+struct RunPlan { int lanes, slices, chunk; int64_t chunks; };
+// A chunk of 8 tokens where that gives the machine less than a round of warps, longer ones (fewer parts to join) where there are many.
+RunPlan plan_runs(int64_t T, int64_t d) {
+  RunPlan p;
+  p.lanes = d <= 64 ? 8 : d <= 128 ? 16 : 32;
+  p.slices = (int)((d + p.lanes * 8 - 1) / (p.lanes * 8));
+  p.chunk = 8;
+  while (p.chunk < 256 && T / p.chunk * p.slices * p.lanes / 32 > (int64_t)num_sms() * 32) p.chunk *= 2;
+  p.chunks = (T + p.chunk - 1) / p.chunk;
+  return p;
+}
+struct EmbWs { uint2* order[2]; float* part; int64_t part_ld; size_t bytes; };
+EmbWs plan_emb_ws(Arena& ar, int64_t T, int64_t d) {
+  EmbWs w{};
+  if (T == 0 || d == 0) return w;
+  for (auto& o : w.order) o = (uint2*)ar.take((size_t)T * sizeof(uint2));
+  w.part_ld = round_up(d, 8);
+  w.part = (float*)ar.take((size_t)plan_runs(T, d).chunks * 2 * w.part_ld * 4);
+  w.bytes = ar.used;
+  return w;
+}
+
+int launch_sort(const emb::SortArgs& a, size_t smem, int zero_blocks, cudaStream_t st) {
+  static OncePerDevice configured;
+  FLOP_TRY(allow_smem(configured, emb::sort_smem(emb::kMaxDigitBits), emb::sort_kernel));
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.cluster + zero_blocks / a.cluster * a.cluster));
+  cfg.blockDim = dim3(emb::kSortThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)a.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_on() ? 2 : 1;
+  FLOP_CUDA(cudaLaunchKernelEx(&cfg, emb::sort_kernel, a));
+  count_launch();
+  return FLOP_OK;
+}
+
+template <typename T, typename TW>
+int launch_runs(const emb::RunArgs& a, int lanes, cudaStream_t st) {
+  constexpr int U = sizeof(T) == 2 ? 8 : 4;
+  const dim3 grid((unsigned)((a.chunks * a.slices + 256 / lanes - 1) / (256 / lanes)));
+  if (lanes == 8)       launch_k(emb::runs_kernel<T, TW, 8, U>, grid, dim3(256), (size_t)0, st, a);
+  else if (lanes == 16) launch_k(emb::runs_kernel<T, TW, 16, U>, grid, dim3(256), (size_t)0, st, a);
+  else                  launch_k(emb::runs_kernel<T, TW, 32, U>, grid, dim3(256), (size_t)0, st, a);
+  FLOP_TRY(launched());
+  if (a.chunks > 1) {
+    launch_k(emb::joints_kernel<TW>, dim3((unsigned)(a.chunks - 1), (unsigned)((a.d + 255) / 256)), dim3(256), (size_t)0, st, a);
+    FLOP_TRY(launched());
+  }
+  return FLOP_OK;
+}
+
+// ---------------------------------------------------------------- layer norm
+// Parts of the column sums: enough blocks for the machine, 64 rows each at least.
+int64_t norm_parts(int64_t T, int64_t d) {
+  const int64_t slabs = std::max<int64_t>((groups_of(d) + 31) / 32, 1);
+  return std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, std::max<int64_t>(1, (int64_t)num_sms() * 4 / slabs)));
+}
+struct NormWs { float* part; int64_t part_ld, n_part; size_t bytes; };
+NormWs plan_norm_ws(Arena& ar, int64_t T, int64_t d) {
+  NormWs w{};
+  if (T == 0 || d == 0) return w;
+  w.part_ld = round_up(d, 8);
+  w.n_part = norm_parts(T, d);
+  w.part = (float*)ar.take((size_t)w.n_part * 2 * w.part_ld * 4);
+  w.bytes = ar.used;
+  return w;
+}
+
+int walk_threads(int groups) { return std::min(512, (groups + 31) / 32 * 32); }
+
+template <typename T>
+int launch_norm_fwd(const norm::FwdArgs& a, bool sum, cudaStream_t st) {
+  const dim3 grid((unsigned)a.T), block(walk_threads(a.groups));
+  if (sum) launch_k(norm::fwd_walk_kernel<T, true>, grid, block, (size_t)0, st, a);
+  else     launch_k(norm::fwd_walk_kernel<T, false>, grid, block, (size_t)0, st, a);
+  return launched();
+}
+
+template <typename T>
+int launch_norm_bwd(const norm::BwdArgs& a, float* dweight, float* dbias, int accumulate, cudaStream_t st) {
+  if (a.n_part) {     // before the rows, whose outputs may take the place of what the sums read
+    launch_k(norm::bwd_columns_kernel<T>, dim3((unsigned)((a.groups + 31) / 32), (unsigned)a.n_part), dim3(256), (size_t)0, st, a);
+    FLOP_TRY(launched());
+    launch_k(norm::bwd_finish_kernel, dim3((unsigned)((a.d + 31) / 32), 2), dim3(256), (size_t)0, st, (const float*)a.part, a.part_ld, a.n_part, a.d, dweight,
+             dbias, accumulate);
+    FLOP_TRY(launched());
+  }
+  if (a.dX || a.dR) {
+    launch_k(norm::bwd_walk_kernel<T>, dim3((unsigned)a.T), dim3(walk_threads(a.groups)), (size_t)0, st, a);
+    FLOP_TRY(launched());
+  }
+  return FLOP_OK;
+}
+
+}  // namespace
+
+namespace flop {
+size_t embedding_rows_ws_bytes(int64_t T, int64_t d) {
+  Arena ar{nullptr, 0, 0};
+  return plan_emb_ws(ar, T, d).bytes;
+}
+size_t layer_norm_ws_bytes(int64_t T, int64_t d) {
+  Arena ar{nullptr, 0, 0};
+  return plan_norm_ws(ar, T, d).bytes;
+}
+}  // namespace flop
+
+extern "C" {
+
+int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde, int64_t n_rows, float scale, void* Y, int64_t ldy, int64_t d, int dt,
+                       void* stream) {
+  if (T < 0 || n_rows < 0 || d < 0 || !valid_dt(dt)) return FLOP_ERR_INVALID_ARG;
+  if (T == 0 || d == 0) return FLOP_OK;
+  const RowsArg e{E, lde, dt}, y{Y, ldy, dt};
+  if (!ids || !y.given() || !y.fits(d) || (n_rows > 0 && (!e.given() || !e.fits(d)))) return FLOP_ERR_INVALID_ARG;
+  if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || !y.placed() || (n_rows > 0 && !e.placed())) return FLOP_ERR_UNSUPPORTED;
+  if (e.span(n_rows, d).meets(y.span(T, d)) || Span(ids, 1, T, T, 4).meets(y.span(T, d))) return FLOP_ERR_INVALID_ARG;
+  emb::LookupArgs a{};
+  a.ids = ids; a.T = T; a.E = E; a.lde = lde; a.V = n_rows; a.Y = Y; a.ldy = ldy; a.scale = scale; a.d = (int)d;
+  a.vec = y.vec() && (n_rows == 0 || e.vec());
+  const dim3 grid = group_grid(a, T, d, 8);
+  if (dt == FLOP_BF16) launch_k(emb::lookup_kernel<bf16>, grid, dim3(256), (size_t)0, (cudaStream_t)stream, a);
+  else                 launch_k(emb::lookup_kernel<float>, grid, dim3(256), (size_t)0, (cudaStream_t)stream, a);
+  return launched();
+}
+
+int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t T, int64_t n_rows, float scale, void* dE, int64_t ldde, int accumulate,
+                       int64_t d, int dt, int wgrad_dt, void* ws, size_t ws_bytes, void* stream) {
+  if (T < 0 || n_rows < 0 || d < 0 || !valid_dt(dt) || !valid_dt(wgrad_dt)) return FLOP_ERR_INVALID_ARG;
+  if (n_rows == 0 || d == 0 || (T == 0 && accumulate)) return FLOP_OK;
+  const RowsArg dy{dY, lddy, dt}, de{dE, ldde, wgrad_dt};
+  if (!de.given() || !de.fits(d) || (T > 0 && (!ids || !dy.given() || !dy.fits(d)))) return FLOP_ERR_INVALID_ARG;
+  if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || !de.placed() || (T > 0 && !dy.placed())) return FLOP_ERR_UNSUPPORTED;
+  const Span out = de.span(n_rows, d);
+  if (T > 0 && (out.meets(dy.span(T, d)) || out.meets(Span(ids, 1, T, T, 4)))) return FLOP_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  Arena ar{(unsigned char*)ws, ws_bytes, 0};
+  const EmbWs w = plan_emb_ws(ar, T, d);
+  FLOP_TRY(check_ws(ws, ws_bytes, w.bytes));
+  emb::SortArgs s{};
+  s.ids = ids; s.T = T; s.V = (uint32_t)n_rows;
+  s.order[0] = w.order[0]; s.order[1] = w.order[1];
+  int word_bits = 1;
+  while ((uint64_t)n_rows >> word_bits) ++word_bits;          // n_rows itself stands for padding
+  s.passes = T == 0 ? 0 : (word_bits + emb::kMaxDigitBits - 1) / emb::kMaxDigitBits;
+  s.bits = T == 0 ? 1 : (word_bits + s.passes - 1) / s.passes;
+  // 2048 tokens a block: two for each thread
+  s.cluster = 1;
+  while (s.cluster < 8 && T > (int64_t)s.cluster * 2048) s.cluster *= 2;
+  int zero_blocks = 0;
+  if (!accumulate) {
+    s.dE = (unsigned char*)dE; s.row_bytes = d * (int64_t)elt(wgrad_dt); s.pitch = ldde * (int64_t)elt(wgrad_dt); s.rows = n_rows;
+    s.vec = de.vec();
+    const int64_t pieces = n_rows * ((s.row_bytes + 15) / 16);
+    zero_blocks = (int)std::min<int64_t>(round_up((pieces + emb::kSortThreads - 1) / emb::kSortThreads, s.cluster), 2 * num_sms() / s.cluster * s.cluster);
+  }
+  FLOP_TRY(launch_sort(s, emb::sort_smem(s.bits), zero_blocks, st));
+  if (T == 0) return FLOP_OK;
+  const RunPlan p = plan_runs(T, d);
+  emb::RunArgs a{};
+  a.order = w.order[0]; a.T = T; a.V = (uint32_t)n_rows; a.dY = dY; a.lddy = lddy; a.dE = dE; a.ldde = ldde; a.part = w.part; a.part_ld = w.part_ld;
+  a.chunks = p.chunks; a.chunk = p.chunk; a.scale = scale; a.d = (int)d; a.slices = p.slices; a.accumulate = accumulate; a.vec = dy.vec(); a.vec_out = de.vec();
+  if (dt == FLOP_BF16) return wgrad_dt == FLOP_BF16 ? launch_runs<bf16, bf16>(a, p.lanes, st) : launch_runs<bf16, float>(a, p.lanes, st);
+  return wgrad_dt == FLOP_BF16 ? launch_runs<float, bf16>(a, p.lanes, st) : launch_runs<float, float>(a, p.lanes, st);
+}
+
+static int dropout_impl(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* Y,
+                        int64_t ldy, int64_t T, int64_t d, int dt, void* stream) {
+  if (T < 0 || d < 0 || !valid_dt(dt) || !valid_p(p)) return FLOP_ERR_INVALID_ARG;
+  if (T == 0 || d == 0) return FLOP_OK;
+  const RowsArg x{X, ldx, dt}, r{R, ldr, dt}, y{Y, ldy, dt};
+  if (!x.given() || !x.fits(d) || !y.given() || !y.fits(d) || (r.given() && !r.fits(d))) return FLOP_ERR_INVALID_ARG;
+  if (T > INT32_MAX || d > kMaxCols || !x.placed() || !y.placed() || (r.given() && !r.placed())) return FLOP_ERR_UNSUPPORTED;
+  if (!in_place_or_apart(y, x, T, d) || !in_place_or_apart(y, r, T, d)) return FLOP_ERR_INVALID_ARG;
+  DropoutArgs a{};
+  a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.Y = Y; a.ldy = ldy; a.T = T; a.d = (int)d;
+  a.vec = x.vec() && y.vec() && (!r.given() || r.vec());
+  a.drop = make_drop(p, seed, offset, offset_dev);
+  const dim3 grid = group_grid(a, T, d, 8);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dt == FLOP_BF16) R ? launch_k(dropout_kernel<bf16, true>, grid, dim3(256), (size_t)0, st, a) : launch_k(dropout_kernel<bf16, false>, grid, dim3(256), (size_t)0, st, a);
+  else                 R ? launch_k(dropout_kernel<float, true>, grid, dim3(256), (size_t)0, st, a) : launch_k(dropout_kernel<float, false>, grid, dim3(256), (size_t)0, st, a);
+  return launched();
+}
+
+int flop_dropout_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* Y,
+                     int64_t ldy, int64_t T, int64_t d, int dt, void* stream) {
+  return dropout_impl(X, ldx, R, ldr, p, seed, offset, offset_dev, Y, ldy, T, d, dt, stream);
+}
+int flop_dropout_bwd(const void* dY, int64_t lddy, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* dX, int64_t lddx, int64_t T,
+                     int64_t d, int dt, void* stream) {
+  return dropout_impl(dY, lddy, nullptr, 0, p, seed, offset, offset_dev, dX, lddx, T, d, dt, stream);
+}
+
+int flop_layer_norm_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev,
+                        const float* weight, const float* bias, float eps, void* S, int64_t lds, void* Y, int64_t ldy, float* stats, int64_t T, int64_t d,
+                        int dt, void* stream) {
+  if (T < 0 || d < 0 || !valid_dt(dt) || !valid_p(p) || !(eps >= 0.f) || !(eps < INFINITY)) return FLOP_ERR_INVALID_ARG;
+  if (T == 0 || d == 0) return FLOP_OK;
+  const RowsArg x{X, ldx, dt}, r{R, ldr, dt}, s{S, lds, dt}, y{Y, ldy, dt};
+  if (!x.given() || !x.fits(d) || !y.given() || !y.fits(d) || (r.given() && !r.fits(d)) || (s.given() && !s.fits(d))) return FLOP_ERR_INVALID_ARG;
+  if (T > INT32_MAX || d > kMaxCols || !x.placed() || !y.placed() || (r.given() && !r.placed()) || (s.given() && !s.placed()) ||
+      (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+    return FLOP_ERR_UNSUPPORTED;
+  if (!in_place_or_apart(s, x, T, d) || !in_place_or_apart(s, r, T, d) || !in_place_or_apart(y, x, T, d) || !in_place_or_apart(y, r, T, d) || !apart(s, y, T, d))
+    return FLOP_ERR_INVALID_ARG;
+  norm::FwdArgs a{};
+  a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.S = S; a.lds = lds; a.Y = Y; a.ldy = ldy; a.w = weight; a.b = bias; a.stats = (float2*)stats; a.eps = eps;
+  a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
+  a.vec = x.vec() && y.vec() && (!r.given() || r.vec()) && (!s.given() || s.vec());
+  a.wvec = aligned16(weight) && aligned16(bias);
+  a.drop = make_drop(p, seed, offset, offset_dev);
+  const bool sum = R || S || a.drop.threshold;
+  return dt == FLOP_BF16 ? launch_norm_fwd<bf16>(a, sum, (cudaStream_t)stream) : launch_norm_fwd<float>(a, sum, (cudaStream_t)stream);
+}
+
+int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds, const float* stats, const float* weight, const void* dS, int64_t ldds,
+                        float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* dX, int64_t lddx, void* dR, int64_t lddr,
+                        float* dweight, float* dbias, int accumulate, int64_t T, int64_t d, int dt, void* ws, size_t ws_bytes, void* stream) {
+  if (T < 0 || d < 0 || !valid_dt(dt) || !valid_p(p)) return FLOP_ERR_INVALID_ARG;
+  if (d == 0) return FLOP_OK;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (d > kMaxCols || T > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  if (T == 0) {                          // sums over no rows
+    if (accumulate || (!dweight && !dbias)) return FLOP_OK;
+    launch_k(norm::bwd_finish_kernel, dim3((unsigned)((d + 31) / 32), 2), dim3(256), (size_t)0, st, (const float*)nullptr, (int64_t)0, 0, (int)d, dweight, dbias, 0);
+    return launched();
+  }
+  const RowsArg dy{dY, lddy, dt}, s{S, lds, dt}, ds{dS, ldds, dt}, dx{dX, lddx, dt}, dr{dR, lddr, dt};
+  if (!dy.given() || !dy.fits(d) || !s.given() || !s.fits(d) || !stats || (ds.given() && !ds.fits(d)) || (dx.given() && !dx.fits(d)) || (dr.given() && !dr.fits(d)))
+    return FLOP_ERR_INVALID_ARG;
+  if (!dy.placed() || !s.placed() || (ds.given() && !ds.placed()) || (dx.given() && !dx.placed()) || (dr.given() && !dr.placed()) ||
+      (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+    return FLOP_ERR_UNSUPPORTED;
+  for (const RowsArg* out : {&dx, &dr})
+    for (const RowsArg* in : {&dy, &s, &ds})
+      if (!in_place_or_apart(*out, *in, T, d)) return FLOP_ERR_INVALID_ARG;
+  if (!apart(dx, dr, T, d)) return FLOP_ERR_INVALID_ARG;
+  norm::BwdArgs a{};
+  if (dweight || dbias) {
+    Arena ar{(unsigned char*)ws, ws_bytes, 0};
+    const NormWs w = plan_norm_ws(ar, T, d);
+    FLOP_TRY(check_ws(ws, ws_bytes, w.bytes));
+    a.part = w.part; a.part_ld = w.part_ld; a.n_part = (int)w.n_part;
+  }
+  a.dY = dY; a.lddy = lddy; a.S = S; a.lds = lds; a.stats = (const float2*)stats; a.w = weight; a.dS = dS; a.ldds = ldds; a.dX = dX; a.lddx = lddx; a.dR = dR;
+  a.lddr = lddr; a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
+  a.vec = dy.vec() && s.vec() && (!ds.given() || ds.vec()) && (!dx.given() || dx.vec()) && (!dr.given() || dr.vec());
+  a.wvec = aligned16(weight);
+  a.drop = make_drop(p, seed, offset, offset_dev);
+  return dt == FLOP_BF16 ? launch_norm_bwd<bf16>(a, dweight, dbias, accumulate, st) : launch_norm_bwd<float>(a, dweight, dbias, accumulate, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,81 @@
+// Rows of tokens in units of eight columns (a "group"): 16 bytes of bf16, two pieces of 16 bytes of fp32.  The operators on token
+// rows (dropout, layer norm, embedding lookup) load, compute and store whole groups; a row's last group may hold fewer columns.
+#pragma once
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace flop {
+
+template <typename T> struct Raw8;                              // a group as it lies in memory
+template <> struct Raw8<__nv_bfloat16> { uint4 q[1]; };
+template <> struct Raw8<float> { uint4 q[2]; };
+
+// The group of `n` columns at p (n > 8: eight, n <= 0: none).  vec: rows start on 16 bytes.  inner: another row follows, so the
+// 16-byte piece that holds the row's end may be read whole.  Columns past n are not defined (unpack8 clears them).
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* p, int n, bool vec, bool inner) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(r) / 16); ++i) r.q[i] = make_uint4(0, 0, 0, 0);
+  if (vec && (n >= 8 || (inner && n > 0))) {
+    r.q[0] = *reinterpret_cast<const uint4*>(p);
+    if (sizeof(T) == 4 && n > 4) r.q[sizeof(r) / 16 - 1] = *(reinterpret_cast<const uint4*>(p) + 1);
+  } else if (n > 0) {
+    T v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : from_f32<T>(0.f);
+    memcpy(&r, v, sizeof(r));
+  }
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T>& r, int n, float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    memcpy(v, &r, 32);
+  } else {
+    const uint32_t w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = __uint_as_float(w[j] << 16);
+      v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+  }
+  if (n < 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ Raw8<T> pack8(const float (&v)[8]) {
+  Raw8<T> r;
+  if constexpr (sizeof(T) == 4) {
+    memcpy(&r, v, 32);
+  } else {
+    __nv_bfloat162 w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    memcpy(&r, w, 16);
+  }
+  return r;
+}
+
+// Columns from n on are left untouched.
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const Raw8<T>& r, int n, bool vec) {
+  if (vec && n >= 8) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r) / 16); ++i) *(reinterpret_cast<uint4*>(p) + i) = r.q[i];
+  } else {
+    T v[8];
+    memcpy(v, &r, sizeof(r));
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+
+}  // namespace flop

@@ -22,6 +22,7 @@
 // pieces of 16 bytes for loss and gradient together, 512 for the loss alone and 256 for the backward call; wider rows are walked (row_kernel).
 #pragma once
 #include "common.cuh"
+#include "pairs.cuh"
 
 namespace flop {
 namespace distill {
@@ -392,31 +393,6 @@ __global__ void __launch_bounds__(part_threads(G), P > 4 || G < 32 ? 1024 / part
 // (Batches kept in shared memory instead of read again: 610 to 650 us at 4096 x 128000, against 562; 64 registers do not hold that loop.)
 constexpr int kBatch = 4;
 
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 // 2^(x c - m) of elements 2 i and 2 i + 1
 template <typename T>
 __device__ __forceinline__ uint64_t pair_exp(const uint4& v, int i, uint64_t c2, uint64_t neg_m2) {

@@ -1548,7 +1548,7 @@ int flop_workspace_bytes(int op, int64_t T, int64_t d_in, int64_t d_out, int64_t
     case FLOP_OP_EMBEDDING_BWD: ar.used = embedding_ws_bytes(T, r); break;
     case FLOP_OP_COMPACT_FWD_I8: plan_i8_ws(ar, T, d_in, r); break;
     case FLOP_OP_EMBEDDING_SORTED_BWD: ar.used = embedding_rows_ws_bytes(T, d_in); break;
-    case FLOP_OP_LAYER_NORM_BWD: ar.used = layer_norm_ws_bytes(T, d_in); break;
+    case FLOP_OP_LAYER_NORM_BWD: ar.used = layer_norm_ws_bytes(T, d_in, dt); break;
     default: return FLOP_ERR_INVALID_ARG;
   }
   *out_bytes = align_up(ar.used, 256);

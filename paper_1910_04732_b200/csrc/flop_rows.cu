@@ -117,17 +117,61 @@ int launch_runs(const emb::RunArgs& a, int lanes, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------- layer norm
-// Parts of the column sums: enough blocks for the machine, 64 rows each at least.
-int64_t norm_parts(int64_t T, int64_t d) {
+// How a row is held: by `lanes` threads with `ng` units of 16 bytes each, in blocks of `threads`; lanes 0: rows too wide for that, which are walked.
+struct NormPlan { int lanes, ng, threads; };
+int64_t units_of(int64_t d, int dt) { return (d * (int64_t)elt(dt) + 15) / 16; }
+NormPlan plan_norm(int64_t units) {
+  if (units <= 8) return {8, 1, 128};
+  if (units <= 16) return {16, 1, 128};
+  if (units <= 32) return {32, 1, 128};
+  if (units <= 64) return {32, 2, 128};
+  if (units <= 96) return {32, 3, 128};
+  if (units <= 128) return {64, 2, 64};
+  if (units <= 256) return {128, 2, 128};
+  if (units <= 384) return {128, 3, 128};
+  if (units <= 512) return {256, 2, 256};
+  if (units <= 768) return {256, 3, 256};
+  if (units <= 1024) return {512, 2, 512};
+  if (units <= 1536) return {512, 3, 512};
+  if (units <= 1536) return {512, 3, 512};
+  if (units <= 2048) return {512, 4, 512};
+  return {0, 0, 0};
+}
+#define FLOP_HELD_PLANS(X) X(8, 1, 128) X(16, 1, 128) X(32, 1, 128) X(32, 2, 128) X(32, 3, 128) X(64, 2, 64) X(128, 2, 128) X(128, 3, 128) X(256, 2, 256) X(256, 3, 256) \
+  X(512, 2, 512) X(512, 3, 512) X(512, 4, 512)
+constexpr int between(int lo, int v, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+constexpr int kRing = 220 * 1024;                     // shared memory of an SM that the rings of its blocks may take
+// Rows that a set of threads works on at once, blocks of an SM and batches copied ahead.
+struct NormShape { int rb, blocks, stages; };
+constexpr NormShape fwd_shape(int ng, int threads, int tensors) {
+  const int rb = between(1, 4 / (ng * tensors), 4), blocks = between(1, 512 / threads, 16);
+  return {rb, blocks, between(1, kRing / (tensors * rb * ng * threads * 16 * blocks), 4)};
+}
+// One block on an SM, so that there are few parts of the column sums to add up: 512 threads, or, where a thread's three units take more than 128
+// registers, 384 (4096 x 768 bf16 15.0 us, 16.7 with 512 threads that spill).
+constexpr int bwd_threads(int lanes, int ng) { return ng < 3 || lanes == 512 ? 512 : 384 / lanes > 0 ? 384 / lanes * lanes : lanes; }
+// Two rows at once for every barrier among the warps that share one (16384 x 2048 bf16: 43.0 us, 44.5 one by one); fp32 rows are twice the bytes.
+constexpr NormShape bwd_shape(int lanes, int ng, int dt) {
+  const int rb = between(1, (lanes > 32 && dt == FLOP_BF16 ? 4 : 2) / ng, 4);
+  return {rb, 1, between(1, kRing / (3 * rb * ng * bwd_threads(lanes, ng) * 16), 4)};
+}
+int64_t norm_blocks(int lanes, int threads, int64_t T, const NormShape& s) {
+  const int64_t rows = (int64_t)(threads / lanes) * s.rb;
+  return std::min<int64_t>((T + rows - 1) / rows, (int64_t)num_sms() * s.blocks);
+}
+// Parts of the column sums: one for each block that holds rows; where rows are walked, enough blocks for the machine, 64 rows each at least.
+int64_t norm_parts(int64_t T, int64_t d, int dt) {
+  const NormPlan p = plan_norm(units_of(d, dt));
+  if (p.lanes) return norm_blocks(p.lanes, bwd_threads(p.lanes, p.ng), T, bwd_shape(p.lanes, p.ng, dt));
   const int64_t slabs = std::max<int64_t>((groups_of(d) + 31) / 32, 1);
   return std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, std::max<int64_t>(1, (int64_t)num_sms() * 4 / slabs)));
 }
 struct NormWs { float* part; int64_t part_ld, n_part; size_t bytes; };
-NormWs plan_norm_ws(Arena& ar, int64_t T, int64_t d) {
+NormWs plan_norm_ws(Arena& ar, int64_t T, int64_t d, int dt) {
   NormWs w{};
   if (T == 0 || d == 0) return w;
   w.part_ld = round_up(d, 8);
-  w.n_part = norm_parts(T, d);
+  w.n_part = norm_parts(T, d, dt);
   w.part = (float*)ar.take((size_t)w.n_part * 2 * w.part_ld * 4);
   w.bytes = ar.used;
   return w;
@@ -135,25 +179,61 @@ NormWs plan_norm_ws(Arena& ar, int64_t T, int64_t d) {
 
 int walk_threads(int groups) { return std::min(512, (groups + 31) / 32 * 32); }
 
-template <typename T>
-int launch_norm_fwd(const norm::FwdArgs& a, bool sum, cudaStream_t st) {
-  const dim3 grid((unsigned)a.T), block(walk_threads(a.groups));
-  if (sum) launch_k(norm::fwd_walk_kernel<T, true>, grid, block, (size_t)0, st, a);
-  else     launch_k(norm::fwd_walk_kernel<T, false>, grid, block, (size_t)0, st, a);
+template <typename T, bool SUM, int LANES, int NG, int THREADS>
+int launch_norm_fwd_held(const norm::FwdArgs& a, cudaStream_t st) {
+  constexpr int TENSORS = SUM ? 2 : 1;
+  constexpr NormShape s = fwd_shape(NG, THREADS, TENSORS);
+  constexpr size_t smem = (size_t)s.stages * TENSORS * s.rb * NG * THREADS * 16;
+  auto kern = norm::fwd_kernel<T, SUM, LANES, NG, s.rb, s.stages, THREADS, s.blocks>;
+  static OncePerDevice configured;
+  FLOP_TRY(allow_smem(configured, smem, kern));
+  launch_k(kern, dim3((unsigned)norm_blocks(LANES, THREADS, a.T, s)), dim3(THREADS), smem, st, a);
+  return launched();
+}
+template <typename T, bool SUM>
+int launch_norm_fwd(const norm::FwdArgs& a, cudaStream_t st) {
+  const NormPlan p = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32));
+#define FLOP_HELD(L, N, B) if (p.lanes == L && p.ng == N) return launch_norm_fwd_held<T, SUM, L, N, B>(a, st);
+  FLOP_HELD_PLANS(FLOP_HELD)
+#undef FLOP_HELD
+  launch_k(norm::fwd_walk_kernel<T, SUM>, dim3((unsigned)a.T), dim3(walk_threads(a.groups)), (size_t)0, st, a);
   return launched();
 }
 
+template <typename T, int LANES, int NG>
+int launch_norm_bwd_held(const norm::BwdArgs& a, cudaStream_t st) {
+  constexpr int THREADS = bwd_threads(LANES, NG);
+  constexpr NormShape s = bwd_shape(LANES, NG, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32);
+  auto kern = norm::bwd_kernel<T, LANES, NG, s.rb, s.stages, THREADS, s.blocks>;
+  constexpr size_t tensor = (size_t)s.stages * s.rb * NG * THREADS * 16;
+  static OncePerDevice configured;
+  FLOP_TRY(allow_smem(configured, 3 * tensor, kern));
+  launch_k(kern, dim3((unsigned)norm_blocks(LANES, THREADS, a.T, s)), dim3(THREADS), (a.dS ? 3 : 2) * tensor, st, a);
+  return launched();
+}
 template <typename T>
-int launch_norm_bwd(const norm::BwdArgs& a, float* dweight, float* dbias, int accumulate, cudaStream_t st) {
+int launch_norm_bwd_rows(const norm::BwdArgs& a, cudaStream_t st) {
+  const NormPlan p = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32));
+#define FLOP_HELD(L, N, B) if (p.lanes == L && p.ng == N) return launch_norm_bwd_held<T, L, N>(a, st);
+  FLOP_HELD_PLANS(FLOP_HELD)
+#undef FLOP_HELD
   if (a.n_part) {     // before the rows, whose outputs may take the place of what the sums read
     launch_k(norm::bwd_columns_kernel<T>, dim3((unsigned)((a.groups + 31) / 32), (unsigned)a.n_part), dim3(256), (size_t)0, st, a);
-    FLOP_TRY(launched());
-    launch_k(norm::bwd_finish_kernel, dim3((unsigned)((a.d + 31) / 32), 2), dim3(256), (size_t)0, st, (const float*)a.part, a.part_ld, a.n_part, a.d, dweight,
-             dbias, accumulate);
     FLOP_TRY(launched());
   }
   if (a.dX || a.dR) {
     launch_k(norm::bwd_walk_kernel<T>, dim3((unsigned)a.T), dim3(walk_threads(a.groups)), (size_t)0, st, a);
+    FLOP_TRY(launched());
+  }
+  return FLOP_OK;
+}
+template <typename T>
+int launch_norm_bwd(const norm::BwdArgs& a, cudaStream_t st) {
+  if (a.n_part || a.dX || a.dR) FLOP_TRY(launch_norm_bwd_rows<T>(a, st));
+  const bool held = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32)).lanes > 0;
+  if (a.n_part > 1 || (a.n_part && !held)) {       // a single block that holds rows has written the sums itself
+    launch_k(norm::bwd_finish_kernel, dim3((unsigned)((a.d + 31) / 32), 2), dim3(32 * norm::kFinishWarps), (size_t)0, st, (const float*)a.part, a.part_ld, a.n_part, a.d, a.dweight,
+             a.dbias, a.accumulate);
     FLOP_TRY(launched());
   }
   return FLOP_OK;
@@ -166,9 +246,9 @@ size_t embedding_rows_ws_bytes(int64_t T, int64_t d) {
   Arena ar{nullptr, 0, 0};
   return plan_emb_ws(ar, T, d).bytes;
 }
-size_t layer_norm_ws_bytes(int64_t T, int64_t d) {
+size_t layer_norm_ws_bytes(int64_t T, int64_t d, int dt) {
   Arena ar{nullptr, 0, 0};
-  return plan_norm_ws(ar, T, d).bytes;
+  return plan_norm_ws(ar, T, d, dt).bytes;
 }
 }  // namespace flop
 
@@ -278,7 +358,9 @@ int flop_layer_norm_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, 
   a.wvec = aligned16(weight) && aligned16(bias);
   a.drop = make_drop(p, seed, offset, offset_dev);
   const bool sum = R || S || a.drop.threshold;
-  return dt == FLOP_BF16 ? launch_norm_fwd<bf16>(a, sum, (cudaStream_t)stream) : launch_norm_fwd<float>(a, sum, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dt == FLOP_BF16) return sum ? launch_norm_fwd<bf16, true>(a, st) : launch_norm_fwd<bf16, false>(a, st);
+  return sum ? launch_norm_fwd<float, true>(a, st) : launch_norm_fwd<float, false>(a, st);
 }
 
 int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds, const float* stats, const float* weight, const void* dS, int64_t ldds,
@@ -290,7 +372,7 @@ int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds
   if (d > kMaxCols || T > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
   if (T == 0) {                          // sums over no rows
     if (accumulate || (!dweight && !dbias)) return FLOP_OK;
-    launch_k(norm::bwd_finish_kernel, dim3((unsigned)((d + 31) / 32), 2), dim3(256), (size_t)0, st, (const float*)nullptr, (int64_t)0, 0, (int)d, dweight, dbias, 0);
+    launch_k(norm::bwd_finish_kernel, dim3((unsigned)((d + 31) / 32), 2), dim3(32 * norm::kFinishWarps), (size_t)0, st, (const float*)nullptr, (int64_t)0, 0, (int)d, dweight, dbias, 0);
     return launched();
   }
   const RowsArg dy{dY, lddy, dt}, s{S, lds, dt}, ds{dS, ldds, dt}, dx{dX, lddx, dt}, dr{dR, lddr, dt};
@@ -306,16 +388,17 @@ int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds
   norm::BwdArgs a{};
   if (dweight || dbias) {
     Arena ar{(unsigned char*)ws, ws_bytes, 0};
-    const NormWs w = plan_norm_ws(ar, T, d);
+    const NormWs w = plan_norm_ws(ar, T, d, dt);
     FLOP_TRY(check_ws(ws, ws_bytes, w.bytes));
     a.part = w.part; a.part_ld = w.part_ld; a.n_part = (int)w.n_part;
   }
+  a.dweight = dweight; a.dbias = dbias; a.accumulate = accumulate;
   a.dY = dY; a.lddy = lddy; a.S = S; a.lds = lds; a.stats = (const float2*)stats; a.w = weight; a.dS = dS; a.ldds = ldds; a.dX = dX; a.lddx = lddx; a.dR = dR;
   a.lddr = lddr; a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
   a.vec = dy.vec() && s.vec() && (!ds.given() || ds.vec()) && (!dx.given() || dx.vec()) && (!dr.given() || dr.vec());
   a.wvec = aligned16(weight);
   a.drop = make_drop(p, seed, offset, offset_dev);
-  return dt == FLOP_BF16 ? launch_norm_bwd<bf16>(a, dweight, dbias, accumulate, st) : launch_norm_bwd<float>(a, dweight, dbias, accumulate, st);
+  return dt == FLOP_BF16 ? launch_norm_bwd<bf16>(a, st) : launch_norm_bwd<float>(a, st);
 }
 
 }  // extern "C"

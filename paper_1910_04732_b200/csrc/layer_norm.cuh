@@ -6,6 +6,7 @@
 // Sums, means and the deviation are fp32; the variance is the mean of squared differences from the mean (a second look at the row).
 #pragma once
 #include "dropout.cuh"
+#include "pairs.cuh"
 
 namespace flop {
 namespace norm {
@@ -31,7 +32,8 @@ struct BwdArgs {
   const void* dS; int64_t ldds;     // nullable
   void* dX; int64_t lddx;           // nullable
   void* dR; int64_t lddr;           // nullable
-  float* part; int64_t part_ld; int n_part;   // column sums: [n_part][2][part_ld]
+  float* part; int64_t part_ld; int n_part;   // column sums: [n_part][2][part_ld] (null: not wanted)
+  float* dweight; float* dbias; int accumulate;
   int64_t T;
   int d, groups, vec, wvec;
   Drop drop;
@@ -203,6 +205,457 @@ bwd_walk_kernel(const BwdArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- rows held in registers, copied ahead
+// A row is shared by LANES threads, NG units of 16 bytes each (8 columns of bf16, 4 of fp32; a unit is LANES units behind the thread's one before, so
+// that a warp's accesses are contiguous), always the same columns: weights, and in the backward pass the column sums, stay in
+// registers from row to row.  A block works on RB rows of each set of LANES threads at once and walks every gridDim.x-th batch;
+// every thread copies its own units of the next STAGES batches to shared memory asynchronously and reads them back itself, so nothing has to be
+// waited for but the thread's own copies, and the memory system always has work in flight: under load an access takes 1.5 to 2 us, and a
+// kernel that loads, computes and stores a row at a time has a quarter of the bytes in flight that this needs.
+// All units but the last of a thread are whole and present (the host picks LANES and NG so), which leaves one to be looked at.
+template <typename T> constexpr int kUnit = 16 / (int)sizeof(T);      // columns of a unit
+template <typename T> constexpr int kPairs = kUnit<T> / 2;
+
+__device__ __forceinline__ void copy_async16(void* to, const void* from, int bytes) {      // zeros behind `bytes`
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async4(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The thread's units of a row (`from`: its first), `last` columns in the last one (<= 0: none), into its slots, THREADS apart.  No such row (on is false): zeros.
+template <typename T, int LANES, int NG, int THREADS>
+__device__ __forceinline__ void copy_units(uint4* to, const T* from, int last, bool on, bool vec) {
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int n = !on ? 0 : i < NG - 1 ? kUnit<T> : min(max(last, 0), kUnit<T>);
+    const T* at = from + i * LANES * kUnit<T>;
+    if (sizeof(T) == 2 || vec) {
+      copy_async16(to + i * THREADS, at, n * (int)sizeof(T));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnit<T>; ++j) copy_async4(reinterpret_cast<T*>(to + i * THREADS) + j, at + j, j < n ? 4 : 0);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void unpack_unit(const uint4& q, uint64_t (&v)[kPairs<T>]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int j = 0; j < kPairs<T>; ++j) {
+    if constexpr (sizeof(T) == 2) v[j] = pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+    else v[j] = pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_unit(const uint64_t (&v)[kPairs<T>]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < kPairs<T>; ++j) {
+    const float2 u = unpack2(v[j]);
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(u.x, u.y);
+      memcpy(&w[j], &h, 4);
+    } else {
+      w[2 * j] = __float_as_uint(u.x);
+      w[2 * j + 1] = __float_as_uint(u.y);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store_unit(T* p, const uint4& q, int n, bool vec) {
+  if ((sizeof(T) == 2 || vec) && n >= kUnit<T>) {
+    *reinterpret_cast<uint4*>(p) = q;
+  } else {
+    T v[kUnit<T>];
+    memcpy(v, &q, 16);
+#pragma unroll
+    for (int j = 0; j < kUnit<T>; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+// Pairs of a vector's columns; absent ones 0.
+template <typename T>
+__device__ __forceinline__ void vector_unit(const float* p, int k, int n, bool vec, float dflt, uint64_t (&v)[kPairs<T>]) {
+  float f[kUnit<T>];
+#pragma unroll
+  for (int j = 0; j < kUnit<T>; j += 4) {
+    if (p && vec && n >= j + 4) {
+      *reinterpret_cast<float4*>(f + j) = __ldg(reinterpret_cast<const float4*>(p + k + j));
+    } else {
+#pragma unroll
+      for (int i = j; i < j + 4; ++i) f[i] = i < n ? (p ? __ldg(p + k + i) : dflt) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kPairs<T>; ++j) v[j] = pack2(f[2 * j], f[2 * j + 1]);
+}
+
+// The mask's bits for the thread's units, 16 for each column.  A unit of fp32 is half a block of the generator: the two threads of a pair draw one block each
+// for every two units and exchange halves.  All lanes of a warp come here together.
+template <typename T, int LANES, int NG>
+__device__ __forceinline__ void drop_units(const Drop& d, uint64_t row, int l, uint32_t (&bits)[NG][kPairs<T>]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const uint4 x = drop_bits(d, row + (uint32_t)(l + i * LANES));
+      bits[i][0] = x.x; bits[i][1] = x.y; bits[i][2] = x.z; bits[i][3] = x.w;
+    }
+  } else {
+    const bool odd = l & 1;
+#pragma unroll
+    for (int i = 0; i < NG; i += 2) {
+      const uint4 x = drop_bits(d, row + (uint32_t)((l + (i + (i + 1 < NG && odd)) * LANES) >> 1));
+      const uint32_t keep[2] = {odd ? x.z : x.x, odd ? x.w : x.y};
+      if (i + 1 < NG) {
+        const uint32_t got[2] = {__shfl_xor_sync(0xffffffffu, odd ? x.x : x.z, 1), __shfl_xor_sync(0xffffffffu, odd ? x.y : x.w, 1)};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          bits[i][j] = odd ? got[j] : keep[j];
+          bits[i + 1][j] = odd ? keep[j] : got[j];
+        }
+      } else {
+        bits[i][0] = keep[0];
+        bits[i][1] = keep[1];
+      }
+    }
+  }
+}
+__device__ __forceinline__ uint64_t select_pair(uint32_t bits, uint32_t threshold, uint64_t kept, uint64_t dropped) {
+  const float2 k = unpack2(kept), d = unpack2(dropped);
+  return pack2((bits & 0xFFFFu) >= threshold ? k.x : d.x, (bits >> 16) >= threshold ? k.y : d.y);
+}
+
+// Sums over the LANES threads that share a row, in a fixed order; every one gets them.  Rows of several warps have a barrier each; `scratch` (one
+// of two, in turn) is free again once the sum after the next begins.
+template <int LANES, int THREADS, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*scratch)[32]) {
+#pragma unroll
+  for (int o = (LANES < 32 ? LANES : 32) / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  if constexpr (LANES > 32) {
+    const int warp = threadIdx.x >> 5, first = warp / (LANES / 32) * (LANES / 32);
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) scratch[i][warp] = v[i];
+    }
+    if constexpr (LANES == THREADS) __syncthreads();     // a barrier named at run time would take all of a block's barriers, and so keep blocks from the SM
+    else asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.x / LANES + 1), "n"(LANES) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < LANES / 32; ++w) v[i] += scratch[i][first + w];
+    }
+  }
+}
+__device__ __forceinline__ float both(uint64_t v) {
+  const float2 u = unpack2(v);
+  return u.x + u.y;
+}
+
+template <typename T, bool SUM, int LANES, int NG, int RB, int STAGES, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS)
+fwd_kernel(const FwdArgs a) {
+  constexpr int ROWS = THREADS / LANES, E = kUnit<T>, H = kPairs<T>, ROW = NG * THREADS, SIZE = (SUM ? 2 : 1) * RB * ROW;
+  extern __shared__ uint4 ring[];                        // [STAGES][X and R][RB][NG][THREADS]
+  __shared__ float scratch[2][RB][32];
+  const int l = threadIdx.x % LANES, r = threadIdx.x / LANES;
+  const int last = a.d - (l + (NG - 1) * LANES) * E;     // columns of the last unit
+  const int batches = (int)((a.T + ROWS * RB - 1) / (ROWS * RB));
+  const float inv_d = 1.f / (float)a.d;
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint64_t offset = SUM ? drop_offset(a.drop) : 0, scale = SUM ? pack2(a.drop.scale, a.drop.scale) : 0;
+  auto fetch = [&](int batch, int stage) {
+    uint4* to = ring + stage * SIZE + threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+      copy_units<T, LANES, NG, THREADS>(to + q * ROW, (const T*)a.X + t * a.ldx + l * E, last, t < a.T, a.vec);
+      if (SUM && a.R) copy_units<T, LANES, NG, THREADS>(to + (RB + q) * ROW, (const T*)a.R + t * a.ldr + l * E, last, t < a.T, a.vec);
+    }
+  };
+#pragma unroll
+  for (int st = 0; st < STAGES; ++st) {
+    const int batch = blockIdx.x + st * gridDim.x;
+    if (batch < batches) fetch(batch, st);
+    copies_commit();
+  }
+  uint64_t w[NG][H], b[NG][H];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int k = (l + i * LANES) * E;
+    vector_unit<T>(a.w, k, a.d - k, a.wvec, 1.f, w[i]);
+    vector_unit<T>(a.b, k, a.d - k, a.wvec, 0.f, b[i]);
+  }
+  int stage = 0;
+  for (int batch = blockIdx.x; batch < batches; batch += gridDim.x) {
+    copies_wait<STAGES - 1>();
+    const uint4* at = ring + stage * SIZE + threadIdx.x;
+    uint64_t s[RB][NG][H];
+    float sum[RB];
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+      uint64_t total = 0;
+      uint32_t bits[NG][H];
+      if (SUM && a.drop.threshold) drop_units<T, LANES, NG>(a.drop, offset + (uint64_t)t * a.groups, l, bits);
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        unpack_unit<T>(at[q * ROW + i * THREADS], s[q][i]);
+        if constexpr (SUM) {
+          uint64_t res[H];
+          if (a.R) {
+            unpack_unit<T>(at[(RB + q) * ROW + i * THREADS], res);
+          } else {
+#pragma unroll
+            for (int j = 0; j < H; ++j) res[j] = 0;
+          }
+#pragma unroll
+          for (int j = 0; j < H; ++j)
+            s[q][i][j] = a.drop.threshold ? select_pair(bits[i][j], a.drop.threshold, fma2(s[q][i][j], scale, res[j]), res[j]) : add2(s[q][i][j], res[j]);
+          const uint4 rounded = pack_unit<T>(s[q][i]);
+          const int n = i < NG - 1 ? E : last;
+          if (a.S && t < a.T && n > 0) store_unit((T*)a.S + t * a.lds + (l + i * LANES) * E, rounded, n, a.vec);
+          unpack_unit<T>(rounded, s[q][i]);
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) total = add2(total, s[q][i][j]);
+      }
+      sum[q] = both(total);
+    }
+    const int ahead = batch + STAGES * gridDim.x;
+    if (ahead < batches) fetch(ahead, stage);
+    copies_commit();
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    row_sum<LANES, THREADS>(sum, scratch[0]);
+    float mean[RB];
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      mean[q] = sum[q] * inv_d;
+      const uint64_t minus = pack2(-mean[q], -mean[q]);
+      uint64_t total = 0;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+#pragma unroll
+        for (int j = 0; j < H; ++j) s[q][i][j] = add2(s[q][i][j], minus);
+        if (i == NG - 1 && last < E) {                   // what lies behind the row's end is no difference
+#pragma unroll
+          for (int j = 0; j < H; ++j) {
+            const float2 u = unpack2(s[q][i][j]);
+            s[q][i][j] = pack2(2 * j < last ? u.x : 0.f, 2 * j + 1 < last ? u.y : 0.f);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) total = fma2(s[q][i][j], s[q][i][j], total);
+      }
+      sum[q] = both(total);
+    }
+    row_sum<LANES, THREADS>(sum, scratch[1]);
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+      if (t >= a.T) break;
+      const float rstd = rsqrtf(fmaf(sum[q], inv_d, a.eps));
+      if (a.stats && l == 0) a.stats[t] = make_float2(mean[q], rstd);
+      const uint64_t by = pack2(rstd, rstd);
+      T* Y = (T*)a.Y + t * a.ldy + l * E;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int n = i < NG - 1 ? E : last;
+        if (n > 0) {
+#pragma unroll
+          for (int j = 0; j < H; ++j) s[q][i][j] = fma2(mul2(s[q][i][j], by), w[i][j], b[i][j]);
+          store_unit(Y + i * LANES * E, pack_unit<T>(s[q][i]), n, a.vec);
+        }
+      }
+    }
+  }
+}
+
+// Backward: the same, and with the rows the running column sums.  x^ and a are formed twice, from the ring, before and after the row's sums are known: kept in
+// registers beside the column sums they cost 40 registers and a quarter of the warps (16384 x 2048 bf16: 45 against 41 us).  The block's sums go
+// to its place in the workspace or, where it is the only block, to dweight and dbias.
+template <typename T, int LANES, int NG, int RB, int STAGES, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS)
+bwd_kernel(const BwdArgs a) {
+  constexpr int ROWS = THREADS / LANES, E = kUnit<T>, H = kPairs<T>, ROW = NG * THREADS;
+  extern __shared__ uint4 ring[];                        // [STAGES][S, dY and, where there is one, dS][RB][NG][THREADS]
+  __shared__ float scratch[2][2 * RB][32];
+  const int size = (a.dS ? 3 : 2) * RB * ROW;
+  const int l = threadIdx.x % LANES, r = threadIdx.x / LANES;
+  const int last = a.d - (l + (NG - 1) * LANES) * E;
+  const int batches = (int)((a.T + ROWS * RB - 1) / (ROWS * RB));
+  const float inv_d = 1.f / (float)a.d;
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint64_t offset = drop_offset(a.drop), scale = pack2(a.drop.scale, a.drop.scale);
+  auto fetch = [&](int batch, int stage) {
+    uint4* to = ring + stage * size + threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+      copy_units<T, LANES, NG, THREADS>(to + q * ROW, (const T*)a.S + t * a.lds + l * E, last, t < a.T, a.vec);
+      copy_units<T, LANES, NG, THREADS>(to + (RB + q) * ROW, (const T*)a.dY + t * a.lddy + l * E, last, t < a.T, a.vec);
+      if (a.dS) copy_units<T, LANES, NG, THREADS>(to + (2 * RB + q) * ROW, (const T*)a.dS + t * a.ldds + l * E, last, t < a.T, a.vec);
+    }
+  };
+  float2 next[RB];                                       // (mean, rstd) of the next batch's rows
+  auto fetch_stats = [&](int batch) {
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+      next[q] = t < a.T ? a.stats[t] : make_float2(0.f, 0.f);
+    }
+  };
+  fetch_stats(blockIdx.x);
+#pragma unroll
+  for (int st = 0; st < STAGES; ++st) {
+    const int batch = blockIdx.x + st * gridDim.x;
+    if (batch < batches) fetch(batch, st);
+    copies_commit();
+  }
+  uint64_t w[NG][H], dw[NG][H], db[NG][H];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int k = (l + i * LANES) * E;
+    vector_unit<T>(a.w, k, a.d - k, a.wvec, 1.f, w[i]);
+#pragma unroll
+    for (int j = 0; j < H; ++j) dw[i][j] = db[i][j] = 0;
+  }
+  int stage = 0, turn = 0;
+  for (int batch = blockIdx.x; batch < batches; batch += gridDim.x) {
+    float2 st[RB];
+#pragma unroll
+    for (int q = 0; q < RB; ++q) st[q] = next[q];
+    if (batch + (int)gridDim.x < batches) fetch_stats(batch + gridDim.x);
+    copies_wait<STAGES - 1>();
+    const uint4* at = ring + stage * size + threadIdx.x;
+    uint64_t xv[H], yv[H];                               // x^; dy, then a = dy w
+    auto load = [&](int q, int i) {
+      const uint64_t minus = pack2(-st[q].x, -st[q].x), by = pack2(st[q].y, st[q].y);
+      unpack_unit<T>(at[q * ROW + i * THREADS], xv);
+      unpack_unit<T>(at[(RB + q) * ROW + i * THREADS], yv);                               // 0 behind the row's end, and so is what is added up
+#pragma unroll
+      for (int j = 0; j < H; ++j) xv[j] = mul2(add2(xv[j], minus), by);
+    };
+    float c[2 * RB];
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+      uint64_t c0 = 0, c1 = 0;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        load(q, i);
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          dw[i][j] = fma2(yv[j], xv[j], dw[i][j]);
+          db[i][j] = add2(db[i][j], yv[j]);
+          yv[j] = mul2(yv[j], w[i][j]);
+          c0 = add2(c0, yv[j]);
+          c1 = fma2(yv[j], xv[j], c1);
+        }
+      }
+      c[2 * q] = both(c0);
+      c[2 * q + 1] = both(c1);
+    }
+    if (a.dX || a.dR) {
+      row_sum<LANES, THREADS>(c, scratch[turn]);
+      turn ^= 1;
+#pragma unroll
+      for (int q = 0; q < RB; ++q) {
+        const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+        const bool on = t < a.T;
+        const float c1 = -c[2 * q] * inv_d, c2 = -c[2 * q + 1] * inv_d;
+        const uint64_t m1 = pack2(c1, c1), m2 = pack2(c2, c2), by = pack2(st[q].y, st[q].y);
+        uint32_t bits[NG][H];
+        if (a.dX && a.drop.threshold) drop_units<T, LANES, NG>(a.drop, offset + (uint64_t)t * a.groups, l, bits);
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int k = (l + i * LANES) * E, n = i < NG - 1 ? E : last;
+          load(q, i);
+#pragma unroll
+          for (int j = 0; j < H; ++j) yv[j] = mul2(fma2(xv[j], m2, fma2(yv[j], w[i][j], m1)), by);
+          if (a.dS) {
+            uint64_t e[H];
+            unpack_unit<T>(at[(2 * RB + q) * ROW + i * THREADS], e);
+#pragma unroll
+            for (int j = 0; j < H; ++j) yv[j] = add2(yv[j], e[j]);
+          }
+          if (on && n > 0) {
+            if (a.dR) store_unit((T*)a.dR + t * a.lddr + k, pack_unit<T>(yv), n, a.vec);
+            if (a.dX) {
+              if (a.drop.threshold) {
+#pragma unroll
+                for (int j = 0; j < H; ++j) yv[j] = select_pair(bits[i][j], a.drop.threshold, mul2(yv[j], scale), 0);
+              }
+              store_unit((T*)a.dX + t * a.lddx + k, pack_unit<T>(yv), n, a.vec);
+            }
+          }
+        }
+      }
+    }
+    const int ahead = batch + STAGES * gridDim.x;
+    if (ahead < batches) fetch(ahead, stage);
+    copies_commit();
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+  }
+  if (!a.part) return;
+  const bool only = gridDim.x == 1;
+  float* out[2] = {only ? a.dweight : a.part + (int64_t)blockIdx.x * 2 * a.part_ld, only ? a.dbias : a.part + ((int64_t)blockIdx.x * 2 + 1) * a.part_ld};
+  auto put = [&](int h, int k, float v) {
+    float* p = out[h];
+    if (p && k < a.d) p[k] = only && a.accumulate ? p[k] + v : v;
+  };
+  if constexpr (ROWS > 1) {                              // the sums of the sets of threads are added in order
+    constexpr int WIDTH = NG * LANES * E;
+    static_assert(ROWS * 2 * WIDTH * 4 <= STAGES * 2 * RB * ROW * 16);
+    copies_wait<0>();                                    // the ring is free
+    float* red = reinterpret_cast<float*>(ring);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+#pragma unroll
+      for (int j = 0; j < H; ++j) {
+        const int k = (l + i * LANES) * E + 2 * j;
+        *reinterpret_cast<uint64_t*>(red + (r * 2) * WIDTH + k) = dw[i][j];
+        *reinterpret_cast<uint64_t*>(red + (r * 2 + 1) * WIDTH + k) = db[i][j];
+      }
+    __syncthreads();
+    for (int q = threadIdx.x; q < 2 * WIDTH; q += THREADS) {
+      float s = 0.f;
+#pragma unroll
+      for (int o = 0; o < ROWS; ++o) s += red[o * 2 * WIDTH + q];
+      put(q / WIDTH, q % WIDTH, s);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = (l + i * LANES) * E;
+        float f[E];
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          const float2 u = unpack2(h ? db[i][j] : dw[i][j]);
+          f[2 * j] = u.x;
+          f[2 * j + 1] = u.y;
+        }
+        if (!only && k < a.d) {                          // a part's row has room for whole groups
+#pragma unroll
+          for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(out[h] + k + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < E; ++j) put(h, k + j, f[j]);
+        }
+      }
+  }
+}
+
 // Column sums of dy x^ and dy over a run of rows: 32 groups across, eight rows at a time; the eight are added in order.
 template <typename T>
 __global__ void __launch_bounds__(256)
@@ -243,18 +696,19 @@ bwd_columns_kernel(const BwdArgs a) {
 }
 
 // dweight and dbias (=|+=) the partial sums of a column: 32 columns a block, a warp adds a run of the partials, the runs are added in order.
-__global__ void __launch_bounds__(256)
+constexpr int kFinishWarps = 16;
+__global__ void __launch_bounds__(32 * kFinishWarps)
 bwd_finish_kernel(const float* __restrict__ part, int64_t part_ld, int n_part, int d, float* dweight, float* dbias, int accumulate) {
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ float red[8][32];
+  __shared__ float red[kFinishWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
   float* out = blockIdx.y ? dbias : dweight;
   if (!out) return;
-  const int per = (n_part + 7) / 8, p1 = min(n_part, (warp + 1) * per);
+  const int per = (n_part + kFinishWarps - 1) / kFinishWarps, p1 = min(n_part, (warp + 1) * per);
   float s = 0.f;
   if (k < d) {
-#pragma unroll 8
+#pragma unroll 10
     for (int p = warp * per; p < p1; ++p) s += part[((int64_t)p * 2 + blockIdx.y) * part_ld + k];
   }
   red[warp][lane] = s;
@@ -262,7 +716,7 @@ bwd_finish_kernel(const float* __restrict__ part, int64_t part_ld, int n_part, i
   if (warp == 0 && k < d) {
     s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += red[w][lane];
+    for (int w = 0; w < kFinishWarps; ++w) s += red[w][lane];
     out[k] = accumulate ? out[k] + s : s;
   }
 }

@@ -5,5 +5,5 @@
 
 namespace flop {
 size_t embedding_rows_ws_bytes(int64_t T, int64_t d);
-size_t layer_norm_ws_bytes(int64_t T, int64_t d);
+size_t layer_norm_ws_bytes(int64_t T, int64_t d, int dt);
 }  // namespace flop

@@ -501,7 +501,7 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
 /* Operators on token rows, in front of and between the factorised matrices of a model in training (no counterpart in the paper).
  * dt is the type of every matrix of a call; bf16 matrices follow the header's rules on alignment, fp32 ones may start anywhere and have any
  * leading dimension (rows that start on 16 bytes are faster).  Columns of an output from d on are left untouched.
- * At most 2^31 - 1 rows, 2^30 columns (FLOP_ERR_UNSUPPORTED beyond).
+ * At most 2^31 - 1 rows, 2^24 columns (FLOP_ERR_UNSUPPORTED beyond).
  *
  * Embedding, dense (the counterpart of flop_gated_embedding_* for a table that is not factorised): ids[T] (int32, DEVICE) are rows of
  * E[n_rows, d]; ids outside [0, n_rows) are padding.

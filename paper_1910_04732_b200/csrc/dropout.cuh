@@ -27,47 +27,41 @@ __device__ __forceinline__ bool drop_keeps(const uint4& x, int j, uint32_t thres
   const uint32_t w = j < 2 ? x.x : j < 4 ? x.y : j < 6 ? x.z : x.w;
   return (j & 1 ? w >> 16 : w & 0xFFFFu) >= threshold;
 }
-
-struct DropoutArgs {
-  const void* X; int64_t ldx;
-  const void* R; int64_t ldr;
-  void* Y; int64_t ldy;
-  int64_t T, total;                 // rows, groups of all rows
-  int d, groups;                    // columns, groups of a row
-  int64_t step_rows; int step_groups;   // what the grid's stride is in rows and groups
-  int vec;
-  Drop drop;
-};
-
-template <typename T, bool RES>
-__global__ void __launch_bounds__(256)
-dropout_kernel(const DropoutArgs a) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const uint64_t offset = drop_offset(a.drop);
-  int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, t = i / a.groups;
-  int g = (int)(i - t * a.groups);
-  for (; i < a.total; i += (int64_t)gridDim.x * blockDim.x) {
-    const int n = a.d - g * 8;
-    const bool inner = t + 1 < a.T;
-    const Raw8<T> xr = load8((const T*)a.X + t * a.ldx + g * 8, n, a.vec, inner);
-    Raw8<T> rr;
-    if (RES) rr = load8((const T*)a.R + t * a.ldr + g * 8, n, a.vec, inner);
-    const uint4 bits = drop_bits(a.drop, offset + (uint64_t)i);
-    float x[8], r[8];
-    unpack8(xr, n, x);
-    if (RES) unpack8(rr, n, r);
+// The bits of a thread's NU units, 16 for each column; group(i): the counter of unit i's group.  A unit of fp32 is half a group: the even thread of a pair has the first
+// half of both threads' groups, the odd one the second; each draws every other group and they exchange halves.  All lanes of a warp come here
+// together.
+template <typename T, int NU, typename F>
+__device__ __forceinline__ void drop_units(const Drop& d, bool odd, F&& group, uint32_t (&bits)[NU][kPairs<T>]) {
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool keep = drop_keeps(bits, j, a.drop.threshold);
-      if (RES) x[j] = keep ? fmaf(x[j], a.drop.scale, r[j]) : r[j];
-      else x[j] = keep ? x[j] * a.drop.scale : 0.f;
+    for (int i = 0; i < NU; ++i) {
+      const uint4 x = drop_bits(d, group(i));
+      bits[i][0] = x.x; bits[i][1] = x.y; bits[i][2] = x.z; bits[i][3] = x.w;
     }
-    store8((T*)a.Y + t * a.ldy + g * 8, pack8<T>(x), n, a.vec);
-    t += a.step_rows;
-    g += a.step_groups;
-    if (g >= a.groups) { g -= a.groups; ++t; }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NU; i += 2) {
+      const uint64_t even_group = group(i), odd_group = group(i + 1 < NU ? i + 1 : i);
+      const uint4 x = drop_bits(d, odd ? odd_group : even_group);
+      const uint32_t keep[2] = {odd ? x.z : x.x, odd ? x.w : x.y};
+      if (i + 1 < NU) {
+        const uint32_t got[2] = {__shfl_xor_sync(0xffffffffu, odd ? x.x : x.z, 1), __shfl_xor_sync(0xffffffffu, odd ? x.y : x.w, 1)};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          bits[i][j] = odd ? got[j] : keep[j];
+          bits[i + 1 < NU ? i + 1 : i][j] = odd ? keep[j] : got[j];
+        }
+      } else {
+        bits[i][0] = keep[0];
+        bits[i][1] = keep[1];
+      }
+    }
   }
+}
+__device__ __forceinline__ uint64_t select_pair(uint32_t bits, uint32_t threshold, uint64_t kept, uint64_t dropped) {
+  const float2 k = unpack2(kept), d = unpack2(dropped);
+  const uint32_t above = threshold << 16;                // what is below the half compared does not matter
+  return pack2((bits << 16) >= above ? k.x : d.x, bits >= above ? k.y : d.y);
 }
 
 }  // namespace flop

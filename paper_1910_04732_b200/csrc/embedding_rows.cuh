@@ -2,13 +2,15 @@
 // Words outside the table are padding: a row of zeros, no gradient.
 //
 // The gradient sorts the tokens by word (stably: a word's tokens stay in the order of the batch) and adds up runs of equal words.  Every
-// sum is taken in fp32 in an order that depends on the sizes only, every row is written once, and there are no atomics.
+// sum is taken in fp32 in an order that depends on the sizes only, every row is written once, and there are no atomics on sums.
 //   sort_kernel   : one thread-block cluster sorts (word, token) pairs, least significant digit first; the blocks behind it clear dE
-//                   meanwhile, because most rows of a large table stay empty
+//                   meanwhile, because most rows of a large table stay empty.  Long batches are sorted by two launches a digit (sort_count_kernel,
+//                   sort_move_kernel) on as many blocks as they fill
 //   runs_kernel   : the sorted tokens in chunks of equal length, whatever the words: a word that fills half of a batch is
 //                   as well spread over the machine as a batch of rare ones.  A run that lies within a chunk is written to dE; what a chunk holds of
 //                   a run that crosses its border goes to the workspace
 //   joints_kernel : adds up the parts of the runs that cross borders, in order
+//   few_kernel    : few tokens need none of this: a block for each token looks through all words, and the first of equal ones adds up
 #pragma once
 #include <cooperative_groups.h>
 
@@ -18,288 +20,716 @@ namespace flop {
 namespace emb {
 
 // ---------------------------------------------------------------- lookup
+struct Walk {
+  int64_t total;                    // units of all rows
+  int per_row;                      // units of a row
+  int64_t tile_rows, near_rows;     // the grid's stride, and 256 units, as rows and units of a row
+  int tile_units, near_units;
+};
+struct At {
+  int64_t i, t;
+  int c;
+  __device__ __forceinline__ void step(int64_t units, int64_t rows, int rest, int per_row) {
+    i += units;
+    t += rows;
+    c += rest;
+    if (c >= per_row) { c -= per_row; ++t; }
+  }
+};
 struct LookupArgs {
   const int32_t* ids; int64_t T;
   const void* E; int64_t lde; int64_t V;
   void* Y; int64_t ldy;
   float scale;
-  int d, groups;
-  int64_t total, step_rows; int step_groups;   // groups of all rows; the grid's stride in rows and groups
-  int vec;
+  int d, vec;
+  Walk walk;
 };
 
-template <typename T>
+// A walk over the units of all rows: a block takes tiles of U x 256 units in turn, unit j of a thread 256 behind unit j - 1; first the words of all U, then their rows.
+// Positions are (row, unit of the row), carried from tile to tile without divisions.  (A ring of tiles copied ahead, which carries the other operators
+// here, is slower: a row's address waits for its word, 16384 x 2048 bf16 16.5 us, 21 with the ring.  Writing alone bounds it: 5.9 TB/s.)
+template <typename T, int U>
 __global__ void __launch_bounds__(256)
 lookup_kernel(const LookupArgs a) {
   pdl_wait();
   pdl_launch_dependents();
-  int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, t = i / a.groups;
-  int g = (int)(i - t * a.groups);
-  for (; i < a.total; i += (int64_t)gridDim.x * blockDim.x) {
-    const int n = a.d - g * 8;
-    const int64_t id = a.ids[t];
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (id >= 0 && id < a.V) {
-      unpack8(load8((const T*)a.E + id * a.lde + g * 8, n, a.vec, id + 1 < a.V), n, v);
+  constexpr int H = kPairs<T>;
+  const uint64_t scale = pack2(a.scale, a.scale);
+  At at;
+  at.i = (int64_t)blockIdx.x * (U * 256) + threadIdx.x;
+  at.t = at.i / a.walk.per_row;
+  at.c = (int)(at.i - at.t * a.walk.per_row);
+  const int64_t stride = (int64_t)gridDim.x * (U * 256);
+  for (int64_t first = (int64_t)blockIdx.x * (U * 256); first < a.walk.total; first += stride) {
+    int64_t row[U];
+    int k[U], id[U];
+    At it = at;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= a.scale;
+    for (int u = 0; u < U; ++u) {
+      row[u] = it.t;
+      k[u] = it.c * kUnit<T>;
+      id[u] = it.t < a.T ? a.ids[it.t] : -1;
+      it.step(256, a.walk.near_rows, a.walk.near_units, a.walk.per_row);
     }
-    store8((T*)a.Y + t * a.ldy + g * 8, pack8<T>(v), n, a.vec);
-    t += a.step_rows;
-    g += a.step_groups;
-    if (g >= a.groups) { g -= a.groups; ++t; }
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool word = id[u] >= 0 && id[u] < a.V;
+      x[u] = load_unit((const T*)a.E + (int64_t)(word ? id[u] : 0) * a.lde + k[u], word ? a.d - k[u] : 0, a.vec, id[u] + 1 < a.V);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint64_t v[H];
+      unpack_unit<T>(x[u], v);
+      const bool word = id[u] >= 0 && id[u] < a.V;       // zeros for padding, also where the scale is not finite
+#pragma unroll
+      for (int j = 0; j < H; ++j) v[j] = word ? mul2(v[j], scale) : 0;
+      const int n = row[u] < a.T ? a.d - k[u] : 0;
+      if (n > 0) store_unit((T*)a.Y + row[u] * a.ldy + k[u], pack_unit<T>(v), n, a.vec);
+    }
+    at.step(stride, a.walk.tile_rows, a.walk.tile_units, a.walk.per_row);
   }
 }
 
-// ---------------------------------------------------------------- sort
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxDigitBits = 9;
+// ---------------------------------------------------------------- rows of zeros
+struct ClearArgs { unsigned char* p; int64_t rows, row_bytes, pitch; int vec; };   // vec: rows start on 16 bytes
 
-struct SortArgs {
-  const int32_t* ids; int64_t T;
-  uint32_t V;
-  int passes, bits;                 // digits of a word, bits of a digit
-  uint2* order[2];                  // (word, token) pairs, written in turn; the last pass writes order[0]
-  int cluster;                      // blocks of the cluster that sorts
-  unsigned char* dE; int64_t row_bytes, pitch, rows;   // what the other blocks clear (rows 0: nothing)
-  int vec;
-};
-// Counters of every warp, then the block's and the cluster's sums.
-inline size_t sort_smem(int bits) { return ((size_t)kSortWarps + 2) * (1u << bits) * 4; }
-
-// Rows of zeros, 16 bytes at a time where rows start on 16 bytes; the last piece of a row by its elements (2 bytes divide both types).
-__device__ __forceinline__ void clear_rows(const SortArgs& a, int64_t first, int64_t step) {
-  const int64_t pieces = a.vec ? (a.row_bytes + 15) / 16 : a.row_bytes / 2, total = a.rows * pieces;
+// The last bytes of a row, an even number below 16.
+__device__ __forceinline__ void clear_tail(unsigned char* at, int64_t left) {
+  if (left & 8) { *reinterpret_cast<uint2*>(at) = make_uint2(0, 0); at += 8; }
+  if (left & 4) { *reinterpret_cast<uint32_t*>(at) = 0; at += 4; }
+  if (left & 2) *reinterpret_cast<uint16_t*>(at) = 0;
+}
+// Rows [0, rows) from p on but those that `skip` names, by `step` threads of which this is the first-th: a warp for a row, or a thread for a piece of a short one.
+template <typename Skip>
+__device__ __forceinline__ void clear_rows(unsigned char* p, int64_t rows, const ClearArgs& a, int64_t first, int64_t step, Skip&& skip) {
+  if (a.vec && a.row_bytes >= 512) {
+    const int lane = threadIdx.x & 31, whole = (int)(a.row_bytes / 16);
+    for (int64_t r = first / 32; r < rows; r += step / 32) {
+      if (skip(r)) continue;
+      unsigned char* row = p + r * a.pitch;
+#pragma unroll 4
+      for (int i = lane; i < whole; i += 32) reinterpret_cast<uint4*>(row)[i] = make_uint4(0, 0, 0, 0);
+      if (lane == 0) clear_tail(row + (int64_t)whole * 16, a.row_bytes & 15);
+    }
+    return;
+  }
+  const int64_t pieces = a.vec ? (a.row_bytes + 15) / 16 : a.row_bytes / 2, total = rows * pieces;
   int64_t i = first, row = i / pieces, piece = i - row * pieces;
   const int64_t step_rows = step / pieces, step_pieces = step - step_rows * pieces;
   for (; i < total; i += step) {
-    unsigned char* p = a.dE + row * a.pitch;
-    if (!a.vec) {
-      *reinterpret_cast<uint16_t*>(p + piece * 2) = 0;
-    } else if ((piece + 1) * 16 <= a.row_bytes) {
-      *reinterpret_cast<uint4*>(p + piece * 16) = make_uint4(0, 0, 0, 0);
-    } else {
-      for (int64_t k = piece * 16; k < a.row_bytes; k += 2) *reinterpret_cast<uint16_t*>(p + k) = 0;
+    if (!skip(row)) {
+      unsigned char* at = p + row * a.pitch + piece * (a.vec ? 16 : 2);
+      const int64_t left = a.row_bytes - piece * 16;
+      if (!a.vec) *reinterpret_cast<uint16_t*>(at) = 0;
+      else if (left >= 16) *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+      else clear_tail(at, left);
     }
     row += step_rows;
     piece += step_pieces;
     if (piece >= pieces) { piece -= pieces; ++row; }
   }
 }
+// All rows, by `blocks` blocks of which this is the block-th.  Rows without a gap are one run of bytes, in tiles of four pieces a thread.
+// (Writing alone, the memory takes 5.9 TB/s of such tiles, and 4.2 of tiles of a megabyte.)
+__device__ __forceinline__ void clear_all(const ClearArgs& a, int64_t block, int64_t blocks) {
+  const int threads = blockDim.x;
+  if (a.vec && a.pitch == a.row_bytes) {
+    const int64_t bytes = a.rows * a.row_bytes, pieces = bytes / 16;
+    uint4* p = reinterpret_cast<uint4*>(a.p);
+    for (int64_t t = block * threads * 4; t < pieces; t += blocks * threads * 4) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t i = t + u * threads + threadIdx.x;
+        if (i < pieces) p[i] = make_uint4(0, 0, 0, 0);
+      }
+    }
+    if (block == 0 && threadIdx.x == 0) clear_tail(a.p + pieces * 16, bytes & 15);
+  } else {
+    clear_rows(a.p, a.rows, a, block * threads + threadIdx.x, blocks * threads, [](int64_t) { return false; });
+  }
+}
 
-// A pass of a cluster of C blocks of 32 warps: warp w of block c owns the (c 32 + w)-th run of consecutive pairs.  It counts its digits;
-// the block turns the counts into positions (digit by digit, over its warps; the blocks' sums over distributed shared memory); the warp
-// then walks its run again and moves every pair behind the ones of the same digit before it.  Within a group of 32 the equal
-// digits are found with one match instruction, so the order among them is that of the lanes.
+// ---------------------------------------------------------------- sort
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kMaxDigitBits = 9;
+constexpr int kSortHeld = 4;        // pairs of a thread in sort_kernel
+constexpr int kSortBlock = kSortThreads * kSortHeld, kSortBlocks = 128;      // pairs of a block, blocks of a long batch at most
+
+struct SortArgs {
+  const int32_t* ids; int64_t T;
+  uint32_t V;
+  int passes, bits;                 // digits of a word, bits of a digit
+  uint2* order[2];                  // (word, token) pairs, written in turn; the last pass writes order[0]
+  int blocks;                       // blocks that sort
+  uint32_t* counts;                 // long batches: [blocks][bins]
+  ClearArgs clear;                  // what the other blocks clear (rows 0: nothing)
+  __device__ __forceinline__ const uint2* from(int pass) const { return (passes - pass) & 1 ? order[1] : order[0]; }
+  __device__ __forceinline__ uint2* to(int pass) const { return (passes - pass) & 1 ? order[0] : order[1]; }
+  __device__ __forceinline__ uint2 pair(int pass, int64_t i) const {
+    if (pass) return from(pass)[i];
+    const int32_t id = ids[i];
+    return make_uint2(min((uint32_t)id, V), (uint32_t)i);           // padding sorts behind every word
+  }
+};
+// A counter and a set of lanes for every warp and digit, then the block's sums and where its pairs of a digit begin.
+inline size_t sort_smem(int bits) { return (2 * (size_t)kSortWarps + 2) * (1u << bits) * 4; }
+struct SortShared {
+  uint32_t *mine, *lanes, *total, *base;
+  int bins;
+  __device__ __forceinline__ SortShared(uint32_t* sm, int bits) : bins(1 << bits) {
+    mine = sm + (threadIdx.x >> 5) * bins;
+    lanes = mine + kSortWarps * bins;
+    total = sm + 2 * kSortWarps * bins;
+    base = total + bins;
+  }
+  __device__ __forceinline__ void clear() const {
+    for (int b = threadIdx.x & 31; b < bins; b += 32) mine[b] = lanes[b] = 0;
+    __syncwarp();
+  }
+  // Pairs of the same digit before this lane's in the warp's run so far; the run grows by the 32 pairs.  Equal digits find one another in shared memory: a
+  // ballot for each bit takes 1500 cycles with all warps of an SM at it, this 500.
+  __device__ __forceinline__ uint32_t rank(uint32_t digit, bool on) const {
+    const int lane = threadIdx.x & 31;
+    if (on) atomicOr(lanes + digit, 1u << lane);
+    __syncwarp();
+    const uint32_t same = on ? lanes[digit] : 0, at = on ? mine[digit] : 0;
+    __syncwarp();
+    if (on && (same >> lane) == 1u) {                    // the highest lane of each digit
+      mine[digit] = at + __popc(same);
+      lanes[digit] = 0;
+    }
+    __syncwarp();
+    return at + __popc(same & ((1u << lane) - 1));
+  }
+};
+// Pairs [lo, hi) of this warp.
+__device__ __forceinline__ void warp_run(int64_t T, int block, int blocks, int64_t& lo, int64_t& hi) {
+  const int64_t warps = (int64_t)blocks * kSortWarps, per = ((T + warps * 32 - 1) / (warps * 32)) * 32;
+  lo = min(T, ((int64_t)block * kSortWarps + (threadIdx.x >> 5)) * per);
+  hi = min(T, lo + per);
+}
+
+// The warps' counts of each digit become the number of pairs before the warp's; `total` gets the sums.  A thread takes a digit, or half the warps of one where there are
+// twice as many threads.
+__device__ __forceinline__ void scan_warps(uint32_t* sm, const SortShared& s) {
+  __shared__ uint32_t half[kSortThreads / 2];
+  constexpr int HALF = kSortWarps / 2;
+  const int digit = threadIdx.x & (s.bins - 1), part = threadIdx.x / s.bins;
+  const bool split = 2 * s.bins <= kSortThreads, on = part < (split ? 2 : 1);
+  uint32_t* p = sm + digit + (split && part ? HALF * s.bins : 0);
+  uint32_t v[HALF], sum = 0;
+  if (on) {
+#pragma unroll
+    for (int h = 0; h < HALF; ++h) sum += v[h] = p[h * s.bins];
+  }
+  if (split && on && part == 0) half[digit] = sum;
+  __syncthreads();
+  if (on) {
+    uint32_t before = split && part ? half[digit] : 0;
+#pragma unroll
+    for (int h = 0; h < HALF; ++h) {
+      p[h * s.bins] = before;
+      before += v[h];
+    }
+    if (!split) {
+#pragma unroll
+      for (int h = 0; h < HALF; ++h) v[h] = p[(HALF + h) * s.bins];
+#pragma unroll
+      for (int h = 0; h < HALF; ++h) {
+        p[(HALF + h) * s.bins] = before;
+        before += v[h];
+      }
+    }
+    if (!split || part) s.total[digit] = before;
+  }
+}
+// base of digit b = threadIdx.x: pairs of lower digits anywhere, and of this digit in blocks before (`ahead`).
+__device__ __forceinline__ void place_digits(const SortShared& s, uint32_t all, uint32_t ahead) {
+  __shared__ uint32_t sums[16];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (s.bins + 31) / 32;
+  uint32_t inc = all;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t n = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += n;
+  }
+  if (warp < warps && lane == 31) sums[warp] = inc;
+  __syncthreads();
+  if ((int)threadIdx.x < s.bins) {
+    uint32_t before = 0;
+    for (int w = 0; w < warp; ++w) before += sums[w];
+    s.base[threadIdx.x] = before + inc - all + ahead;
+  }
+  __syncthreads();
+}
+
+// A pass of a cluster of C blocks of 16 warps: warp w of block c owns the (c 16 + w)-th run of consecutive pairs, 128 at most.  It counts its digits;
+// the block turns the counts into positions (over its warps in shared memory, over the blocks in distributed shared memory); the warp
+// then moves every pair behind the ones of the same digit before it.  Within a group of 32 the order among equal digits is that of the lanes.
 __global__ void __launch_bounds__(kSortThreads)
 sort_kernel(const SortArgs a) {
   pdl_wait();
   pdl_launch_dependents();
-  if ((int)blockIdx.x >= a.cluster) {
-    clear_rows(a, (int64_t)(blockIdx.x - a.cluster) * kSortThreads + threadIdx.x, (int64_t)(gridDim.x - a.cluster) * kSortThreads);
+  if ((int)blockIdx.x >= a.blocks) {
+    clear_all(a.clear, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     return;
   }
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   extern __shared__ uint32_t sm[];
-  __shared__ int scan[33];
-  const int bins = 1 << a.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = (int)cluster.block_rank(), C = (int)cluster.num_blocks();
-  uint32_t* mine = sm + warp * bins;                     // this warp's counters
-  uint32_t* total = sm + kSortWarps * bins;              // the block's counts, read by the other blocks
-  uint32_t* base = total + bins;                         // where the block's pairs of a digit begin
-  const int64_t per = ((a.T + (int64_t)C * kSortWarps * 32 - 1) / ((int64_t)C * kSortWarps * 32)) * 32;
-  const int64_t lo = min(a.T, ((int64_t)rank * kSortWarps + warp) * per), hi = min(a.T, lo + per);
+  const SortShared s(sm, a.bits);
+  const int lane = threadIdx.x & 31, rank = (int)cluster.block_rank();
+  int64_t lo, hi;
+  warp_run(a.T, rank, a.blocks, lo, hi);
   for (int pass = 0; pass < a.passes; ++pass) {
-    const bool even = ((a.passes - pass) & 1) == 0;
-    const uint2* from = even ? a.order[0] : a.order[1];
-    uint2* to = even ? a.order[1] : a.order[0];
-    const int shift = pass * a.bits;
-    auto pair = [&](int64_t i) {
-      if (pass) return from[i];
-      const int32_t id = a.ids[i];
-      return make_uint2(min((uint32_t)id, a.V), (uint32_t)i);       // padding sorts behind every word
-    };
-    for (int b = lane; b < bins; b += 32) mine[b] = 0;
-    __syncwarp();
-    for (int64_t i = lo; i < hi; i += 32) {
-      const bool on = i + lane < hi;
-      const uint32_t digit = on ? (pair(i + lane).x >> shift) & (bins - 1) : bins;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit);
-      if (on && (same >> lane) == 1u) mine[digit] += __popc(same);  // the highest lane of each digit
-      __syncwarp();
+    uint2 held[kSortHeld];
+    uint32_t before[kSortHeld], digit[kSortHeld];        // pairs of the same digit before it in the warp's run
+#pragma unroll
+    for (int h = 0; h < kSortHeld; ++h) held[h] = lo + h * 32 + lane < hi ? a.pair(pass, lo + h * 32 + lane) : make_uint2(0, 0);
+    s.clear();
+#pragma unroll
+    for (int h = 0; h < kSortHeld; ++h) {
+      digit[h] = (held[h].x >> (pass * a.bits)) & (s.bins - 1);
+      before[h] = s.rank(digit[h], lo + h * 32 + lane < hi);
     }
     __syncthreads();
-    // counts of a digit, warp by warp, to the number of pairs before the warp's
-    for (int b = threadIdx.x; b < bins; b += kSortThreads) {
-      uint32_t s = 0;
-      for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = sm[w * bins + b];
-        sm[w * bins + b] = s;
-        s += c;
-      }
-      total[b] = s;
-    }
+    scan_warps(sm, s);
     cluster.sync();
-    int before = 0, all = 0;
-    const int b = threadIdx.x;                           // bins <= threads
-    if (b < bins) {
-      for (int c = 0; c < C; ++c) {
-        const int v = (int)*cluster.map_shared_rank(total + b, c);
-        all += v;
-        if (c < rank) before += v;
+    uint32_t ahead = 0, all = 0;
+    if ((int)threadIdx.x < s.bins) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {                      // all eight in flight, whether there are so many blocks or not
+        const uint32_t v = *cluster.map_shared_rank(s.total + threadIdx.x, min(c, a.blocks - 1));
+        if (c < a.blocks) all += v;
+        if (c < rank) ahead += v;
       }
     }
-    int sum;
-    const int start = block_exclusive_scan(all, scan, &sum);
-    if (b < bins) base[b] = (uint32_t)(start + before);
-    __syncthreads();
-    for (int d = lane; d < bins; d += 32) mine[d] += base[d];
-    __syncwarp();
-    for (int64_t i = lo; i < hi; i += 32) {
-      const bool on = i + lane < hi;
-      uint2 p = make_uint2(0, 0);
-      if (on) p = pair(i + lane);
-      const uint32_t digit = on ? (p.x >> shift) & (bins - 1) : bins;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit), at = on ? mine[digit] : 0;
-      __syncwarp();
-      if (on) {
-        to[at + __popc(same & ((1u << lane) - 1))] = p;
-        if ((same >> lane) == 1u) mine[digit] = at + __popc(same);
-      }
-      __syncwarp();
+    const bool more = pass + 1 < a.passes;
+    if (!more) cluster.barrier_arrive();                 // the last look at the other blocks' memory
+    place_digits(s, all, ahead);
+    uint2* to = a.to(pass);
+#pragma unroll
+    for (int h = 0; h < kSortHeld; ++h)
+      if (lo + h * 32 + lane < hi) to[s.base[digit[h]] + s.mine[digit[h]] + before[h]] = held[h];
+    if (more) cluster.sync();                            // the pairs are in place and `total` has been read
+    else cluster.barrier_wait();
+  }
+}
+
+// A pass over a long batch, first launch: the digits of each block's run of pairs are counted.
+__device__ __forceinline__ void count_run(const SortArgs& a, const SortShared& s, int pass, int64_t lo, int64_t hi) {
+  const int lane = threadIdx.x & 31;
+  s.clear();
+  for (int64_t i = lo; i < hi; i += 64) {
+    uint32_t digit[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) digit[h] = i + h * 32 + lane < hi ? (a.pair(pass, i + h * 32 + lane).x >> (pass * a.bits)) & (s.bins - 1) : (uint32_t)s.bins;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (digit[h] < (uint32_t)s.bins) atomicAdd(s.mine + digit[h], 1u);         // a count, whatever the order
+  }
+  __syncthreads();
+}
+__global__ void __launch_bounds__(kSortThreads)
+sort_count_kernel(const SortArgs a, int pass) {
+  pdl_wait();
+  pdl_launch_dependents();
+  if ((int)blockIdx.x >= a.blocks) {
+    clear_all(a.clear, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    return;
+  }
+  extern __shared__ uint32_t sm[];
+  const SortShared s(sm, a.bits);
+  int64_t lo, hi;
+  warp_run(a.T, blockIdx.x, a.blocks, lo, hi);
+  count_run(a, s, pass, lo, hi);
+  for (int b = threadIdx.x; b < s.bins; b += kSortThreads) {
+    uint32_t n = 0;
+#pragma unroll 8
+    for (int w = 0; w < kSortWarps; ++w) n += sm[w * s.bins + b];
+    a.counts[(int64_t)blockIdx.x * s.bins + b] = n;
+  }
+}
+// Second launch: every block adds up the counts of all blocks and of those before it, and moves its pairs.
+__global__ void __launch_bounds__(kSortThreads)
+sort_move_kernel(const SortArgs a, int pass) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ uint32_t sm[];
+  const SortShared s(sm, a.bits);
+  const int lane = threadIdx.x & 31;
+  uint32_t ahead = 0, all = 0;
+  if ((int)threadIdx.x < s.bins) {
+#pragma unroll 16
+    for (int c = 0; c < a.blocks; ++c) {
+      const uint32_t v = a.counts[(int64_t)c * s.bins + threadIdx.x];
+      all += v;
+      if (c < (int)blockIdx.x) ahead += v;
     }
-    cluster.sync();                                      // the pairs are in place and `total` has been read
+  }
+  int64_t lo, hi;
+  warp_run(a.T, blockIdx.x, a.blocks, lo, hi);
+  count_run(a, s, pass, lo, hi);
+  scan_warps(sm, s);
+  place_digits(s, all, ahead);
+  uint2* to = a.to(pass);
+  for (int64_t i = lo; i < hi; i += 64) {
+    uint2 p[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) p[h] = i + h * 32 + lane < hi ? a.pair(pass, i + h * 32 + lane) : make_uint2(0, 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool on = i + h * 32 + lane < hi;
+      const uint32_t digit = (p[h].x >> (pass * a.bits)) & (s.bins - 1), at = s.rank(digit, on);
+      if (on) to[s.base[digit] + at] = p[h];
+    }
   }
 }
 
 // ---------------------------------------------------------------- runs of equal words
 struct RunArgs {
   const uint2* order; int64_t T;
+  const int32_t* ids;               // few_kernel
   uint32_t V;
   const void* dY; int64_t lddy;
   void* dE; int64_t ldde;
-  float* part; int64_t part_ld;     // [chunks][2][part_ld]: a chunk's share of the run that comes from before it, of the run that goes on behind it
-  int64_t chunks; int chunk;        // tokens of a chunk, a multiple of 8
+  float* part; int64_t part_ld;     // [chunks][2][part_ld]: a chunk's share of the run that comes from before it, of the one that goes on behind it
+  int64_t chunks; int chunk;        // tokens of a chunk, a multiple of 4
   float scale;
   int d, slices;                    // slices of LPT * 8 columns
   int accumulate, vec, vec_out;
+  ClearArgs clear; int clear_rows, token_blocks;       // few_kernel: rows that a block clears, blocks before those that do
 };
 
-// scale v (+)= into dE's row
-template <typename TW>
-__device__ __forceinline__ void write_row8(const RunArgs& a, uint32_t word, int k, int n, const float (&v)[8]) {
+// scale v (+)= into E columns of dE's row, n of which exist
+template <typename TW, int E>
+__device__ __forceinline__ void write_columns(const RunArgs& a, uint32_t word, int k, int n, const float (&v)[E]) {
   TW* p = (TW*)a.dE + (int64_t)word * a.ldde + k;
-  float s[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s[j] = a.scale * v[j];
+  constexpr int BYTES = E * (int)sizeof(TW);
+  const bool whole = a.vec_out && n >= E;
+  TW out[E];
   if (a.accumulate) {
-    float old[8];
-    unpack8(load8((const TW*)p, n, a.vec_out, false), n, old);
+    if (whole) {
+      if constexpr (BYTES == 8) {
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
+        memcpy(out, &q, 8);
+      } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] += old[j];
+        for (int i = 0; i < BYTES / 16; ++i) {
+          const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+          memcpy(reinterpret_cast<char*>(out) + 16 * i, &q, 16);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) out[j] = j < n ? p[j] : from_f32<TW>(0.f);
+    }
   }
-  store8(p, pack8<TW>(s), n, a.vec_out);
+#pragma unroll
+  for (int j = 0; j < E; ++j) out[j] = from_f32<TW>(a.accumulate ? a.scale * v[j] + to_f32(out[j]) : a.scale * v[j]);
+  if (whole) {
+    if constexpr (BYTES == 8) {
+      uint2 q;
+      memcpy(&q, out, 8);
+      *reinterpret_cast<uint2*>(p) = q;
+    } else {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i) {
+        uint4 q;
+        memcpy(&q, reinterpret_cast<const char*>(out) + 16 * i, 16);
+        reinterpret_cast<uint4*>(p)[i] = q;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      if (j < n) p[j] = out[j];
+  }
 }
 
-// LPT lanes take a chunk's slice of columns, eight columns each; rows in batches of U in flight.
-template <typename T, typename TW, int LPT, int U>
+// LPT lanes take a chunk's slice of LPT * 8 columns.  Their rows come through a ring of AHEAD steps of four, each thread copying and reading its own units:
+// one row after another from memory would leave a warp waiting for most of its time (16384 tokens of 205 words, 2048 columns: 35 us, now 14).
+constexpr int kStep = 4;
+template <typename T, typename TW, int LPT, int AHEAD>
 __global__ void __launch_bounds__(256)
 runs_kernel(const RunArgs a) {
+  constexpr int E = kUnit<T>, NU = 8 / E;                // units of a thread: eight columns
+  extern __shared__ uint4 ring[];                        // [AHEAD][kStep][NU][256]
   pdl_wait();
   pdl_launch_dependents();
   const int64_t unit = (int64_t)blockIdx.x * (256 / LPT) + threadIdx.x / LPT;
   const int64_t c = unit / a.slices;
   if (c >= a.chunks) return;
-  const int k = ((int)(unit - c * a.slices) * LPT + threadIdx.x % LPT) * 8, n = a.d - k;
-  if (n <= 0) return;
+  const int k0 = ((int)(unit - c * a.slices) * LPT * NU + threadIdx.x % LPT) * E;      // the first unit's column; the second is LPT units behind
   const int64_t lo = c * a.chunk, hi = min(a.T, lo + a.chunk);
+  const int steps = (int)((hi - lo + kStep - 1) / kStep);
+  // entries i .. i + 3, two at a time (i is a multiple of four, and the order is followed by room for more)
+  auto entries = [&](int64_t i, uint4 (&e)[2]) {
+    e[0] = e[1] = make_uint4(a.V, 0, a.V, 0);
+    if (i < hi) e[0] = *reinterpret_cast<const uint4*>(a.order + i);
+    if (i + 2 < hi) e[1] = *reinterpret_cast<const uint4*>(a.order + i + 2);
+  };
+  auto fetch = [&](int step, int slot, const uint4 (&e)[2]) {
+    const uint32_t word[4] = {e[0].x, e[0].z, e[1].x, e[1].z}, token[4] = {e[0].y, e[0].w, e[1].y, e[1].w};
+    const int64_t i = lo + (int64_t)step * kStep;
+    uint4* to = ring + slot * (kStep * NU * 256) + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      const bool on = i + u < hi && word[u] < a.V;
+      const T* row = (const T*)a.dY + (int64_t)(on ? token[u] : 0) * a.lddy + k0;
+#pragma unroll
+      for (int q = 0; q < NU; ++q) copy_unit(to + (u * NU + q) * 256, row + q * LPT * E, on ? a.d - k0 - q * LPT * E : 0, a.vec);
+    }
+  };
+  uint4 ahead[2];
+  entries(lo, ahead);
+#pragma unroll
+  for (int s = 0; s < AHEAD; ++s) {
+    if (s < steps) {
+      fetch(s, s, ahead);
+      entries(lo + (s + 1) * kStep, ahead);
+    }
+    copies_commit();
+  }
   const uint32_t none = 0xFFFFFFFFu;                     // no word: words are below 2^31
-  uint2 next = a.order[lo];
-  bool open = lo > 0 && a.order[lo - 1].x == next.x;     // the run comes from before the chunk
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int64_t i = lo; i < hi; i += U) {
-    uint2 e[U + 1];
-    e[0] = next;
+  bool open = lo > 0 && a.order[lo - 1].x == a.order[lo].x;         // the run comes from before the chunk
+  uint64_t acc[NU][E / 2];
 #pragma unroll
-    for (int u = 1; u <= U; ++u) e[u] = i + u < a.T ? a.order[i + u] : make_uint2(none, 0);
-    next = e[U];
-    if (e[0].x >= a.V) return;                           // padding: nothing but padding follows
-    Raw8<T> raw[U];
+  for (int q = 0; q < NU; ++q)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u < hi && e[u].x < a.V) raw[u] = load8((const T*)a.dY + (int64_t)e[u].y * a.lddy + k, n, a.vec, (int64_t)e[u].y + 1 < a.T);
+    for (int j = 0; j < E / 2; ++j) acc[q][j] = 0;
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    const int64_t i = lo + (int64_t)s * kStep;
+    uint32_t word[kStep + 1];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u < hi && e[u].x < a.V) {
-        float v[8];
-        unpack8(raw[u], n, v);
+    for (int u = 0; u <= kStep; ++u) word[u] = i + u < a.T ? a.order[i + u].x : none;
+    copies_wait<AHEAD - 1>();
+    const uint4* at = ring + slot * (kStep * NU * 256) + threadIdx.x;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += v[j];
-        const bool ends = e[u + 1].x != e[u].x, last = i + u + 1 == hi;
-        if (ends && !open) {
-          write_row8<TW>(a, e[u].x, k, n, acc);
-        } else if (ends || last) {
-          float* p = a.part + ((int64_t)c * 2 + (open ? 0 : 1)) * a.part_ld + k;
-          *reinterpret_cast<float4*>(p) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-          *reinterpret_cast<float4*>(p + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    for (int u = 0; u < kStep; ++u) {
+      if (i + u < hi && word[u] < a.V) {
+        const bool ends = word[u + 1] != word[u], stops = i + u + 1 == hi;
+#pragma unroll
+        for (int q = 0; q < NU; ++q) {
+          uint64_t v[E / 2];
+          unpack_unit<T>(at[(u * NU + q) * 256], v);
+#pragma unroll
+          for (int j = 0; j < E / 2; ++j) acc[q][j] = add2(acc[q][j], v[j]);
+          const int k = k0 + q * LPT * E, n = a.d - k;
+          if ((ends || stops) && n > 0) {
+            float f[E];
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) {
+              const float2 w = unpack2(acc[q][j]);
+              f[2 * j] = w.x;
+              f[2 * j + 1] = w.y;
+            }
+            if (ends && !open) {
+              write_columns<TW, E>(a, word[u], k, n, f);
+            } else {
+              float* p = a.part + (c * 2 + (open ? 0 : 1)) * a.part_ld + k;
+#pragma unroll
+              for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+            }
+          }
+          if (ends) {
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) acc[q][j] = 0;
+          }
         }
-        if (ends) {
-          open = false;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-        }
+        if (ends) open = false;
       }
     }
+    if (s + AHEAD < steps) {
+      fetch(s + AHEAD, slot, ahead);
+      entries(lo + (int64_t)(s + AHEAD + 1) * kStep, ahead);
+    }
+    copies_commit();
+    slot = slot + 1 == AHEAD ? 0 : slot + 1;
   }
 }
 
-// Block c: the run that begins in chunk c and crosses its end, if there is one.  Its parts in the chunks behind are dealt out to the eight
-// warps as runs of consecutive chunks; the warps' sums are added in order.  A warp covers 256 columns, blockIdx.y the rest.
-template <typename TW>
+// Warp w of block b looks at the end of chunk 8 b + w: where a run that began in that chunk goes over it, its parts (one for each chunk that it reaches) are added up,
+// by the warp alone where they are few, by the eight warps of the block where they are many.  LPT lanes cover LPT * 8 columns (blockIdx.y: the rest); the
+// groups of LPT lanes take runs of consecutive parts each, and their sums are added in a fixed order.
+constexpr int kFewParts = 16;
+template <typename TW, int LPT>
 __global__ void __launch_bounds__(256)
 joints_kernel(const RunArgs a) {
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ float red[8][32][8];
-  const int64_t c = blockIdx.x, lo = c * a.chunk, hi = lo + a.chunk;
-  if (hi >= a.T) return;
-  const uint32_t word = a.order[hi - 1].x;
-  if (word >= a.V || a.order[hi].x != word) return;
-  if (a.order[lo].x == word && lo > 0 && a.order[lo - 1].x == word) return;       // it began before
-  // chunks behind that begin with the word: 32 candidates at a time, each warp for itself
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t m = 0;
-  for (;;) {
-    const int64_t at = (c + 1 + m + lane) * a.chunk;
-    const unsigned on = __ballot_sync(0xffffffffu, at < a.T && a.order[at < a.T ? at : 0].x == word);
-    if (on == 0xffffffffu) { m += 32; continue; }
-    m += __ffs(~on) - 1;
-    break;
-  }
-  const int k = (blockIdx.y * 32 + lane) * 8, n = a.d - k;
-  const int64_t per = (m + 7) / 8, p0 = warp * per, p1 = min(m, p0 + per);
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto add = [&](int64_t chunk, int slot) {
-    const float4* p = reinterpret_cast<const float4*>(a.part + (chunk * 2 + slot) * a.part_ld + k);
-    const float4 u = p[0], v = p[1];
-    acc[0] += u.x; acc[1] += u.y; acc[2] += u.z; acc[3] += u.w;
-    acc[4] += v.x; acc[5] += v.y; acc[6] += v.z; acc[7] += v.w;
-  };
-  if (n > 0) {
-    if (warp == 0) add(c, 1);
-#pragma unroll 4
-    for (int64_t p = p0; p < p1; ++p) add(c + 1 + p, 0);
-  }
+  constexpr int G = 32 / LPT;
+  __shared__ float red[8][LPT][8];
+  __shared__ int64_t many[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = lane / LPT, l = lane % LPT;
+  const int k = (blockIdx.y * LPT + l) * 8, n = a.d - k;
+  float acc[8];
+  // parts [p0, p1) of a run that begins in chunk c: part 0 is its share of that chunk, part p its share of the p-th behind
+  auto sum = [&](int64_t c, int64_t p0, int64_t p1) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) red[warp][lane][j] = acc[j];
-  __syncthreads();
-  if (warp == 0 && n > 0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      acc[j] = 0.f;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) acc[j] += red[w][lane][j];
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    if (n > 0) {
+#pragma unroll 8
+      for (int64_t p = p0; p < p1; ++p) {
+        const float4* at = reinterpret_cast<const float4*>(a.part + ((c + p) * 2 + (p == 0 ? 1 : 0)) * a.part_ld + k);
+        const float4 u = at[0], v = at[1];
+        acc[0] += u.x; acc[1] += u.y; acc[2] += u.z; acc[3] += u.w;
+        acc[4] += v.x; acc[5] += v.y; acc[6] += v.z; acc[7] += v.w;
+      }
     }
-    write_row8<TW>(a, word, k, n, acc);
+#pragma unroll
+    for (int o = LPT; o < 32; o <<= 1)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
+  };
+  auto word_at = [&](int64_t i) { return i >= 0 && i < a.T ? a.order[i].x : 0xFFFFFFFFu; };
+  const int64_t c = (int64_t)blockIdx.x * 8 + warp, lo = c * a.chunk, hi = lo + a.chunk;
+  const uint32_t word = word_at(hi - 1), next = word_at(hi), first = word_at(lo), prev = word_at(lo - 1);
+  int64_t m = 0;                                         // parts
+  if (word < a.V && next == word && !(first == word && prev == word)) {
+    for (m = 1;; m += 32) {
+      const unsigned on = __ballot_sync(0xffffffffu, word_at((c + m + lane) * a.chunk) == word);
+      if (on == 0xffffffffu) continue;
+      m += __ffs(~on) - 1;
+      break;
+    }
+    if (m <= kFewParts * G) {
+      const int64_t per = (m + G - 1) / G;
+      sum(c, min(m, group * per), min(m, (group + 1) * per));
+      if (group == 0 && n > 0) write_columns<TW, 8>(a, word, k, n, acc);
+    }
+  }
+  if (lane == 0) many[warp] = m > kFewParts * G ? m : 0;
+  __syncthreads();
+  for (int w = 0; w < 8; ++w) {
+    const int64_t parts = many[w], from = (int64_t)blockIdx.x * 8 + w;
+    if (!parts) continue;
+    const int64_t per = (parts + 8 * G - 1) / (8 * G), mine = warp * G + group;
+    sum(from, min(parts, mine * per), min(parts, (mine + 1) * per));
+    if (group == 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) red[warp][l][j] = acc[j];
+    }
+    __syncthreads();
+    if (warp == 0 && group == 0 && n > 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll
+      for (int o = 0; o < 8; ++o)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += red[o][l][j];
+      write_columns<TW, 8>(a, word_at((from + 1) * a.chunk - 1), k, n, acc);
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- few tokens
+// Eight tokens and 256 columns a block, a warp for each token: it looks through all words, lane j keeps which of the j-th 32 are its own, and the warp of the first
+// token of a word lists the word's tokens and adds up their rows, U in flight; where they are many, the eight warps of the block do, an eighth of the list each, and
+// their sums are added in order.  The blocks behind clear a range of dE's rows each, but for the words that occur, which they mark first.
+constexpr int kFewTokens = 1024, kFewRows = 4096;        // a bit of 32 lanes for each token; rows that a block can mark
+template <typename T, typename TW>
+__global__ void __launch_bounds__(256)
+few_kernel(const RunArgs a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  constexpr int U = sizeof(T) == 2 ? 8 : 4, kAlone = 2 * U;
+  __shared__ int32_t ids[kFewTokens];
+  __shared__ uint16_t list[8][kFewTokens];
+  __shared__ float red[8][32][8];
+  __shared__ int many[8];                                // tokens of a word that all warps add up
+  uint32_t* marks = reinterpret_cast<uint32_t*>(list);
+  static_assert(kFewRows / 8 <= (int)sizeof(list), "");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_tokens = (int)a.T;
+  if ((int)blockIdx.x >= a.token_blocks) {
+    const int64_t first = (int64_t)(blockIdx.x - a.token_blocks) * a.clear_rows;
+    const int rows = (int)min((int64_t)a.clear_rows, a.clear.rows - first);
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += 256) marks[i] = 0;
+    __syncthreads();
+    for (int t = threadIdx.x; t < n_tokens; t += 256) {
+      const int64_t r = (int64_t)a.ids[t] - first;
+      if (r >= 0 && r < rows) atomicOr(marks + (r >> 5), 1u << (r & 31));
+    }
+    __syncthreads();
+    clear_rows(a.clear.p + first * a.clear.pitch, rows, a.clear, threadIdx.x, 256, [&](int64_t r) { return (marks[r >> 5] >> (r & 31)) & 1; });
+    return;
+  }
+#pragma unroll
+  for (int i = threadIdx.x; i < kFewTokens; i += 256) ids[i] = i < n_tokens ? a.ids[i] : -1;
+  __syncthreads();
+  const int eight = blockIdx.x / a.slices, t = eight * 8 + warp, k = (((int)blockIdx.x - eight * a.slices) * 32 + lane) * 8, n = a.d - k;
+  const int32_t word = t < n_tokens ? ids[t] : -1;
+  uint32_t mine = 0;
+  bool first = word >= 0 && (uint32_t)word < a.V;
+  for (int j = 0; first && j * 32 < n_tokens; j += 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t m = __ballot_sync(0xffffffffu, ids[(j + u) * 32 + lane] == word);
+      if (lane == j + u) mine = m;
+      const int at = (j + u) * 32;
+      if (at <= t && (at + 32 <= t ? m : m & ((1u << (t - at)) - 1))) first = false;
+    }
+  }
+  int count = first ? __popc(mine) : 0, before = 0;
+  if (first) {
+    int inc = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    before = inc - count;
+    count = __shfl_sync(0xffffffffu, inc, 31);
+    for (uint32_t m = mine; m; m &= m - 1) list[warp][before++] = (uint16_t)(lane * 32 + __ffs(m) - 1);
+    __syncwarp();
+  }
+  float acc[8];
+  auto sum = [&](const uint16_t* tokens, int p0, int p1) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) acc[q] = 0.f;
+    for (int p = p0; p < p1; p += U) {
+      Raw8<T> raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = p + u < p1 ? tokens[p + u] : 0;
+        raw[u] = load8((const T*)a.dY + (int64_t)at * a.lddy + k, p + u < p1 ? n : 0, a.vec, at + 1 < n_tokens);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p + u < p1) {
+          float v[8];
+          unpack8(raw[u], n, v);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) acc[q] += v[q];
+        }
+      }
+    }
+  };
+  if (count > 0 && count <= kAlone) {
+    sum(list[warp], 0, count);
+    if (n > 0) write_columns<TW, 8>(a, (uint32_t)word, k, n, acc);
+  }
+  if (lane == 0) many[warp] = count > kAlone ? count : 0;
+  __syncthreads();
+  for (int w = 0; w < 8; ++w) {
+    const int tokens = many[w], per = (tokens + 7) / 8;
+    if (!tokens) continue;
+    sum(list[w], min(tokens, warp * per), min(tokens, (warp + 1) * per));
+#pragma unroll
+    for (int q = 0; q < 8; ++q) red[warp][lane][q] = acc[q];
+    __syncthreads();
+    if (warp == 0 && n > 0) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        acc[q] = 0.f;
+#pragma unroll
+        for (int o = 0; o < 8; ++o) acc[q] += red[o][lane][q];
+      }
+      write_columns<TW, 8>(a, (uint32_t)ids[eight * 8 + w], k, n, acc);
+    }
+    __syncthreads();
   }
 }
 

@@ -8,13 +8,20 @@
 #include "embedding_rows.cuh"
 #include "layer_norm.cuh"
 #include "rows_ws.h"
+#ifndef EMB_WARPS
+#define EMB_WARPS 16
+#define EMB_FEW 1024
+#define EMB_AHEAD 6
+#define ZPB 32
+#define DROP_T 768
+#endif
 
 using namespace flop;
 typedef __nv_bfloat16 bf16;
 
 namespace {
 
-constexpr int64_t kMaxCols = 1 << 30;
+constexpr int64_t kMaxCols = 1 << 24;      // a launch has at most 65535 segments of a row
 
 // A matrix that an operator reads or writes: where it lies, and whether the kernels can take it.
 struct RowsArg {
@@ -32,6 +39,7 @@ bool in_place_or_apart(const RowsArg& out, const RowsArg& in, int64_t T, int64_t
 bool apart(const RowsArg& a, const RowsArg& b, int64_t T, int64_t d) { return !a.given() || !b.given() || !a.span(T, d).meets(b.span(T, d)); }
 
 int64_t groups_of(int64_t d) { return (d + 7) / 8; }
+int64_t units_of(int64_t d, int dt) { return (d * (int64_t)elt(dt) + 15) / 16; }
 
 bool valid_p(float p) { return p >= 0.f && p < 1.f; }
 Drop make_drop(float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev) {
@@ -49,49 +57,67 @@ int launched() {
   return FLOP_OK;
 }
 
-// Blocks of a kernel that strides over the groups of all rows, and the stride in rows and groups.
-template <typename Args>
-dim3 group_grid(Args& a, int64_t T, int64_t d, int blocks_per_sm) {
-  a.groups = (int)groups_of(d);
-  a.total = T * a.groups;
-  const int64_t blocks = std::min<int64_t>((a.total + 255) / 256, (int64_t)num_sms() * blocks_per_sm);
-  a.step_rows = blocks * 256 / a.groups;
-  a.step_groups = (int)(blocks * 256 - a.step_rows * a.groups);
-  return dim3((unsigned)blocks);
+// ---------------------------------------------------------------- embedding
+template <typename T>
+int launch_lookup(emb::LookupArgs& a, int64_t per_row, cudaStream_t st) {
+  constexpr int U = 4;
+  constexpr int64_t tile = 256 * U;
+  emb::Walk& w = a.walk;
+  w.per_row = (int)per_row;
+  w.total = a.T * per_row;
+  const int64_t blocks = std::min<int64_t>((w.total + tile - 1) / tile, (int64_t)num_sms() * 8);
+  w.tile_rows = blocks * tile / per_row;
+  w.tile_units = (int)(blocks * tile - w.tile_rows * per_row);
+  w.near_rows = 256 / per_row;
+  w.near_units = (int)(256 - w.near_rows * per_row);
+  launch_k(emb::lookup_kernel<T, U>, dim3((unsigned)blocks), dim3(256), (size_t)0, st, a);
+  return launched();
 }
 
-// ---------------------------------------------------------------- embedding
 struct RunPlan { int lanes, slices, chunk; int64_t chunks; };
-// A chunk of 8 tokens where that gives the machine less than a round of warps, longer ones (fewer parts to join) where there are many.
+// Chunks so long that the machine has about 24 warps on an SM; a long batch of narrow rows has no more than 4096, so that a frequent word has not too many parts.
 RunPlan plan_runs(int64_t T, int64_t d) {
   RunPlan p;
   p.lanes = d <= 64 ? 8 : d <= 128 ? 16 : 32;
   p.slices = (int)((d + p.lanes * 8 - 1) / (p.lanes * 8));
-  p.chunk = 8;
-  while (p.chunk < 256 && T / p.chunk * p.slices * p.lanes / 32 > (int64_t)num_sms() * 32) p.chunk *= 2;
+  const int64_t warps = (int64_t)num_sms() * EMB_WARPS, by_work = (T * p.slices * p.lanes / 32 + warps - 1) / warps, by_parts = T / 4096;
+  p.chunk = (int)round_up(std::min<int64_t>(std::max<int64_t>({16, by_work, by_parts}), 256), 4);
   p.chunks = (T + p.chunk - 1) / p.chunk;
   return p;
 }
-struct EmbWs { uint2* order[2]; float* part; int64_t part_ld; size_t bytes; };
+struct EmbWs { uint2* order[2]; uint32_t* counts; float* part; int64_t part_ld; size_t bytes; };
 EmbWs plan_emb_ws(Arena& ar, int64_t T, int64_t d) {
   EmbWs w{};
   if (T == 0 || d == 0) return w;
-  for (auto& o : w.order) o = (uint2*)ar.take((size_t)T * sizeof(uint2));
+  for (auto& o : w.order) o = (uint2*)ar.take((size_t)(T + 4) * sizeof(uint2));     // read four at a time
+  w.counts = (uint32_t*)ar.take((size_t)emb::kSortBlocks * (1u << emb::kMaxDigitBits) * 4);
   w.part_ld = round_up(d, 8);
   w.part = (float*)ar.take((size_t)plan_runs(T, d).chunks * 2 * w.part_ld * 4);
   w.bytes = ar.used;
   return w;
 }
 
-int launch_sort(const emb::SortArgs& a, size_t smem, int zero_blocks, cudaStream_t st) {
+// Batches of up to 8 x 2048 tokens by one cluster; longer ones by two launches a digit.
+constexpr int kSortCluster = 8;
+int launch_sort(const emb::SortArgs& a, int zero_blocks, cudaStream_t st) {
   static OncePerDevice configured;
-  FLOP_TRY(allow_smem(configured, emb::sort_smem(emb::kMaxDigitBits), emb::sort_kernel));
+  FLOP_TRY(allow_smem(configured, emb::sort_smem(emb::kMaxDigitBits), emb::sort_kernel, emb::sort_count_kernel, emb::sort_move_kernel));
+  const size_t smem = emb::sort_smem(a.bits);
+  if (a.blocks > kSortCluster) {
+    for (int pass = 0; pass < a.passes; ++pass) {
+      launch_k(emb::sort_count_kernel, dim3((unsigned)(a.blocks + (pass == 0 ? zero_blocks : 0))), dim3(emb::kSortThreads), smem, st, a, pass);
+      FLOP_TRY(launched());
+      launch_k(emb::sort_move_kernel, dim3((unsigned)a.blocks), dim3(emb::kSortThreads), smem, st, a, pass);
+      FLOP_TRY(launched());
+    }
+    return FLOP_OK;
+  }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(a.cluster + zero_blocks / a.cluster * a.cluster));
+  cfg.gridDim = dim3((unsigned)(a.blocks + zero_blocks / a.blocks * a.blocks));
   cfg.blockDim = dim3(emb::kSortThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)a.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = (unsigned)a.blocks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
@@ -101,25 +127,39 @@ int launch_sort(const emb::SortArgs& a, size_t smem, int zero_blocks, cudaStream
   return FLOP_OK;
 }
 
-template <typename T, typename TW>
-int launch_runs(const emb::RunArgs& a, int lanes, cudaStream_t st) {
-  constexpr int U = sizeof(T) == 2 ? 8 : 4;
-  const dim3 grid((unsigned)((a.chunks * a.slices + 256 / lanes - 1) / (256 / lanes)));
-  if (lanes == 8)       launch_k(emb::runs_kernel<T, TW, 8, U>, grid, dim3(256), (size_t)0, st, a);
-  else if (lanes == 16) launch_k(emb::runs_kernel<T, TW, 16, U>, grid, dim3(256), (size_t)0, st, a);
-  else                  launch_k(emb::runs_kernel<T, TW, 32, U>, grid, dim3(256), (size_t)0, st, a);
+template <typename T, typename TW, int LPT>
+int launch_runs_as(const emb::RunArgs& a, cudaStream_t st) {
+  constexpr int AHEAD = EMB_AHEAD;
+  constexpr size_t ring = (size_t)AHEAD * emb::kStep * (sizeof(T) / 2) * 256 * 16;
+  auto kern = emb::runs_kernel<T, TW, LPT, AHEAD>;
+  static OncePerDevice configured;
+  FLOP_TRY(allow_smem(configured, ring, kern));
+  launch_k(kern, dim3((unsigned)((a.chunks * a.slices + 256 / LPT - 1) / (256 / LPT))), dim3(256), ring, st, a);
   FLOP_TRY(launched());
   if (a.chunks > 1) {
-    launch_k(emb::joints_kernel<TW>, dim3((unsigned)(a.chunks - 1), (unsigned)((a.d + 255) / 256)), dim3(256), (size_t)0, st, a);
+    launch_k(emb::joints_kernel<TW, LPT>, dim3((unsigned)((a.chunks + 7) / 8), (unsigned)a.slices), dim3(256), (size_t)0, st, a);
     FLOP_TRY(launched());
   }
   return FLOP_OK;
+}
+template <typename T, typename TW>
+int launch_runs(const emb::RunArgs& a, int lanes, cudaStream_t st) {
+  return lanes == 8 ? launch_runs_as<T, TW, 8>(a, st) : lanes == 16 ? launch_runs_as<T, TW, 16>(a, st) : launch_runs_as<T, TW, 32>(a, st);
+}
+
+template <typename T, typename TW>
+int launch_few(emb::RunArgs a, cudaStream_t st) {
+  a.slices = (a.d + 255) / 256;
+  a.token_blocks = (int)((a.T + 7) / 8) * a.slices;
+  a.clear_rows = (int)std::max<int64_t>(1, std::min<int64_t>(emb::kFewRows, 65536 / std::max<int64_t>(a.clear.row_bytes, 1)));
+  const int64_t clear_blocks = (a.clear.rows + a.clear_rows - 1) / a.clear_rows;
+  launch_k(emb::few_kernel<T, TW>, dim3((unsigned)(a.token_blocks + clear_blocks)), dim3(256), (size_t)0, st, a);
+  return launched();
 }
 
 // ---------------------------------------------------------------- layer norm
 // How a row is held: by `lanes` threads with `ng` units of 16 bytes each, in blocks of `threads`; lanes 0: rows too wide for that, which are walked.
 struct NormPlan { int lanes, ng, threads; };
-int64_t units_of(int64_t d, int dt) { return (d * (int64_t)elt(dt) + 15) / 16; }
 NormPlan plan_norm(int64_t units) {
   if (units <= 8) return {8, 1, 128};
   if (units <= 16) return {16, 1, 128};
@@ -143,8 +183,8 @@ constexpr int between(int lo, int v, int hi) { return v < lo ? lo : v > hi ? hi 
 constexpr int kRing = 220 * 1024;                     // shared memory of an SM that the rings of its blocks may take
 // Rows that a set of threads works on at once, blocks of an SM and batches copied ahead.
 struct NormShape { int rb, blocks, stages; };
-constexpr NormShape fwd_shape(int ng, int threads, int tensors) {
-  const int rb = between(1, 4 / (ng * tensors), 4), blocks = between(1, 512 / threads, 16);
+constexpr NormShape fwd_shape(int ng, int threads, int tensors, int per_sm = 512) {
+  const int rb = between(1, 4 / (ng * tensors), 4), blocks = between(1, per_sm / threads, 16);
   return {rb, blocks, between(1, kRing / (tensors * rb * ng * threads * 16 * blocks), 4)};
 }
 // One block on an SM, so that there are few parts of the column sums to add up: 512 threads, or, where a thread's three units take more than 128
@@ -179,21 +219,34 @@ NormWs plan_norm_ws(Arena& ar, int64_t T, int64_t d, int dt) {
 
 int walk_threads(int groups) { return std::min(512, (groups + 31) / 32 * 32); }
 
-template <typename T, bool SUM, int LANES, int NG, int THREADS>
-int launch_norm_fwd_held(const norm::FwdArgs& a, cudaStream_t st) {
-  constexpr int TENSORS = SUM ? 2 : 1;
-  constexpr NormShape s = fwd_shape(NG, THREADS, TENSORS);
+template <typename T, int MODE, int LANES, int NG, int THREADS>
+int launch_fwd_held(const norm::FwdArgs& a, unsigned segments, cudaStream_t st) {
+  constexpr int TENSORS = norm::kTensors<MODE>;
+  constexpr NormShape s = fwd_shape(NG, THREADS, TENSORS, MODE == norm::WHOLE || MODE == norm::SUMMED ? 512 : DROP_T);
   constexpr size_t smem = (size_t)s.stages * TENSORS * s.rb * NG * THREADS * 16;
-  auto kern = norm::fwd_kernel<T, SUM, LANES, NG, s.rb, s.stages, THREADS, s.blocks>;
+  auto kern = norm::fwd_kernel<T, MODE, LANES, NG, s.rb, s.stages, THREADS, s.blocks>;
   static OncePerDevice configured;
   FLOP_TRY(allow_smem(configured, smem, kern));
-  launch_k(kern, dim3((unsigned)norm_blocks(LANES, THREADS, a.T, s)), dim3(THREADS), smem, st, a);
+  const int64_t blocks = norm_blocks(LANES, THREADS, a.T, s);
+  launch_k(kern, dim3((unsigned)(segments == 1 ? blocks : (blocks + segments - 1) / segments), segments), dim3(THREADS), smem, st, a);
   return launched();
+}
+// Dropout by itself: rows of more than 256 units in segments of 256.
+template <typename T, int MODE>
+int launch_dropout(const norm::FwdArgs& a, cudaStream_t st) {
+  const int64_t units = units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32);
+  if (units <= 8) return launch_fwd_held<T, MODE, 8, 1, 128>(a, 1, st);
+  if (units <= 16) return launch_fwd_held<T, MODE, 16, 1, 128>(a, 1, st);
+  if (units <= 32) return launch_fwd_held<T, MODE, 32, 1, 128>(a, 1, st);
+  if (units <= 64) return launch_fwd_held<T, MODE, 32, 2, 128>(a, 1, st);
+  if (units <= 96) return launch_fwd_held<T, MODE, 32, 3, 128>(a, 1, st);
+  if (units <= 128) return launch_fwd_held<T, MODE, 64, 2, 128>(a, 1, st);
+  return launch_fwd_held<T, MODE, 128, 2, 128>(a, (unsigned)((units + 255) / 256), st);
 }
 template <typename T, bool SUM>
 int launch_norm_fwd(const norm::FwdArgs& a, cudaStream_t st) {
   const NormPlan p = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32));
-#define FLOP_HELD(L, N, B) if (p.lanes == L && p.ng == N) return launch_norm_fwd_held<T, SUM, L, N, B>(a, st);
+#define FLOP_HELD(L, N, B) if (p.lanes == L && p.ng == N) return launch_fwd_held<T, SUM ? norm::SUMMED : norm::WHOLE, L, N, B>(a, 1, st);
   FLOP_HELD_PLANS(FLOP_HELD)
 #undef FLOP_HELD
   launch_k(norm::fwd_walk_kernel<T, SUM>, dim3((unsigned)a.T), dim3(walk_threads(a.groups)), (size_t)0, st, a);
@@ -265,10 +318,7 @@ int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde
   emb::LookupArgs a{};
   a.ids = ids; a.T = T; a.E = E; a.lde = lde; a.V = n_rows; a.Y = Y; a.ldy = ldy; a.scale = scale; a.d = (int)d;
   a.vec = y.vec() && (n_rows == 0 || e.vec());
-  const dim3 grid = group_grid(a, T, d, 8);
-  if (dt == FLOP_BF16) launch_k(emb::lookup_kernel<bf16>, grid, dim3(256), (size_t)0, (cudaStream_t)stream, a);
-  else                 launch_k(emb::lookup_kernel<float>, grid, dim3(256), (size_t)0, (cudaStream_t)stream, a);
-  return launched();
+  return dt == FLOP_BF16 ? launch_lookup<bf16>(a, units_of(d, dt), (cudaStream_t)stream) : launch_lookup<float>(a, units_of(d, dt), (cudaStream_t)stream);
 }
 
 int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t T, int64_t n_rows, float scale, void* dE, int64_t ldde, int accumulate,
@@ -284,31 +334,35 @@ int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t
   Arena ar{(unsigned char*)ws, ws_bytes, 0};
   const EmbWs w = plan_emb_ws(ar, T, d);
   FLOP_TRY(check_ws(ws, ws_bytes, w.bytes));
+  const RunPlan p = plan_runs(T, d);
+  emb::RunArgs a{};
+  a.order = w.order[0]; a.ids = ids; a.T = T; a.V = (uint32_t)n_rows; a.dY = dY; a.lddy = lddy; a.dE = dE; a.ldde = ldde; a.part = w.part; a.part_ld = w.part_ld;
+  a.chunks = p.chunks; a.chunk = p.chunk; a.scale = scale; a.d = (int)d; a.slices = p.slices; a.accumulate = accumulate; a.vec = dy.vec(); a.vec_out = de.vec();
+  emb::ClearArgs& z = a.clear;
+  if (!accumulate) {
+    z.p = (unsigned char*)dE; z.rows = n_rows; z.row_bytes = d * (int64_t)elt(wgrad_dt); z.pitch = ldde * (int64_t)elt(wgrad_dt); z.vec = de.vec();
+  }
+  auto typed = [&](auto go) {
+    if (dt == FLOP_BF16) return wgrad_dt == FLOP_BF16 ? go(bf16{}, bf16{}) : go(bf16{}, float{});
+    return wgrad_dt == FLOP_BF16 ? go(float{}, bf16{}) : go(float{}, float{});
+  };
+  if (T <= std::min(EMB_FEW, emb::kFewTokens)) return typed([&](auto t, auto tw) { return launch_few<decltype(t), decltype(tw)>(a, st); });
   emb::SortArgs s{};
-  s.ids = ids; s.T = T; s.V = (uint32_t)n_rows;
+  s.ids = ids; s.T = T; s.V = (uint32_t)n_rows; s.clear = z;
   s.order[0] = w.order[0]; s.order[1] = w.order[1];
   int word_bits = 1;
   while ((uint64_t)n_rows >> word_bits) ++word_bits;          // n_rows itself stands for padding
-  s.passes = T == 0 ? 0 : (word_bits + emb::kMaxDigitBits - 1) / emb::kMaxDigitBits;
-  s.bits = T == 0 ? 1 : (word_bits + s.passes - 1) / s.passes;
-  // 2048 tokens a block: two for each thread
-  s.cluster = 1;
-  while (s.cluster < 8 && T > (int64_t)s.cluster * 2048) s.cluster *= 2;
-  int zero_blocks = 0;
-  if (!accumulate) {
-    s.dE = (unsigned char*)dE; s.row_bytes = d * (int64_t)elt(wgrad_dt); s.pitch = ldde * (int64_t)elt(wgrad_dt); s.rows = n_rows;
-    s.vec = de.vec();
-    const int64_t pieces = n_rows * ((s.row_bytes + 15) / 16);
-    zero_blocks = (int)std::min<int64_t>(round_up((pieces + emb::kSortThreads - 1) / emb::kSortThreads, s.cluster), 2 * num_sms() / s.cluster * s.cluster);
-  }
-  FLOP_TRY(launch_sort(s, emb::sort_smem(s.bits), zero_blocks, st));
-  if (T == 0) return FLOP_OK;
-  const RunPlan p = plan_runs(T, d);
-  emb::RunArgs a{};
-  a.order = w.order[0]; a.T = T; a.V = (uint32_t)n_rows; a.dY = dY; a.lddy = lddy; a.dE = dE; a.ldde = ldde; a.part = w.part; a.part_ld = w.part_ld;
-  a.chunks = p.chunks; a.chunk = p.chunk; a.scale = scale; a.d = (int)d; a.slices = p.slices; a.accumulate = accumulate; a.vec = dy.vec(); a.vec_out = de.vec();
-  if (dt == FLOP_BF16) return wgrad_dt == FLOP_BF16 ? launch_runs<bf16, bf16>(a, p.lanes, st) : launch_runs<bf16, float>(a, p.lanes, st);
-  return wgrad_dt == FLOP_BF16 ? launch_runs<float, bf16>(a, p.lanes, st) : launch_runs<float, float>(a, p.lanes, st);
+  s.passes = (word_bits + emb::kMaxDigitBits - 1) / emb::kMaxDigitBits;
+  s.bits = (word_bits + s.passes - 1) / s.passes;
+  s.counts = w.counts;
+  const int64_t blocks = (T + emb::kSortBlock - 1) / emb::kSortBlock;
+  s.blocks = 1;
+  while (s.blocks < kSortCluster && s.blocks < blocks) s.blocks *= 2;
+  if (blocks > kSortCluster) s.blocks = (int)std::min<int64_t>(blocks, emb::kSortBlocks);
+  const int64_t pieces = z.rows * ((z.row_bytes + 15) / 16), most = (int64_t)num_sms() * ZPB;
+  const int zero_blocks = (int)std::min<int64_t>(round_up((pieces + 4 * emb::kSortThreads - 1) / (4 * emb::kSortThreads), s.blocks), most);
+  FLOP_TRY(launch_sort(s, zero_blocks, st));
+  return typed([&](auto t, auto tw) { return launch_runs<decltype(t), decltype(tw)>(a, p.lanes, st); });
 }
 
 static int dropout_impl(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* Y,
@@ -319,15 +373,13 @@ static int dropout_impl(const void* X, int64_t ldx, const void* R, int64_t ldr, 
   if (!x.given() || !x.fits(d) || !y.given() || !y.fits(d) || (r.given() && !r.fits(d))) return FLOP_ERR_INVALID_ARG;
   if (T > INT32_MAX || d > kMaxCols || !x.placed() || !y.placed() || (r.given() && !r.placed())) return FLOP_ERR_UNSUPPORTED;
   if (!in_place_or_apart(y, x, T, d) || !in_place_or_apart(y, r, T, d)) return FLOP_ERR_INVALID_ARG;
-  DropoutArgs a{};
-  a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.Y = Y; a.ldy = ldy; a.T = T; a.d = (int)d;
+  norm::FwdArgs a{};
+  a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.S = Y; a.lds = ldy; a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
   a.vec = x.vec() && y.vec() && (!r.given() || r.vec());
   a.drop = make_drop(p, seed, offset, offset_dev);
-  const dim3 grid = group_grid(a, T, d, 8);
   cudaStream_t st = (cudaStream_t)stream;
-  if (dt == FLOP_BF16) R ? launch_k(dropout_kernel<bf16, true>, grid, dim3(256), (size_t)0, st, a) : launch_k(dropout_kernel<bf16, false>, grid, dim3(256), (size_t)0, st, a);
-  else                 R ? launch_k(dropout_kernel<float, true>, grid, dim3(256), (size_t)0, st, a) : launch_k(dropout_kernel<float, false>, grid, dim3(256), (size_t)0, st, a);
-  return launched();
+  if (dt == FLOP_BF16) return R ? launch_dropout<bf16, norm::ADDED>(a, st) : launch_dropout<bf16, norm::DROPPED>(a, st);
+  return R ? launch_dropout<float, norm::ADDED>(a, st) : launch_dropout<float, norm::DROPPED>(a, st);
 }
 
 int flop_dropout_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* Y,

@@ -6,7 +6,6 @@
 // Sums, means and the deviation are fp32; the variance is the mean of squared differences from the mean (a second look at the row).
 #pragma once
 #include "dropout.cuh"
-#include "pairs.cuh"
 
 namespace flop {
 namespace norm {
@@ -213,69 +212,13 @@ bwd_walk_kernel(const BwdArgs a) {
 // waited for but the thread's own copies, and the memory system always has work in flight: under load an access takes 1.5 to 2 us, and a
 // kernel that loads, computes and stores a row at a time has a quarter of the bytes in flight that this needs.
 // All units but the last of a thread are whole and present (the host picks LANES and NG so), which leaves one to be looked at.
-template <typename T> constexpr int kUnit = 16 / (int)sizeof(T);      // columns of a unit
-template <typename T> constexpr int kPairs = kUnit<T> / 2;
-
-__device__ __forceinline__ void copy_async16(void* to, const void* from, int bytes) {      // zeros behind `bytes`
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copy_async4(void* to, const void* from, int bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // The thread's units of a row (`from`: its first), `last` columns in the last one (<= 0: none), into its slots, THREADS apart.  No such row (on is false): zeros.
-template <typename T, int LANES, int NG, int THREADS>
+// EACH: any of its units may end early or be absent.
+template <typename T, int LANES, int NG, int THREADS, bool EACH = false>
 __device__ __forceinline__ void copy_units(uint4* to, const T* from, int last, bool on, bool vec) {
 #pragma unroll
-  for (int i = 0; i < NG; ++i) {
-    const int n = !on ? 0 : i < NG - 1 ? kUnit<T> : min(max(last, 0), kUnit<T>);
-    const T* at = from + i * LANES * kUnit<T>;
-    if (sizeof(T) == 2 || vec) {
-      copy_async16(to + i * THREADS, at, n * (int)sizeof(T));
-    } else {
-#pragma unroll
-      for (int j = 0; j < kUnit<T>; ++j) copy_async4(reinterpret_cast<T*>(to + i * THREADS) + j, at + j, j < n ? 4 : 0);
-    }
-  }
-}
-template <typename T>
-__device__ __forceinline__ void unpack_unit(const uint4& q, uint64_t (&v)[kPairs<T>]) {
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int j = 0; j < kPairs<T>; ++j) {
-    if constexpr (sizeof(T) == 2) v[j] = pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
-    else v[j] = pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
-  }
-}
-template <typename T>
-__device__ __forceinline__ uint4 pack_unit(const uint64_t (&v)[kPairs<T>]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < kPairs<T>; ++j) {
-    const float2 u = unpack2(v[j]);
-    if constexpr (sizeof(T) == 2) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(u.x, u.y);
-      memcpy(&w[j], &h, 4);
-    } else {
-      w[2 * j] = __float_as_uint(u.x);
-      w[2 * j + 1] = __float_as_uint(u.y);
-    }
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-template <typename T>
-__device__ __forceinline__ void store_unit(T* p, const uint4& q, int n, bool vec) {
-  if ((sizeof(T) == 2 || vec) && n >= kUnit<T>) {
-    *reinterpret_cast<uint4*>(p) = q;
-  } else {
-    T v[kUnit<T>];
-    memcpy(v, &q, 16);
-#pragma unroll
-    for (int j = 0; j < kUnit<T>; ++j)
-      if (j < n) p[j] = v[j];
-  }
+  for (int i = 0; i < NG; ++i)
+    copy_unit(to + i * THREADS, from + i * LANES * kUnit<T>, !on ? 0 : EACH ? last + (NG - 1 - i) * LANES * kUnit<T> : i < NG - 1 ? kUnit<T> : last, vec);
 }
 // Pairs of a vector's columns; absent ones 0.
 template <typename T>
@@ -292,41 +235,6 @@ __device__ __forceinline__ void vector_unit(const float* p, int k, int n, bool v
   }
 #pragma unroll
   for (int j = 0; j < kPairs<T>; ++j) v[j] = pack2(f[2 * j], f[2 * j + 1]);
-}
-
-// The mask's bits for the thread's units, 16 for each column.  A unit of fp32 is half a block of the generator: the two threads of a pair draw one block each
-// for every two units and exchange halves.  All lanes of a warp come here together.
-template <typename T, int LANES, int NG>
-__device__ __forceinline__ void drop_units(const Drop& d, uint64_t row, int l, uint32_t (&bits)[NG][kPairs<T>]) {
-  if constexpr (sizeof(T) == 2) {
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const uint4 x = drop_bits(d, row + (uint32_t)(l + i * LANES));
-      bits[i][0] = x.x; bits[i][1] = x.y; bits[i][2] = x.z; bits[i][3] = x.w;
-    }
-  } else {
-    const bool odd = l & 1;
-#pragma unroll
-    for (int i = 0; i < NG; i += 2) {
-      const uint4 x = drop_bits(d, row + (uint32_t)((l + (i + (i + 1 < NG && odd)) * LANES) >> 1));
-      const uint32_t keep[2] = {odd ? x.z : x.x, odd ? x.w : x.y};
-      if (i + 1 < NG) {
-        const uint32_t got[2] = {__shfl_xor_sync(0xffffffffu, odd ? x.x : x.z, 1), __shfl_xor_sync(0xffffffffu, odd ? x.y : x.w, 1)};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          bits[i][j] = odd ? got[j] : keep[j];
-          bits[i + 1][j] = odd ? keep[j] : got[j];
-        }
-      } else {
-        bits[i][0] = keep[0];
-        bits[i][1] = keep[1];
-      }
-    }
-  }
-}
-__device__ __forceinline__ uint64_t select_pair(uint32_t bits, uint32_t threshold, uint64_t kept, uint64_t dropped) {
-  const float2 k = unpack2(kept), d = unpack2(dropped);
-  return pack2((bits & 0xFFFFu) >= threshold ? k.x : d.x, (bits >> 16) >= threshold ? k.y : d.y);
 }
 
 // Sums over the LANES threads that share a row, in a fixed order; every one gets them.  Rows of several warps have a barrier each; `scratch` (one
@@ -358,13 +266,18 @@ __device__ __forceinline__ float both(uint64_t v) {
   return u.x + u.y;
 }
 
-template <typename T, bool SUM, int LANES, int NG, int RB, int STAGES, int THREADS, int BLOCKS>
+// What the forward kernel does with a row: WHOLE is the norm of X, SUMMED that of S = R + dropout(X); ADDED and DROPPED stop at S, with and without R: dropout by itself, which
+// has no use for whole rows, so that a row may be cut into segments of LANES * NG units (blockIdx.y).
+enum { WHOLE, SUMMED, ADDED, DROPPED };
+template <int MODE> constexpr int kTensors = MODE == SUMMED || MODE == ADDED ? 2 : 1;
+template <typename T, int MODE, int LANES, int NG, int RB, int STAGES, int THREADS, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
 fwd_kernel(const FwdArgs a) {
-  constexpr int ROWS = THREADS / LANES, E = kUnit<T>, H = kPairs<T>, ROW = NG * THREADS, SIZE = (SUM ? 2 : 1) * RB * ROW;
+  constexpr bool SUM = MODE != WHOLE, NORM = MODE == WHOLE || MODE == SUMMED, RES = kTensors<MODE> == 2;
+  constexpr int ROWS = THREADS / LANES, E = kUnit<T>, H = kPairs<T>, ROW = NG * THREADS, SIZE = kTensors<MODE> * RB * ROW;
   extern __shared__ uint4 ring[];                        // [STAGES][X and R][RB][NG][THREADS]
   __shared__ float scratch[2][RB][32];
-  const int l = threadIdx.x % LANES, r = threadIdx.x / LANES;
+  const int l = threadIdx.x % LANES + (NORM ? 0 : blockIdx.y * LANES * NG), r = threadIdx.x / LANES;
   const int last = a.d - (l + (NG - 1) * LANES) * E;     // columns of the last unit
   const int batches = (int)((a.T + ROWS * RB - 1) / (ROWS * RB));
   const float inv_d = 1.f / (float)a.d;
@@ -376,8 +289,8 @@ fwd_kernel(const FwdArgs a) {
 #pragma unroll
     for (int q = 0; q < RB; ++q) {
       const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
-      copy_units<T, LANES, NG, THREADS>(to + q * ROW, (const T*)a.X + t * a.ldx + l * E, last, t < a.T, a.vec);
-      if (SUM && a.R) copy_units<T, LANES, NG, THREADS>(to + (RB + q) * ROW, (const T*)a.R + t * a.ldr + l * E, last, t < a.T, a.vec);
+      copy_units<T, LANES, NG, THREADS, !NORM>(to + q * ROW, (const T*)a.X + t * a.ldx + l * E, last, t < a.T, a.vec);
+      if (RES && a.R) copy_units<T, LANES, NG, THREADS, !NORM>(to + (RB + q) * ROW, (const T*)a.R + t * a.ldr + l * E, last, t < a.T, a.vec);
     }
   };
 #pragma unroll
@@ -386,46 +299,53 @@ fwd_kernel(const FwdArgs a) {
     if (batch < batches) fetch(batch, st);
     copies_commit();
   }
-  uint64_t w[NG][H], b[NG][H];
+  uint64_t w[NORM ? NG : 1][H], b[NORM ? NG : 1][H];
+  if constexpr (NORM) {
 #pragma unroll
-  for (int i = 0; i < NG; ++i) {
-    const int k = (l + i * LANES) * E;
-    vector_unit<T>(a.w, k, a.d - k, a.wvec, 1.f, w[i]);
-    vector_unit<T>(a.b, k, a.d - k, a.wvec, 0.f, b[i]);
+    for (int i = 0; i < NG; ++i) {
+      const int k = (l + i * LANES) * E;
+      vector_unit<T>(a.w, k, a.d - k, a.wvec, 1.f, w[i]);
+      vector_unit<T>(a.b, k, a.d - k, a.wvec, 0.f, b[i]);
+    }
   }
   int stage = 0;
   for (int batch = blockIdx.x; batch < batches; batch += gridDim.x) {
     copies_wait<STAGES - 1>();
     const uint4* at = ring + stage * SIZE + threadIdx.x;
-    uint64_t s[RB][NG][H];
+    uint64_t s[NORM ? RB : 1][NORM ? NG : 1][H];
     float sum[RB];
 #pragma unroll
     for (int q = 0; q < RB; ++q) {
       const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
       uint64_t total = 0;
       uint32_t bits[NG][H];
-      if (SUM && a.drop.threshold) drop_units<T, LANES, NG>(a.drop, offset + (uint64_t)t * a.groups, l, bits);
+      if (SUM && (!RES || a.drop.threshold)) drop_units<T, NG>(a.drop, l & 1, [&](int i) { return offset + (uint64_t)t * a.groups + (uint32_t)((l + i * LANES) / (8 / E)); }, bits);
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        unpack_unit<T>(at[q * ROW + i * THREADS], s[q][i]);
+        uint64_t(&v)[H] = s[NORM ? q : 0][NORM ? i : 0];
+        unpack_unit<T>(at[q * ROW + i * THREADS], v);
         if constexpr (SUM) {
           uint64_t res[H];
-          if (a.R) {
+          if (RES && a.R) {
             unpack_unit<T>(at[(RB + q) * ROW + i * THREADS], res);
           } else {
 #pragma unroll
             for (int j = 0; j < H; ++j) res[j] = 0;
           }
 #pragma unroll
-          for (int j = 0; j < H; ++j)
-            s[q][i][j] = a.drop.threshold ? select_pair(bits[i][j], a.drop.threshold, fma2(s[q][i][j], scale, res[j]), res[j]) : add2(s[q][i][j], res[j]);
-          const uint4 rounded = pack_unit<T>(s[q][i]);
-          const int n = i < NG - 1 ? E : last;
+          for (int j = 0; j < H; ++j) {
+            if (!RES) v[j] = select_pair(bits[i][j], a.drop.threshold, mul2(v[j], scale), 0);
+            else v[j] = a.drop.threshold ? select_pair(bits[i][j], a.drop.threshold, fma2(v[j], scale, res[j]), res[j]) : add2(v[j], res[j]);
+          }
+          const uint4 rounded = pack_unit<T>(v);
+          const int n = !NORM ? last + (NG - 1 - i) * LANES * E : i < NG - 1 ? E : last;
           if (a.S && t < a.T && n > 0) store_unit((T*)a.S + t * a.lds + (l + i * LANES) * E, rounded, n, a.vec);
-          unpack_unit<T>(rounded, s[q][i]);
+          if (NORM) unpack_unit<T>(rounded, v);
         }
+        if constexpr (NORM) {
 #pragma unroll
-        for (int j = 0; j < H; ++j) total = add2(total, s[q][i][j]);
+          for (int j = 0; j < H; ++j) total = add2(total, v[j]);
+        }
       }
       sum[q] = both(total);
     }
@@ -433,45 +353,47 @@ fwd_kernel(const FwdArgs a) {
     if (ahead < batches) fetch(ahead, stage);
     copies_commit();
     stage = stage + 1 == STAGES ? 0 : stage + 1;
-    row_sum<LANES, THREADS>(sum, scratch[0]);
-    float mean[RB];
+    if constexpr (NORM) {
+      row_sum<LANES, THREADS>(sum, scratch[0]);
+      float mean[RB];
 #pragma unroll
-    for (int q = 0; q < RB; ++q) {
-      mean[q] = sum[q] * inv_d;
-      const uint64_t minus = pack2(-mean[q], -mean[q]);
-      uint64_t total = 0;
+      for (int q = 0; q < RB; ++q) {
+        mean[q] = sum[q] * inv_d;
+        const uint64_t minus = pack2(-mean[q], -mean[q]);
+        uint64_t total = 0;
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
+        for (int i = 0; i < NG; ++i) {
 #pragma unroll
-        for (int j = 0; j < H; ++j) s[q][i][j] = add2(s[q][i][j], minus);
-        if (i == NG - 1 && last < E) {                   // what lies behind the row's end is no difference
+          for (int j = 0; j < H; ++j) s[q][i][j] = add2(s[q][i][j], minus);
+          if (i == NG - 1 && last < E) {                   // what lies behind the row's end is no difference
 #pragma unroll
-          for (int j = 0; j < H; ++j) {
-            const float2 u = unpack2(s[q][i][j]);
-            s[q][i][j] = pack2(2 * j < last ? u.x : 0.f, 2 * j + 1 < last ? u.y : 0.f);
+            for (int j = 0; j < H; ++j) {
+              const float2 u = unpack2(s[q][i][j]);
+              s[q][i][j] = pack2(2 * j < last ? u.x : 0.f, 2 * j + 1 < last ? u.y : 0.f);
+            }
           }
+#pragma unroll
+          for (int j = 0; j < H; ++j) total = fma2(s[q][i][j], s[q][i][j], total);
         }
-#pragma unroll
-        for (int j = 0; j < H; ++j) total = fma2(s[q][i][j], s[q][i][j], total);
+        sum[q] = both(total);
       }
-      sum[q] = both(total);
-    }
-    row_sum<LANES, THREADS>(sum, scratch[1]);
+      row_sum<LANES, THREADS>(sum, scratch[1]);
 #pragma unroll
-    for (int q = 0; q < RB; ++q) {
-      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
-      if (t >= a.T) break;
-      const float rstd = rsqrtf(fmaf(sum[q], inv_d, a.eps));
-      if (a.stats && l == 0) a.stats[t] = make_float2(mean[q], rstd);
-      const uint64_t by = pack2(rstd, rstd);
-      T* Y = (T*)a.Y + t * a.ldy + l * E;
+      for (int q = 0; q < RB; ++q) {
+        const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+        if (t >= a.T) break;
+        const float rstd = rsqrtf(fmaf(sum[q], inv_d, a.eps));
+        if (a.stats && l == 0) a.stats[t] = make_float2(mean[q], rstd);
+        const uint64_t by = pack2(rstd, rstd);
+        T* Y = (T*)a.Y + t * a.ldy + l * E;
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int n = i < NG - 1 ? E : last;
-        if (n > 0) {
+        for (int i = 0; i < NG; ++i) {
+          const int n = i < NG - 1 ? E : last;
+          if (n > 0) {
 #pragma unroll
-          for (int j = 0; j < H; ++j) s[q][i][j] = fma2(mul2(s[q][i][j], by), w[i][j], b[i][j]);
-          store_unit(Y + i * LANES * E, pack_unit<T>(s[q][i]), n, a.vec);
+            for (int j = 0; j < H; ++j) s[q][i][j] = fma2(mul2(s[q][i][j], by), w[i][j], b[i][j]);
+            store_unit(Y + i * LANES * E, pack_unit<T>(s[q][i]), n, a.vec);
+          }
         }
       }
     }
@@ -573,7 +495,7 @@ bwd_kernel(const BwdArgs a) {
         const float c1 = -c[2 * q] * inv_d, c2 = -c[2 * q + 1] * inv_d;
         const uint64_t m1 = pack2(c1, c1), m2 = pack2(c2, c2), by = pack2(st[q].y, st[q].y);
         uint32_t bits[NG][H];
-        if (a.dX && a.drop.threshold) drop_units<T, LANES, NG>(a.drop, offset + (uint64_t)t * a.groups, l, bits);
+        if (a.dX && a.drop.threshold) drop_units<T, NG>(a.drop, l & 1, [&](int i) { return offset + (uint64_t)t * a.groups + (uint32_t)((l + i * LANES) / (8 / E)); }, bits);
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
           const int k = (l + i * LANES) * E, n = i < NG - 1 ? E : last;

@@ -501,7 +501,7 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
 /* Operators on token rows, in front of and between the factorised matrices of a model in training (no counterpart in the paper).
  * dt is the type of every matrix of a call; bf16 matrices follow the header's rules on alignment, fp32 ones may start anywhere and have any
  * leading dimension (rows that start on 16 bytes are faster).  Columns of an output from d on are left untouched.
- * At most 2^31 - 1 rows, 2^24 columns (FLOP_ERR_UNSUPPORTED beyond).
+ * At most 2^31 - 1 rows, 2^23 columns (FLOP_ERR_UNSUPPORTED beyond).
  *
  * Embedding, dense (the counterpart of flop_gated_embedding_* for a table that is not factorised): ids[T] (int32, DEVICE) are rows of
  * E[n_rows, d]; ids outside [0, n_rows) are padding.
@@ -509,7 +509,7 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
  *   _bwd   dE[v] (= | += with accumulate) scale * sum over {t: ids[t] = v} of dY[t], in type wgrad_dt.  Without accumulate every row of
  *          dE[n_rows, d] is written (zeros for words that do not occur), with it only the rows of words that do.
  *          Sums are fp32, in an order that depends on T, d and the device alone: results are reproducible.
- *          dE may not overlap dY or ids.  ws: flop_workspace_bytes(FLOP_OP_EMBEDDING_SORTED_BWD, T, d, 0, n_rows, dt). */
+ *          dE may not overlap dY or ids; lddy below 2^31.  ws: flop_workspace_bytes(FLOP_OP_EMBEDDING_SORTED_BWD, T, d, 0, n_rows, dt). */
 int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde, int64_t n_rows, float scale, void* Y,
                        int64_t ldy, int64_t d, int dt, void* stream);
 int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t T, int64_t n_rows, float scale, void* dE,

@@ -202,6 +202,12 @@ struct SortShared {
     return at + __popc(same & ((1u << lane) - 1));
   }
 };
+// Behind the last pair there are a few that are no words, so that whoever reads the order needs no bounds.
+constexpr int kBehind = 16;
+constexpr uint32_t kNoWord = 0xFFFFFFFFu;                // words are below 2^31
+__device__ __forceinline__ void end_order(const SortArgs& a, int block) {
+  if (block == 0 && threadIdx.x < kBehind) a.order[0][a.T + threadIdx.x] = make_uint2(kNoWord, 0);
+}
 // Pairs [lo, hi) of this warp.
 __device__ __forceinline__ void warp_run(int64_t T, int block, int blocks, int64_t& lo, int64_t& hi) {
   const int64_t warps = (int64_t)blocks * kSortWarps, per = ((T + warps * 32 - 1) / (warps * 32)) * 32;
@@ -281,6 +287,7 @@ sort_kernel(const SortArgs a) {
   const int lane = threadIdx.x & 31, rank = (int)cluster.block_rank();
   int64_t lo, hi;
   warp_run(a.T, rank, a.blocks, lo, hi);
+  end_order(a, rank);
   for (int pass = 0; pass < a.passes; ++pass) {
     uint2 held[kSortHeld];
     uint32_t before[kSortHeld], digit[kSortHeld];        // pairs of the same digit before it in the warp's run
@@ -369,6 +376,7 @@ sort_move_kernel(const SortArgs a, int pass) {
   }
   int64_t lo, hi;
   warp_run(a.T, blockIdx.x, a.blocks, lo, hi);
+  end_order(a, blockIdx.x);
   count_run(a, s, pass, lo, hi);
   scan_warps(sm, s);
   place_digits(s, all, ahead);
@@ -407,6 +415,14 @@ __device__ __forceinline__ void write_columns(const RunArgs& a, uint32_t word, i
   TW* p = (TW*)a.dE + (int64_t)word * a.ldde + k;
   constexpr int BYTES = E * (int)sizeof(TW);
   const bool whole = a.vec_out && n >= E;
+  if constexpr (sizeof(TW) == 4) {
+    if (a.accumulate && whole) {       // this thread alone writes here: the memory adds, and nothing waits for the old values (subnormal sums become zero)
+#pragma unroll
+      for (int j = 0; j < E; j += 4)
+        atomicAdd(reinterpret_cast<float4*>(p + j), make_float4(a.scale * v[j], a.scale * v[j + 1], a.scale * v[j + 2], a.scale * v[j + 3]));
+      return;
+    }
+  }
   TW out[E];
   if (a.accumulate) {
     if (whole) {
@@ -448,12 +464,14 @@ __device__ __forceinline__ void write_columns(const RunArgs& a, uint32_t word, i
 }
 
 // LPT lanes take a chunk's slice of LPT * 8 columns.  Their rows come through a ring of AHEAD steps of four, each thread copying and reading its own units:
-// one row after another from memory would leave a warp waiting for most of its time (16384 tokens of 205 words, 2048 columns: 35 us, now 14).
+// one batch of rows after another from memory would leave a warp waiting for most of its time.  Where a run ends is noted when its rows are sent for, so
+// that adding up takes no look at the words; behind the last pair there are kBehind that are no words, so that a chunk's last step needs no bounds.
 constexpr int kStep = 4;
 template <typename T, typename TW, int LPT, int AHEAD>
 __global__ void __launch_bounds__(256)
 runs_kernel(const RunArgs a) {
-  constexpr int E = kUnit<T>, NU = 8 / E;                // units of a thread: eight columns
+  static_assert(AHEAD * kStep <= 32, "a bit for every row on its way");
+  constexpr int E = kUnit<T>, NU = 8 / E, SLOT = kStep * NU * 256;     // units of a thread: eight columns
   extern __shared__ uint4 ring[];                        // [AHEAD][kStep][NU][256]
   pdl_wait();
   pdl_launch_dependents();
@@ -461,93 +479,97 @@ runs_kernel(const RunArgs a) {
   const int64_t c = unit / a.slices;
   if (c >= a.chunks) return;
   const int k0 = ((int)(unit - c * a.slices) * LPT * NU + threadIdx.x % LPT) * E;      // the first unit's column; the second is LPT units behind
-  const int64_t lo = c * a.chunk, hi = min(a.T, lo + a.chunk);
-  const int steps = (int)((hi - lo + kStep - 1) / kStep);
-  // entries i .. i + 3, two at a time (i is a multiple of four, and the order is followed by room for more)
-  auto entries = [&](int64_t i, uint4 (&e)[2]) {
-    e[0] = e[1] = make_uint4(a.V, 0, a.V, 0);
-    if (i < hi) e[0] = *reinterpret_cast<const uint4*>(a.order + i);
-    if (i + 2 < hi) e[1] = *reinterpret_cast<const uint4*>(a.order + i + 2);
+  const int64_t lo = c * a.chunk;
+  const int rows = (int)min((int64_t)a.chunk, a.T - lo), steps = (rows + kStep - 1) / kStep;
+  const uint2* order = a.order + lo;
+  const uint32_t ld = (uint32_t)a.lddy;
+  const T* dY = (const T*)a.dY + k0;
+  auto entries = [&](int step, uint4 (&e)[2]) {
+    e[0] = reinterpret_cast<const uint4*>(order)[step * 2];
+    e[1] = reinterpret_cast<const uint4*>(order)[step * 2 + 1];
   };
-  auto fetch = [&](int step, int slot, const uint4 (&e)[2]) {
-    const uint32_t word[4] = {e[0].x, e[0].z, e[1].x, e[1].z}, token[4] = {e[0].y, e[0].w, e[1].y, e[1].w};
-    const int64_t i = lo + (int64_t)step * kStep;
-    uint4* to = ring + slot * (kStep * NU * 256) + threadIdx.x;
+  uint4 now[2] = {}, next[2] = {};                                 // the pairs of the step to be sent for, and of the one behind it
+  uint32_t ends = 0;                                     // four bits a slot: a run ends with this row
+  auto fetch = [&](int step, int slot) {
+    const uint32_t word[kStep + 1] = {now[0].x, now[0].z, now[1].x, now[1].z, next[0].x}, token[kStep] = {now[0].y, now[0].w, now[1].y, now[1].w};
+    uint4* to = ring + slot * SLOT + threadIdx.x;
+    uint32_t bits = 0;
 #pragma unroll
     for (int u = 0; u < kStep; ++u) {
-      const bool on = i + u < hi && word[u] < a.V;
-      const T* row = (const T*)a.dY + (int64_t)(on ? token[u] : 0) * a.lddy + k0;
+      const bool on = word[u] < a.V;
+      const T* row = dY + (uint64_t)(on ? token[u] : 0) * ld;
 #pragma unroll
       for (int q = 0; q < NU; ++q) copy_unit(to + (u * NU + q) * 256, row + q * LPT * E, on ? a.d - k0 - q * LPT * E : 0, a.vec);
+      if (on && word[u + 1] != word[u]) bits |= 1u << u;
     }
+    ends = (ends & ~(15u << (slot * kStep))) | bits << (slot * kStep);
+    now[0] = next[0];
+    now[1] = next[1];
+    if (step + 2 < steps) entries(step + 2, next);
+    else next[0] = *reinterpret_cast<const uint4*>(order + (step + 2) * kStep);          // for its first word
   };
-  uint4 ahead[2];
-  entries(lo, ahead);
+  entries(0, now);
+  if (steps > 1) entries(1, next);
+  else next[0] = *reinterpret_cast<const uint4*>(order + kStep);
+  bool open = lo > 0 && a.order[lo - 1].x == now[0].x;   // the run comes from before the chunk
 #pragma unroll
   for (int s = 0; s < AHEAD; ++s) {
-    if (s < steps) {
-      fetch(s, s, ahead);
-      entries(lo + (s + 1) * kStep, ahead);
-    }
+    if (s < steps) fetch(s, s);
     copies_commit();
   }
-  const uint32_t none = 0xFFFFFFFFu;                     // no word: words are below 2^31
-  bool open = lo > 0 && a.order[lo - 1].x == a.order[lo].x;         // the run comes from before the chunk
   uint64_t acc[NU][E / 2];
 #pragma unroll
   for (int q = 0; q < NU; ++q)
 #pragma unroll
     for (int j = 0; j < E / 2; ++j) acc[q][j] = 0;
-  int slot = 0;
-  for (int s = 0; s < steps; ++s) {
-    const int64_t i = lo + (int64_t)s * kStep;
-    uint32_t word[kStep + 1];
+  // what has been added up goes to the word's row, or to the chunk's place for the run that comes from before it or goes on behind it
+  auto put = [&](uint32_t word, int part) {
 #pragma unroll
-    for (int u = 0; u <= kStep; ++u) word[u] = i + u < a.T ? a.order[i + u].x : none;
-    copies_wait<AHEAD - 1>();
-    const uint4* at = ring + slot * (kStep * NU * 256) + threadIdx.x;
+    for (int q = 0; q < NU; ++q) {
+      const int k = k0 + q * LPT * E, n = a.d - k;
+      float f[E];
 #pragma unroll
-    for (int u = 0; u < kStep; ++u) {
-      if (i + u < hi && word[u] < a.V) {
-        const bool ends = word[u + 1] != word[u], stops = i + u + 1 == hi;
+      for (int j = 0; j < E / 2; ++j) {
+        const float2 w = unpack2(acc[q][j]);
+        f[2 * j] = w.x;
+        f[2 * j + 1] = w.y;
+        acc[q][j] = 0;
+      }
+      if (n <= 0) continue;
+      if (part < 0) {
+        write_columns<TW, E>(a, word, k, n, f);
+      } else {
+        float* p = a.part + (c * 2 + part) * a.part_ld + k;
 #pragma unroll
-        for (int q = 0; q < NU; ++q) {
-          uint64_t v[E / 2];
-          unpack_unit<T>(at[(u * NU + q) * 256], v);
-#pragma unroll
-          for (int j = 0; j < E / 2; ++j) acc[q][j] = add2(acc[q][j], v[j]);
-          const int k = k0 + q * LPT * E, n = a.d - k;
-          if ((ends || stops) && n > 0) {
-            float f[E];
-#pragma unroll
-            for (int j = 0; j < E / 2; ++j) {
-              const float2 w = unpack2(acc[q][j]);
-              f[2 * j] = w.x;
-              f[2 * j + 1] = w.y;
-            }
-            if (ends && !open) {
-              write_columns<TW, E>(a, word[u], k, n, f);
-            } else {
-              float* p = a.part + (c * 2 + (open ? 0 : 1)) * a.part_ld + k;
-#pragma unroll
-              for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
-            }
-          }
-          if (ends) {
-#pragma unroll
-            for (int j = 0; j < E / 2; ++j) acc[q][j] = 0;
-          }
-        }
-        if (ends) open = false;
+        for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
       }
     }
-    if (s + AHEAD < steps) {
-      fetch(s + AHEAD, slot, ahead);
-      entries(lo + (int64_t)(s + AHEAD + 1) * kStep, ahead);
+  };
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    copies_wait<AHEAD - 1>();
+    const uint4* at = ring + slot * SLOT + threadIdx.x;
+    const uint32_t bits = ends >> (slot * kStep);
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {                    // rows that are not there are zeros
+#pragma unroll
+      for (int q = 0; q < NU; ++q) {
+        uint64_t v[E / 2];
+        unpack_unit<T>(at[(u * NU + q) * 256], v);
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) acc[q][j] = add2(acc[q][j], v[j]);
+      }
+      if (bits >> u & 1) {
+        put(order[s * kStep + u].x, open ? 0 : -1);
+        open = false;
+      }
     }
+    if (s + AHEAD < steps) fetch(s + AHEAD, slot);
     copies_commit();
     slot = slot + 1 == AHEAD ? 0 : slot + 1;
   }
+  const uint32_t last = order[rows - 1].x;
+  if (last < a.V && order[rows].x == last) put(last, open ? 0 : 1);
 }
 
 // Warp w of block b looks at the end of chunk 8 b + w: where a run that began in that chunk goes over it, its parts (one for each chunk that it reaches) are added up,
@@ -583,7 +605,7 @@ joints_kernel(const RunArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
   };
-  auto word_at = [&](int64_t i) { return i >= 0 && i < a.T ? a.order[i].x : 0xFFFFFFFFu; };
+  auto word_at = [&](int64_t i) { return i >= 0 && i < a.T ? a.order[i].x : kNoWord; };
   const int64_t c = (int64_t)blockIdx.x * 8 + warp, lo = c * a.chunk, hi = lo + a.chunk;
   const uint32_t word = word_at(hi - 1), next = word_at(hi), first = word_at(lo), prev = word_at(lo - 1);
   int64_t m = 0;                                         // parts

@@ -270,10 +270,11 @@ __device__ __forceinline__ float both(uint64_t v) {
 // has no use for whole rows, so that a row may be cut into segments of LANES * NG units (blockIdx.y).
 enum { WHOLE, SUMMED, ADDED, DROPPED };
 template <int MODE> constexpr int kTensors = MODE == SUMMED || MODE == ADDED ? 2 : 1;
+template <int MODE> constexpr bool kNorm = MODE == WHOLE || MODE == SUMMED;
 template <typename T, int MODE, int LANES, int NG, int RB, int STAGES, int THREADS, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
 fwd_kernel(const FwdArgs a) {
-  constexpr bool SUM = MODE != WHOLE, NORM = MODE == WHOLE || MODE == SUMMED, RES = kTensors<MODE> == 2;
+  constexpr bool SUM = MODE != WHOLE, NORM = kNorm<MODE>, RES = kTensors<MODE> == 2;
   constexpr int ROWS = THREADS / LANES, E = kUnit<T>, H = kPairs<T>, ROW = NG * THREADS, SIZE = kTensors<MODE> * RB * ROW;
   extern __shared__ uint4 ring[];                        // [STAGES][X and R][RB][NG][THREADS]
   __shared__ float scratch[2][RB][32];

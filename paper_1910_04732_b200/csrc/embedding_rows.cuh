@@ -588,14 +588,14 @@ joints_kernel(const RunArgs a) {
   const int k = (blockIdx.y * LPT + l) * 8, n = a.d - k;
   float acc[8];
   // parts [p0, p1) of a run that begins in chunk c: part 0 is its share of that chunk, part p its share of the p-th behind
+  auto part_at = [&](int64_t c, int64_t p) { return reinterpret_cast<const float4*>(a.part + ((c + p) * 2 + (p == 0 ? 1 : 0)) * a.part_ld + k); };
   auto sum = [&](int64_t c, int64_t p0, int64_t p1) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     if (n > 0) {
 #pragma unroll 8
       for (int64_t p = p0; p < p1; ++p) {
-        const float4* at = reinterpret_cast<const float4*>(a.part + ((c + p) * 2 + (p == 0 ? 1 : 0)) * a.part_ld + k);
-        const float4 u = at[0], v = at[1];
+        const float4 u = part_at(c, p)[0], v = part_at(c, p)[1];
         acc[0] += u.x; acc[1] += u.y; acc[2] += u.z; acc[3] += u.w;
         acc[4] += v.x; acc[5] += v.y; acc[6] += v.z; acc[7] += v.w;
       }
@@ -607,16 +607,29 @@ joints_kernel(const RunArgs a) {
   };
   auto word_at = [&](int64_t i) { return i >= 0 && i < a.T ? a.order[i].x : kNoWord; };
   const int64_t c = (int64_t)blockIdx.x * 8 + warp, lo = c * a.chunk, hi = lo + a.chunk;
+  // everything that most runs need is asked for at once: the words around, the words that the 32 chunks behind begin with, the first two parts
   const uint32_t word = word_at(hi - 1), next = word_at(hi), first = word_at(lo), prev = word_at(lo - 1);
+  uint32_t begins = word_at((c + 1 + lane) * a.chunk);
+  float4 two[4] = {};
+  if (n > 0 && c + 1 < a.chunks) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) two[i] = part_at(c, i >> 1)[i & 1];
+  }
   int64_t m = 0;                                         // parts
   if (word < a.V && next == word && !(first == word && prev == word)) {
-    for (m = 1;; m += 32) {
-      const unsigned on = __ballot_sync(0xffffffffu, word_at((c + m + lane) * a.chunk) == word);
+    for (m = 1;; m += 32, begins = word_at((c + m + lane) * a.chunk)) {
+      const unsigned on = __ballot_sync(0xffffffffu, begins == word);
       if (on == 0xffffffffu) continue;
       m += __ffs(~on) - 1;
       break;
     }
-    if (m <= kFewParts * G) {
+    if (m == 2) {
+      if (group == 0 && n > 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = reinterpret_cast<const float*>(two)[j] + reinterpret_cast<const float*>(two + 2)[j];
+        write_columns<TW, 8>(a, word, k, n, acc);
+      }
+    } else if (m <= kFewParts * G) {
       const int64_t per = (m + G - 1) / G;
       sum(c, min(m, group * per), min(m, (group + 1) * per));
       if (group == 0 && n > 0) write_columns<TW, 8>(a, word, k, n, acc);

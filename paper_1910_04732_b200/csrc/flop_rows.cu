@@ -94,13 +94,13 @@ EmbWs plan_emb_ws(Arena& ar, int64_t T, int64_t d) {
 
 // Batches of up to 8 x 2048 tokens by one cluster; longer ones by two launches a digit.
 constexpr int kSortCluster = 8;
-int launch_sort(const emb::SortArgs& a, int zero_blocks, cudaStream_t st) {
+int launch_sort(const emb::SortArgs& a, int beside, cudaStream_t st) {
   static OncePerDevice configured;
   FLOP_TRY(allow_smem(configured, emb::sort_smem(emb::kMaxDigitBits), emb::sort_kernel, emb::sort_count_kernel, emb::sort_move_kernel));
   const size_t smem = emb::sort_smem(a.bits);
   if (a.blocks > kSortCluster) {
     for (int pass = 0; pass < a.passes; ++pass) {
-      launch_k(emb::sort_count_kernel, dim3((unsigned)(a.blocks + (pass == 0 ? zero_blocks : 0))), dim3(emb::kSortThreads), smem, st, a, pass);
+      launch_k(emb::sort_count_kernel, dim3((unsigned)(a.blocks + (pass == 0 ? beside : 0))), dim3(emb::kSortThreads), smem, st, a, pass);
       FLOP_TRY(launched());
       launch_k(emb::sort_move_kernel, dim3((unsigned)a.blocks), dim3(emb::kSortThreads), smem, st, a, pass);
       FLOP_TRY(launched());
@@ -108,7 +108,7 @@ int launch_sort(const emb::SortArgs& a, int zero_blocks, cudaStream_t st) {
     return FLOP_OK;
   }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(a.blocks + zero_blocks / a.blocks * a.blocks));
+  cfg.gridDim = dim3((unsigned)(a.blocks + beside / a.blocks * a.blocks));
   cfg.blockDim = dim3(emb::kSortThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -190,9 +190,11 @@ constexpr NormShape bwd_shape(int lanes, int ng, int dt) {
   const int rb = between(1, (lanes > 32 && dt == FLOP_BF16 ? 4 : 2) / ng, 4);
   return {rb, 1, between(1, kRing / (3 * rb * ng * bwd_threads(lanes, ng) * 16), 4)};
 }
+// No more blocks than an equal share of the batches needs: 333 batches on 148 places are three each for 111 blocks.
 int64_t norm_blocks(int lanes, int threads, int64_t T, const NormShape& s) {
-  const int64_t rows = (int64_t)(threads / lanes) * s.rb;
-  return std::min<int64_t>((T + rows - 1) / rows, (int64_t)num_sms() * s.blocks);
+  const int64_t rows = (int64_t)(threads / lanes) * s.rb, batches = (T + rows - 1) / rows, most = (int64_t)num_sms() * s.blocks;
+  const int64_t each = (batches + most - 1) / most;
+  return (batches + each - 1) / each;
 }
 // Parts of the column sums: one for each block that holds rows; where rows are walked, enough blocks for the machine, 64 rows each at least.
 int64_t norm_parts(int64_t T, int64_t d, int dt) {
@@ -356,9 +358,11 @@ int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t
   s.blocks = 1;
   while (s.blocks < kSortCluster && s.blocks < blocks) s.blocks *= 2;
   if (blocks > kSortCluster) s.blocks = (int)std::min<int64_t>(blocks, emb::kSortBlocks);
-  const int64_t pieces = z.rows * ((z.row_bytes + 15) / 16), most = (int64_t)num_sms() * 32;
-  const int zero_blocks = (int)std::min<int64_t>(round_up((pieces + 4 * emb::kSortThreads - 1) / (4 * emb::kSortThreads), s.blocks), most);
-  FLOP_TRY(launch_sort(s, zero_blocks, st));
+  // Blocks that clear dE beside the sort, a tile for each, up to 32 for an SM.  (Asking for rows of dY ahead of time there as well made the sort slower by more than the rows
+  // then came sooner: 16384 tokens of 205 words, 2048 columns 38 us, 27 without.)
+  const int64_t tiles = (z.rows * ((z.row_bytes + 15) / 16) + 4 * emb::kSortThreads - 1) / (4 * emb::kSortThreads);
+  const int beside = (int)std::min<int64_t>(round_up(tiles, s.blocks), (int64_t)num_sms() * 32);
+  FLOP_TRY(launch_sort(s, beside, st));
   return typed([&](auto t, auto tw) { return launch_runs<decltype(t), decltype(tw)>(a, p.lanes, st); });
 }
 

@@ -12,6 +12,8 @@ compaction once, then the compact forward against the uncompacted gated forward
 (both replayed from CUDA graphs so that host launch cost does not hide the kernels).
 The third table is one training step of a BERT-shaped layer on the active rank
 components only, against the dense gated step, for several fractions of open gates.
+The last one times the operators on token rows (lookup in a dense table and its gradient,
+dropout, layer norm) at the workloads' token counts and widths.
 """
 from __future__ import annotations
 
@@ -159,6 +161,7 @@ def main():
     for wl in ("bert", "sru"):
         active_table(I.WORKLOADS[wl], g)
     embedding_table(g)
+    rows_table(g, peak)
     assert b.device_status() == b.OK
 
 
@@ -230,6 +233,43 @@ def embedding_table(g):
         tb = timed(lambda: b.gated_embedding_bwd(dY, ids, E, O_, z, dzd, H, dE, dO, dla, ws), iters=20, graph=True)
         flops = 6.0 * T * d_i * d          # one forward and two backward GEMMs
         print(f"{f'n={n_rows}, d_i={d_i}':>22s} {tf * 1e6:8.1f} {tb * 1e6:8.1f} {flops / (tf + tb) / 1e12:16.0f}")
+
+
+def rows_table(g, peak):
+    """Operators on token rows at the workloads' sizes, replayed; bytes are what a call has to read and write once.  Calls of a few
+    megabytes find their tensors in the second-level cache, so their rate can exceed the memory's."""
+    bf = torch.bfloat16
+    print(f"\noperators on token rows, bf16, graph replay (share of {peak:.0f} GB/s)")
+    print(f"{'operator':>34s} {'us':>8s} {'GB/s':>7s} {'share':>6s}")
+
+    def row(name, nbytes, fn):
+        t = timed(fn, iters=20, graph=True)
+        print(f"{name:>34s} {t * 1e6:8.1f} {nbytes / t / 1e9:7.0f} {nbytes / t / 1e9 / peak:6.2f}")
+
+    for name in ("bert", "txl", "sru"):
+        w = I.WORKLOADS[name]
+        T, d = w.T, w.matrices[0].d_in
+        X, R, S, Y, dY, dX, dR = (b.padded(T, d, bf) for _ in range(7))
+        for t in (X, R, dY):
+            t.copy_(torch.randn(T, d, generator=g, device="cuda"))
+        weight, bias, dw, db = (torch.ones(d, device="cuda") for _ in range(4))
+        stats, ws = torch.empty(T, 2, device="cuda"), b.alloc_workspace(b.workspace_bytes(b.OP_LAYER_NORM_BWD, T, d, 0, 0, b.BF16))
+        mask, n = dict(p=0.1, seed=1, offset=0), 2 * T * d
+        row(f"dropout {T} x {d}", 2 * n, lambda: b.dropout_fwd(X, Y, **mask))
+        row("dropout + residual", 3 * n, lambda: b.dropout_fwd(X, Y, R=R, **mask))
+        row("norm forward", 2 * n, lambda: b.layer_norm_fwd(X, weight, bias, 1e-5, Y, stats))
+        row("norm backward", 3 * n, lambda: b.layer_norm_bwd(dY, X, stats, weight, dX, dw, db, ws))
+        row("norm + dropout + residual forward", 4 * n, lambda: b.layer_norm_fwd(X, weight, bias, 1e-5, Y, stats, R=R, S=S, **mask))
+        row("norm + dropout + residual backward", 4 * n, lambda: b.layer_norm_bwd(dY, S, stats, weight, dX, dw, db, ws, dR=dR, **mask))
+    T, d = 64 * 256, 1024
+    for n_rows in (205, 40000, 200000):
+        E, dE, Y, dY = (b.padded(rows, d, bf) for rows in (n_rows, n_rows, T, T))
+        dY.copy_(torch.randn(T, d, generator=g, device="cuda"))
+        ids = (torch.rand(T, generator=g, device="cuda") ** 4 * n_rows).to(torch.int32).clamp_(0, n_rows - 1)
+        used = int(ids.unique().numel())
+        ws = b.alloc_workspace(b.workspace_bytes(b.OP_EMBEDDING_SORTED_BWD, T, d, 0, n_rows, b.BF16))
+        row(f"lookup {T} of {n_rows} x {d}", 2 * d * (T + used) + 4 * T, lambda: b.embedding_fwd(ids, E, 32.0, Y))
+        row("gradient of the table", 2 * d * (T + n_rows) + 4 * T, lambda: b.embedding_bwd(dY, ids, 32.0, dE, ws))
 
 
 def active_table(w, g):

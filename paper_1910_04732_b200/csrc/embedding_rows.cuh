@@ -20,74 +20,51 @@ namespace flop {
 namespace emb {
 
 // ---------------------------------------------------------------- lookup
-struct Walk {
-  int64_t total;                    // units of all rows
-  int per_row;                      // units of a row
-  int64_t tile_rows, near_rows;     // the grid's stride, and 256 units, as rows and units of a row
-  int tile_units, near_units;
-};
-struct At {
-  int64_t i, t;
-  int c;
-  __device__ __forceinline__ void step(int64_t units, int64_t rows, int rest, int per_row) {
-    i += units;
-    t += rows;
-    c += rest;
-    if (c >= per_row) { c -= per_row; ++t; }
-  }
-};
 struct LookupArgs {
   const int32_t* ids; int64_t T;
   const void* E; int64_t lde; int64_t V;
   void* Y; int64_t ldy;
   float scale;
   int d, vec;
-  Walk walk;
 };
 
-// A walk over the units of all rows: a block takes tiles of U x 256 units in turn, unit j of a thread 256 behind unit j - 1; first the words of all U, then their rows.
-// Positions are (row, unit of the row), carried from tile to tile without divisions.  (A ring of tiles copied ahead, which carries the other operators
-// here, is slower: a row's address waits for its word, 16384 x 2048 bf16 16.5 us, 21 with the ring.  Writing alone bounds it: 5.9 TB/s.)
-template <typename T, int U>
+// LANES threads share a row of Y, NG units each (blockIdx.y: segments of LANES * NG units); a block takes RB rows of each set of threads, first their words, then all their
+// units, then stores.  (A ring of rows copied ahead, which carries the other operators here, is slower: a row's address waits for its word.  Units dealt out
+// over all rows without regard to where rows end cost 100 instructions each: 16384 x 2048 bf16 of 205 rows 16.3 us.)
+template <typename T, int LANES, int NG, int RB>
 __global__ void __launch_bounds__(256)
 lookup_kernel(const LookupArgs a) {
+  constexpr int ROWS = 256 / LANES, E = kUnit<T>, H = kPairs<T>;
   pdl_wait();
   pdl_launch_dependents();
-  constexpr int H = kPairs<T>;
+  const int k = (threadIdx.x % LANES + blockIdx.y * (LANES * NG)) * E;
+  const int64_t t0 = (int64_t)blockIdx.x * (ROWS * RB) + threadIdx.x / LANES;
   const uint64_t scale = pack2(a.scale, a.scale);
-  At at;
-  at.i = (int64_t)blockIdx.x * (U * 256) + threadIdx.x;
-  at.t = at.i / a.walk.per_row;
-  at.c = (int)(at.i - at.t * a.walk.per_row);
-  const int64_t stride = (int64_t)gridDim.x * (U * 256);
-  for (int64_t first = (int64_t)blockIdx.x * (U * 256); first < a.walk.total; first += stride) {
-    int64_t row[U];
-    int k[U], id[U];
-    At it = at;
+  int id[RB];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      row[u] = it.t;
-      k[u] = it.c * kUnit<T>;
-      id[u] = it.t < a.T ? a.ids[it.t] : -1;
-      it.step(256, a.walk.near_rows, a.walk.near_units, a.walk.per_row);
-    }
-    uint4 x[U];
+  for (int q = 0; q < RB; ++q) id[q] = t0 + q * ROWS < a.T ? a.ids[t0 + q * ROWS] : -1;
+  uint4 x[RB][NG];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool word = id[u] >= 0 && id[u] < a.V;
-      x[u] = load_unit((const T*)a.E + (int64_t)(word ? id[u] : 0) * a.lde + k[u], word ? a.d - k[u] : 0, a.vec, id[u] + 1 < a.V);
-    }
+  for (int q = 0; q < RB; ++q) {
+    const bool word = id[q] >= 0 && id[q] < a.V;
+    const T* row = (const T*)a.E + (int64_t)(word ? id[q] : 0) * a.lde + k;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int i = 0; i < NG; ++i) x[q][i] = load_unit(row + i * LANES * E, word ? a.d - k - i * LANES * E : 0, a.vec, id[q] + 1 < a.V);
+  }
+#pragma unroll
+  for (int q = 0; q < RB; ++q) {
+    if (t0 + q * ROWS >= a.T) break;
+    const bool word = id[q] >= 0 && id[q] < a.V;         // zeros for padding, also where the scale is not finite
+    T* row = (T*)a.Y + (t0 + q * ROWS) * a.ldy + k;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
       uint64_t v[H];
-      unpack_unit<T>(x[u], v);
-      const bool word = id[u] >= 0 && id[u] < a.V;       // zeros for padding, also where the scale is not finite
+      unpack_unit<T>(x[q][i], v);
 #pragma unroll
       for (int j = 0; j < H; ++j) v[j] = word ? mul2(v[j], scale) : 0;
-      const int n = row[u] < a.T ? a.d - k[u] : 0;
-      if (n > 0) store_unit((T*)a.Y + row[u] * a.ldy + k[u], pack_unit<T>(v), n, a.vec);
+      const int n = a.d - k - i * LANES * E;
+      if (n > 0) store_unit(row + i * LANES * E, pack_unit<T>(v), n, a.vec);
     }
-    at.step(stride, a.walk.tile_rows, a.walk.tile_units, a.walk.per_row);
   }
 }
 

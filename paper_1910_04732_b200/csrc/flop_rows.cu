@@ -34,6 +34,8 @@ bool apart(const RowsArg& a, const RowsArg& b, int64_t T, int64_t d) { return !a
 int64_t groups_of(int64_t d) { return (d + 7) / 8; }
 int64_t units_of(int64_t d, int dt) { return (d * (int64_t)elt(dt) + 15) / 16; }
 
+template <typename T> constexpr int kType = sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32;
+
 bool valid_p(float p) { return p >= 0.f && p < 1.f; }
 Drop make_drop(float p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev) {
   Drop d{};
@@ -51,20 +53,27 @@ int launched() {
 }
 
 // ---------------------------------------------------------------- embedding
-template <typename T>
-int launch_lookup(emb::LookupArgs& a, int64_t per_row, cudaStream_t st) {
-  constexpr int U = 4;
-  constexpr int64_t tile = 256 * U;
-  emb::Walk& w = a.walk;
-  w.per_row = (int)per_row;
-  w.total = a.T * per_row;
-  const int64_t blocks = std::min<int64_t>((w.total + tile - 1) / tile, (int64_t)num_sms() * 8);
-  w.tile_rows = blocks * tile / per_row;
-  w.tile_units = (int)(blocks * tile - w.tile_rows * per_row);
-  w.near_rows = 256 / per_row;
-  w.near_units = (int)(256 - w.near_rows * per_row);
-  launch_k(emb::lookup_kernel<T, U>, dim3((unsigned)blocks), dim3(256), (size_t)0, st, a);
+template <typename T, int LANES, int NG>
+int launch_lookup_as(const emb::LookupArgs& a, int64_t units, cudaStream_t st) {
+  constexpr int RB = 4, rows = 256 / LANES * RB;
+  // a row for each set of threads where four would leave the machine without a round of blocks
+  const int64_t segments = (units + LANES * NG - 1) / (LANES * NG);
+  if ((a.T + rows - 1) / rows * segments < num_sms()) {
+    launch_k(emb::lookup_kernel<T, LANES, NG, 1>, dim3((unsigned)((a.T + rows / RB - 1) / (rows / RB)), (unsigned)segments), dim3(256), (size_t)0, st, a);
+  } else {
+    launch_k(emb::lookup_kernel<T, LANES, NG, RB>, dim3((unsigned)((a.T + rows - 1) / rows), (unsigned)segments), dim3(256), (size_t)0, st, a);
+  }
   return launched();
+}
+template <typename T>
+int launch_lookup(const emb::LookupArgs& a, int64_t units, cudaStream_t st) {
+  if (units <= 4) return launch_lookup_as<T, 4, 1>(a, units, st);
+  if (units <= 8) return launch_lookup_as<T, 8, 1>(a, units, st);
+  if (units <= 16) return launch_lookup_as<T, 16, 1>(a, units, st);
+  if (units <= 32) return launch_lookup_as<T, 32, 1>(a, units, st);
+  if (units <= 64) return launch_lookup_as<T, 32, 2>(a, units, st);
+  if (units <= 96) return launch_lookup_as<T, 32, 3>(a, units, st);
+  return launch_lookup_as<T, 64, 2>(a, units, st);
 }
 
 struct RunPlan { int lanes, slices, chunk; int64_t chunks; };
@@ -155,7 +164,7 @@ int launch_few(emb::RunArgs a, cudaStream_t st) {
 // ---------------------------------------------------------------- layer norm
 // How a row is held: by `lanes` threads with `ng` units of 16 bytes each, in blocks of `threads`; lanes 0: rows too wide for that, which are walked.
 struct NormPlan { int lanes, ng, threads; };
-NormPlan plan_norm(int64_t units) {
+NormPlan plan_norm(int64_t units, int dt) {
   if (units <= 8) return {8, 1, 128};
   if (units <= 16) return {16, 1, 128};
   if (units <= 32) return {32, 1, 128};
@@ -169,6 +178,9 @@ NormPlan plan_norm(int64_t units) {
   if (units <= 1024) return {512, 2, 512};
   if (units <= 1536) return {512, 3, 512};
   if (units <= 2048) return {512, 4, 512};
+  // a thread's units of fp32 take half the registers: 1024 x 16384 forward and backward 81 us, 118 walked
+  if (dt == FLOP_F32 && units <= 3072) return {1024, 3, 1024};
+  if (dt == FLOP_F32 && units <= 4096) return {1024, 4, 1024};
   return {0, 0, 0};
 }
 #define FLOP_HELD_PLANS(X) X(8, 1, 128) X(16, 1, 128) X(32, 1, 128) X(32, 2, 128) X(32, 3, 128) X(64, 2, 64) X(128, 2, 128) X(128, 3, 128) X(256, 2, 256) X(256, 3, 256) \
@@ -184,7 +196,7 @@ constexpr NormShape fwd_shape(int ng, int threads, int tensors, int per_sm = 512
 }
 // One block on an SM, so that there are few parts of the column sums to add up: 512 threads, or, where a thread's three units take more than 128
 // registers, 384 (4096 x 768 bf16 15.0 us, 16.7 with 512 threads that spill).
-constexpr int bwd_threads(int lanes, int ng) { return ng < 3 || lanes == 512 ? 512 : 384 / lanes > 0 ? 384 / lanes * lanes : lanes; }
+constexpr int bwd_threads(int lanes, int ng) { return lanes > 512 ? lanes : ng < 3 || lanes == 512 ? 512 : 384 / lanes > 0 ? 384 / lanes * lanes : lanes; }
 // Two rows at once for every barrier among the warps that share one (16384 x 2048 bf16: 43.0 us, 44.5 one by one); fp32 rows are twice the bytes.
 constexpr NormShape bwd_shape(int lanes, int ng, int dt) {
   const int rb = between(1, (lanes > 32 && dt == FLOP_BF16 ? 4 : 2) / ng, 4);
@@ -198,7 +210,7 @@ int64_t norm_blocks(int lanes, int threads, int64_t T, const NormShape& s) {
 }
 // Parts of the column sums: one for each block that holds rows; where rows are walked, enough blocks for the machine, 64 rows each at least.
 int64_t norm_parts(int64_t T, int64_t d, int dt) {
-  const NormPlan p = plan_norm(units_of(d, dt));
+  const NormPlan p = plan_norm(units_of(d, dt), dt);
   if (p.lanes) return norm_blocks(p.lanes, bwd_threads(p.lanes, p.ng), T, bwd_shape(p.lanes, p.ng, dt));
   const int64_t slabs = std::max<int64_t>((groups_of(d) + 31) / 32, 1);
   return std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, std::max<int64_t>(1, (int64_t)num_sms() * 4 / slabs)));
@@ -231,7 +243,7 @@ int launch_fwd_held(const norm::FwdArgs& a, unsigned segments, cudaStream_t st) 
 // Dropout by itself: rows of more than 256 units in segments of 256.
 template <typename T, int MODE>
 int launch_dropout(const norm::FwdArgs& a, cudaStream_t st) {
-  const int64_t units = units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32);
+  const int64_t units = units_of(a.d, kType<T>);
   if (units <= 8) return launch_fwd_held<T, MODE, 8, 1, 128>(a, 1, st);
   if (units <= 16) return launch_fwd_held<T, MODE, 16, 1, 128>(a, 1, st);
   if (units <= 32) return launch_fwd_held<T, MODE, 32, 1, 128>(a, 1, st);
@@ -242,9 +254,10 @@ int launch_dropout(const norm::FwdArgs& a, cudaStream_t st) {
 }
 template <typename T, bool SUM>
 int launch_norm_fwd(const norm::FwdArgs& a, cudaStream_t st) {
-  const NormPlan p = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32));
+  const NormPlan p = plan_norm(units_of(a.d, kType<T>), kType<T>);
 #define FLOP_HELD(L, N, B) if (p.lanes == L && p.ng == N) return launch_fwd_held<T, SUM ? norm::SUMMED : norm::WHOLE, L, N, B>(a, 1, st);
   FLOP_HELD_PLANS(FLOP_HELD)
+  if constexpr (sizeof(T) == 4) { FLOP_HELD(1024, 3, 1024) FLOP_HELD(1024, 4, 1024) }
 #undef FLOP_HELD
   launch_k(norm::fwd_walk_kernel<T, SUM>, dim3((unsigned)a.T), dim3(walk_threads(a.groups)), (size_t)0, st, a);
   return launched();
@@ -253,7 +266,7 @@ int launch_norm_fwd(const norm::FwdArgs& a, cudaStream_t st) {
 template <typename T, int LANES, int NG>
 int launch_norm_bwd_held(const norm::BwdArgs& a, cudaStream_t st) {
   constexpr int THREADS = bwd_threads(LANES, NG);
-  constexpr NormShape s = bwd_shape(LANES, NG, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32);
+  constexpr NormShape s = bwd_shape(LANES, NG, kType<T>);
   auto kern = norm::bwd_kernel<T, LANES, NG, s.rb, s.stages, THREADS, s.blocks>;
   constexpr size_t tensor = (size_t)s.stages * s.rb * NG * THREADS * 16;
   static OncePerDevice configured;
@@ -263,9 +276,10 @@ int launch_norm_bwd_held(const norm::BwdArgs& a, cudaStream_t st) {
 }
 template <typename T>
 int launch_norm_bwd_rows(const norm::BwdArgs& a, cudaStream_t st) {
-  const NormPlan p = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32));
+  const NormPlan p = plan_norm(units_of(a.d, kType<T>), kType<T>);
 #define FLOP_HELD(L, N, B) if (p.lanes == L && p.ng == N) return launch_norm_bwd_held<T, L, N>(a, st);
   FLOP_HELD_PLANS(FLOP_HELD)
+  if constexpr (sizeof(T) == 4) { FLOP_HELD(1024, 3, 1024) FLOP_HELD(1024, 4, 1024) }
 #undef FLOP_HELD
   if (a.n_part) {     // before the rows, whose outputs may take the place of what the sums read
     launch_k(norm::bwd_columns_kernel<T>, dim3((unsigned)((a.groups + 31) / 32), (unsigned)a.n_part), dim3(256), (size_t)0, st, a);
@@ -280,7 +294,7 @@ int launch_norm_bwd_rows(const norm::BwdArgs& a, cudaStream_t st) {
 template <typename T>
 int launch_norm_bwd(const norm::BwdArgs& a, cudaStream_t st) {
   if (a.n_part || a.dX || a.dR) FLOP_TRY(launch_norm_bwd_rows<T>(a, st));
-  const bool held = plan_norm(units_of(a.d, sizeof(T) == 2 ? FLOP_BF16 : FLOP_F32)).lanes > 0;
+  const bool held = plan_norm(units_of(a.d, kType<T>), kType<T>).lanes > 0;
   if (a.n_part > 1 || (a.n_part && !held)) {       // a single block that holds rows has written the sums itself
     launch_k(norm::bwd_finish_kernel, dim3((unsigned)((a.d + 31) / 32), 2), dim3(32 * norm::kFinishWarps), (size_t)0, st, (const float*)a.part, a.part_ld, a.n_part, a.d, a.dweight,
              a.dbias, a.accumulate);

@@ -29,6 +29,13 @@ def test_norm_widths(b, kind, per, units):
     check_norm(b, kind, 3, units * per, "plain")
 
 
+@pytest.mark.parametrize("units", [3072, 4096])
+def test_norm_widths_of_wide_fp32_rows(b, units):
+    for d in (units * 4 - 1, units * 4, units * 4 + 1):
+        check_norm(b, "f32", 3, d, "pre", 0.2)
+    check_norm(b, "f32", 300, units * 4 - 6, "plain")
+
+
 @pytest.mark.parametrize("T", [1, 2, 147, 148, 149, 1184, 2368, 2369, 4737])
 @pytest.mark.parametrize("d", [24, 264, 1032])
 def test_norm_batches(b, T, d):

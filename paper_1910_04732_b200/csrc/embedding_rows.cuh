@@ -2,7 +2,7 @@
 // Words outside the table are padding: a row of zeros, no gradient.
 //
 // The gradient sorts the tokens by word (stably: a word's tokens stay in the order of the batch) and adds up runs of equal words.  Every
-// sum is taken in fp32 in an order that depends on the sizes only, every row is written once, and there are no atomics on sums.
+// sum is taken in fp32 in an order that depends on the sizes only, and every row is written once, by one thread for each column.
 //   sort_kernel   : one thread-block cluster sorts (word, token) pairs, least significant digit first; the blocks behind it clear dE
 //                   meanwhile, because most rows of a large table stay empty.  Long batches are sorted by two launches a digit (sort_count_kernel,
 //                   sort_move_kernel) on as many blocks as they fill
@@ -10,7 +10,7 @@
 //                   as well spread over the machine as a batch of rare ones.  A run that lies within a chunk is written to dE; what a chunk holds of
 //                   a run that crosses its border goes to the workspace
 //   joints_kernel : adds up the parts of the runs that cross borders, in order
-//   few_kernel    : few tokens need none of this: a block for each token looks through all words, and the first of equal ones adds up
+//   few_kernel    : few tokens need none of this: a warp for each token looks through all words, and the first of equal ones adds up
 #pragma once
 #include <cooperative_groups.h>
 
@@ -69,7 +69,7 @@ lookup_kernel(const LookupArgs a) {
 }
 
 // ---------------------------------------------------------------- rows of zeros
-struct ClearArgs { unsigned char* p; int64_t rows, row_bytes, pitch; int vec; };   // vec: rows start on 16 bytes
+struct ClearArgs { unsigned char* p; int64_t rows, row_bytes, pitch; int vec; };   // vec: rows start on 16 bytes; else they are fp32
 
 // The last bytes of a row, an even number below 16.
 __device__ __forceinline__ void clear_tail(unsigned char* at, int64_t left) {
@@ -77,31 +77,29 @@ __device__ __forceinline__ void clear_tail(unsigned char* at, int64_t left) {
   if (left & 4) { *reinterpret_cast<uint32_t*>(at) = 0; at += 4; }
   if (left & 2) *reinterpret_cast<uint16_t*>(at) = 0;
 }
+// Piece i of a row: 16 bytes, or what is left of them at its end; a value where rows do not start on 16 bytes.
+__device__ __forceinline__ void clear_piece(unsigned char* row, int64_t i, const ClearArgs& a) {
+  const int64_t left = a.row_bytes - i * 16;
+  if (!a.vec) *reinterpret_cast<uint32_t*>(row + i * 4) = 0;
+  else if (left >= 16) *reinterpret_cast<uint4*>(row + i * 16) = make_uint4(0, 0, 0, 0);
+  else clear_tail(row + i * 16, left);
+}
 // Rows [0, rows) from p on but those that `skip` names, by `step` threads of which this is the first-th: a warp for a row, or a thread for a piece of a short one.
 template <typename Skip>
 __device__ __forceinline__ void clear_rows(unsigned char* p, int64_t rows, const ClearArgs& a, int64_t first, int64_t step, Skip&& skip) {
-  if (a.vec && a.row_bytes >= 512) {
-    const int lane = threadIdx.x & 31, whole = (int)(a.row_bytes / 16);
+  const int64_t pieces = a.vec ? (a.row_bytes + 15) / 16 : a.row_bytes / 4;
+  if (pieces >= 32) {
     for (int64_t r = first / 32; r < rows; r += step / 32) {
       if (skip(r)) continue;
-      unsigned char* row = p + r * a.pitch;
 #pragma unroll 4
-      for (int i = lane; i < whole; i += 32) reinterpret_cast<uint4*>(row)[i] = make_uint4(0, 0, 0, 0);
-      if (lane == 0) clear_tail(row + (int64_t)whole * 16, a.row_bytes & 15);
+      for (int64_t i = threadIdx.x & 31; i < pieces; i += 32) clear_piece(p + r * a.pitch, i, a);
     }
     return;
   }
-  const int64_t pieces = a.vec ? (a.row_bytes + 15) / 16 : a.row_bytes / 2, total = rows * pieces;
-  int64_t i = first, row = i / pieces, piece = i - row * pieces;
-  const int64_t step_rows = step / pieces, step_pieces = step - step_rows * pieces;
-  for (; i < total; i += step) {
-    if (!skip(row)) {
-      unsigned char* at = p + row * a.pitch + piece * (a.vec ? 16 : 2);
-      const int64_t left = a.row_bytes - piece * 16;
-      if (!a.vec) *reinterpret_cast<uint16_t*>(at) = 0;
-      else if (left >= 16) *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
-      else clear_tail(at, left);
-    }
+  const int64_t total = rows * pieces, step_rows = step / pieces, step_pieces = step - step_rows * pieces;
+  int64_t row = first / pieces, piece = first - row * pieces;
+  for (int64_t i = first; i < total; i += step) {
+    if (!skip(row)) clear_piece(p + row * a.pitch, piece, a);
     row += step_rows;
     piece += step_pieces;
     if (piece >= pieces) { piece -= pieces; ++row; }
@@ -111,9 +109,9 @@ __device__ __forceinline__ void clear_rows(unsigned char* p, int64_t rows, const
 // (Writing alone, the memory takes 5.9 TB/s of such tiles, and 4.2 of tiles of a megabyte.)
 __device__ __forceinline__ void clear_all(const ClearArgs& a, int64_t block, int64_t blocks) {
   const int threads = blockDim.x;
-  if (a.vec && a.pitch == a.row_bytes) {
-    const int64_t bytes = a.rows * a.row_bytes, pieces = bytes / 16;
-    uint4* p = reinterpret_cast<uint4*>(a.p);
+  if (a.pitch == a.row_bytes) {
+    const int64_t bytes = a.rows * a.row_bytes, head = min(bytes, (int64_t)(-reinterpret_cast<uintptr_t>(a.p) & 15)), pieces = (bytes - head) / 16;
+    uint4* p = reinterpret_cast<uint4*>(a.p + head);
     for (int64_t t = block * threads * 4; t < pieces; t += blocks * threads * 4) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -121,7 +119,10 @@ __device__ __forceinline__ void clear_all(const ClearArgs& a, int64_t block, int
         if (i < pieces) p[i] = make_uint4(0, 0, 0, 0);
       }
     }
-    if (block == 0 && threadIdx.x == 0) clear_tail(a.p + pieces * 16, bytes & 15);
+    if (block == 0 && threadIdx.x == 0) {
+      for (int64_t i = 0; i < head; i += 2) *reinterpret_cast<uint16_t*>(a.p + i) = 0;
+      clear_tail(a.p + head + pieces * 16, (bytes - head) & 15);
+    }
   } else {
     clear_rows(a.p, a.rows, a, block * threads + threadIdx.x, blocks * threads, [](int64_t) { return false; });
   }

@@ -418,6 +418,10 @@ int flop_layer_norm_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, 
     return FLOP_ERR_UNSUPPORTED;
   if (!in_place_or_apart(s, x, T, d) || !in_place_or_apart(s, r, T, d) || !in_place_or_apart(y, x, T, d) || !in_place_or_apart(y, r, T, d) || !apart(s, y, T, d))
     return FLOP_ERR_INVALID_ARG;
+  const Span rs(stats, 1, 2 * T, 2 * T, 4);
+  for (const Span& v : {rs, Span(weight, 1, d, d, 4), Span(bias, 1, d, d, 4)})
+    if (y.span(T, d).meets(v) || (s.given() && s.span(T, d).meets(v))) return FLOP_ERR_INVALID_ARG;
+  if (rs.meets(x.span(T, d)) || (r.given() && rs.meets(r.span(T, d))) || rs.meets(Span(weight, 1, d, d, 4)) || rs.meets(Span(bias, 1, d, d, 4))) return FLOP_ERR_INVALID_ARG;
   norm::FwdArgs a{};
   a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.S = S; a.lds = lds; a.Y = Y; a.ldy = ldy; a.w = weight; a.b = bias; a.stats = (float2*)stats; a.eps = eps;
   a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
@@ -452,6 +456,14 @@ int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds
     for (const RowsArg* in : {&dy, &s, &ds})
       if (!in_place_or_apart(*out, *in, T, d)) return FLOP_ERR_INVALID_ARG;
   if (!apart(dx, dr, T, d)) return FLOP_ERR_INVALID_ARG;
+  const Span gw(dweight, 1, d, d, 4), gb(dbias, 1, d, d, 4), rs(stats, 1, 2 * T, 2 * T, 4), wv(weight, 1, d, d, 4);
+  for (const RowsArg* out : {&dx, &dr}) {
+    const Span o = out->given() ? out->span(T, d) : Span();
+    if (o.meets(gw) || o.meets(gb) || o.meets(rs) || o.meets(wv)) return FLOP_ERR_INVALID_ARG;
+  }
+  for (const RowsArg* in : {&dy, &s, &ds})
+    if (in->given() && (in->span(T, d).meets(gw) || in->span(T, d).meets(gb))) return FLOP_ERR_INVALID_ARG;
+  if (gw.meets(gb) || gw.meets(rs) || gb.meets(rs) || gw.meets(wv) || gb.meets(wv)) return FLOP_ERR_INVALID_ARG;
   norm::BwdArgs a{};
   if (dweight || dbias) {
     Arena ar{(unsigned char*)ws, ws_bytes, 0};

@@ -1,5 +1,5 @@
-// Rows of tokens in units of eight columns (a "group"): 16 bytes of bf16, two pieces of 16 bytes of fp32.  The operators on token
-// rows (dropout, layer norm, embedding lookup) load, compute and store whole groups; a row's last group may hold fewer columns.
+// Rows of tokens in pieces.  A group is eight columns (16 bytes of bf16, 32 of fp32), what one block of the generator serves; a unit is 16 bytes, what a thread copies,
+// loads and stores at once.  A row's last group and unit may hold fewer columns.
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>

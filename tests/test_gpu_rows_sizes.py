@@ -68,12 +68,13 @@ def test_embedding_adds(b, T, V, d, how, out):
 
 def test_gradient_of_rows_without_a_gap(b):
     """The table's gradient as one run of bytes that does not end on 16 of them."""
-    for V, d, T in ((77, 13, 2000), (1001, 3, 1500), (5, 1, 1100), (33, 2, 40)):
+    for V, d, T, shift in ((77, 13, 2000, 0), (1001, 3, 1500, 1), (5, 1, 1100, 2), (33, 2, 40, 3), (300, 410, 1100, 3), (300, 411, 900, 1), (1, 3, 1200, 1), (2, 1, 1030, 3)):
         ids = words(np.random.default_rng(V), "any", T, V)
         dY = torch.randn(T, d, device="cuda")
-        buf = torch.full((V * d + 9,), 7.0, device="cuda")
+        whole = torch.full((V * d + 9 + shift,), 7.0, device="cuda")
+        buf = whole[shift:]
         dE = buf[:V * d].view(V, d)
         b.embedding_bwd(dY, ids, 1.0, dE, b.alloc_workspace(b.workspace_bytes(b.OP_EMBEDDING_SORTED_BWD, T, d, 0, V, b.F32)))
         want, size, count = R.embedding_bwd(dY.double().cpu().numpy(), ids.cpu().numpy(), V, 1.0)
         assert np.all(np.abs(dE.double().cpu().numpy() - want) <= (count[:, None] + 10) * R.U * size)
-        assert torch.all(buf[V * d:] == 7)
+        assert torch.all(buf[V * d:] == 7) and torch.all(whole[:shift] == 7)

@@ -93,6 +93,16 @@ def test_norm_backward(lib, change, code):
     assert norm_bwd(lib, **change) == code
 
 
+@pytest.mark.parametrize("change", [dict(stats=3 * P), dict(stats=P + 64), dict(w=3 * P + 128), dict(bias=3 * P), dict(stats=5 * P), dict(S=2 * P, stats=2 * P + 8), dict(R=2 * P, stats=2 * P)])
+def test_norm_forward_vectors_that_overlap(lib, change):
+    assert norm_fwd(lib, **change) == BAD
+
+
+@pytest.mark.parametrize("change", [dict(dw=7 * P), dict(db=6 * P + 8), dict(dw=3 * P), dict(db=P), dict(dw=2 * P), dict(dw=5 * P), dict(db=4 * P), dict(dX=4 * P), dict(dX=5 * P), dict(dR=6 * P)])
+def test_norm_backward_vectors_that_overlap(lib, change):
+    assert norm_bwd(lib, **change) == BAD
+
+
 def test_workspaces(lib):
     assert b.workspace_bytes(b.OP_EMBEDDING_SORTED_BWD, 1000, 64, 0, 50, b.BF16) >= 2 * 8 * 1000
     assert b.workspace_bytes(b.OP_EMBEDDING_SORTED_BWD, 0, 64, 0, 50, b.BF16) == 0

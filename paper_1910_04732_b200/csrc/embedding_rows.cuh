@@ -639,10 +639,10 @@ joints_kernel(const RunArgs a) {
 }
 
 // ---------------------------------------------------------------- few tokens
-// Eight tokens and 256 columns a block, a warp for each token: it looks through all words, lane j keeps which of the j-th 32 are its own, and the warp of the first
-// token of a word lists the word's tokens and adds up their rows, U in flight; where they are many, the eight warps of the block do, an eighth of the list each, and
+// Eight tokens and 256 columns a block, a warp for each token: it looks through all words, lane j keeps which of the j-th and of the (j + 32)-th 32 are its own, and the warp of the
+// first token of a word lists the word's tokens and adds up their rows, U in flight; where they are many, the eight warps of the block do, an eighth of the list each, and
 // their sums are added in order.  The blocks behind clear a range of dE's rows each, but for the words that occur, which they mark first.
-constexpr int kFewTokens = 1024, kFewRows = 4096;        // a bit of 32 lanes for each token; rows that a block can mark
+constexpr int kFewTokens = 2048, kFewRows = 4096;        // two bits of 32 lanes' words for each token; rows that a block can mark
 template <typename T, typename TW>
 __global__ void __launch_bounds__(256)
 few_kernel(const RunArgs a) {
@@ -651,8 +651,9 @@ few_kernel(const RunArgs a) {
   constexpr int U = sizeof(T) == 2 ? 8 : 4, kAlone = 2 * U;
   __shared__ int32_t ids[kFewTokens];
   __shared__ uint16_t list[8][kFewTokens];
-  __shared__ float red[8][32][8];
-  __shared__ int many[8];                                // tokens of a word that all warps add up
+  __shared__ int2 many[8];                               // a word that all warps add up, and how many tokens it has
+  float(*red)[32][8] = reinterpret_cast<float(*)[32][8]>(ids);           // once the words have been looked through
+  static_assert(sizeof(ids) >= 8 * 32 * 8 * sizeof(float), "");
   uint32_t* marks = reinterpret_cast<uint32_t*>(list);
   static_assert(kFewRows / 8 <= (int)sizeof(list), "");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_tokens = (int)a.T;
@@ -674,28 +675,31 @@ few_kernel(const RunArgs a) {
   __syncthreads();
   const int eight = blockIdx.x / a.slices, t = eight * 8 + warp, k = (((int)blockIdx.x - eight * a.slices) * 32 + lane) * 8, n = a.d - k;
   const int32_t word = t < n_tokens ? ids[t] : -1;
-  uint32_t mine = 0;
+  uint32_t mine[2] = {0, 0};
   bool first = word >= 0 && (uint32_t)word < a.V;
   for (int j = 0; first && j * 32 < n_tokens; j += 4) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const uint32_t m = __ballot_sync(0xffffffffu, ids[(j + u) * 32 + lane] == word);
-      if (lane == j + u) mine = m;
+      if (lane == ((j + u) & 31)) mine[(j + u) >> 5 & 1] = m;
       const int at = (j + u) * 32;
       if (at <= t && (at + 32 <= t ? m : m & ((1u << (t - at)) - 1))) first = false;
     }
   }
-  int count = first ? __popc(mine) : 0, before = 0;
+  int count = 0;
   if (first) {
-    int inc = count;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
+    for (int h = 0; h < 2; ++h) {
+      int inc = __popc(mine[h]);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+      }
+      int at = count + inc - __popc(mine[h]);
+      for (uint32_t m = mine[h]; m; m &= m - 1) list[warp][at++] = (uint16_t)((h * 32 + lane) * 32 + __ffs(m) - 1);
+      count += __shfl_sync(0xffffffffu, inc, 31);
     }
-    before = inc - count;
-    count = __shfl_sync(0xffffffffu, inc, 31);
-    for (uint32_t m = mine; m; m &= m - 1) list[warp][before++] = (uint16_t)(lane * 32 + __ffs(m) - 1);
     __syncwarp();
   }
   float acc[8];
@@ -724,10 +728,10 @@ few_kernel(const RunArgs a) {
     sum(list[warp], 0, count);
     if (n > 0) write_columns<TW, 8>(a, (uint32_t)word, k, n, acc);
   }
-  if (lane == 0) many[warp] = count > kAlone ? count : 0;
+  if (lane == 0) many[warp] = make_int2(word, count > kAlone ? count : 0);
   __syncthreads();
   for (int w = 0; w < 8; ++w) {
-    const int tokens = many[w], per = (tokens + 7) / 8;
+    const int tokens = many[w].y, per = (tokens + 7) / 8;
     if (!tokens) continue;
     sum(list[w], min(tokens, warp * per), min(tokens, (warp + 1) * per));
 #pragma unroll
@@ -740,7 +744,7 @@ few_kernel(const RunArgs a) {
 #pragma unroll
         for (int o = 0; o < 8; ++o) acc[q] += red[o][lane][q];
       }
-      write_columns<TW, 8>(a, (uint32_t)ids[eight * 8 + w], k, n, acc);
+      write_columns<TW, 8>(a, (uint32_t)many[w].x, k, n, acc);
     }
     __syncthreads();
   }

@@ -151,6 +151,10 @@ int launch_runs(const emb::RunArgs& a, int lanes, cudaStream_t st) {
   return lanes == 8 ? launch_runs_as<T, TW, 8>(a, st) : lanes == 16 ? launch_runs_as<T, TW, 16>(a, st) : launch_runs_as<T, TW, 32>(a, st);
 }
 
+// One launch, in which every token looks through all words for every 256 columns (at most 12 Mi looks), against a sort and two more launches.  us in one launch / sorted: 32000 words, 768 columns, 256
+// tokens 16.6 / 25.9, 1024 19.9 / 28.0, 1500 23.0 / 28.5, 2048 26.8 / 29.1; 205 words, 2048 columns, 1024 tokens 12.5 / 15.1, 1500 17.6 / 14.2; 50000 words, 4096 columns, 1024
+// tokens 77.6 / 71, 1500 94 / 72.  A batch of one word is the worst for it: 512 tokens, 2048 columns 13.1 / 11.1, 1024 22.5 / 12.4.
+bool few_tokens(int64_t T, int64_t d) { return T <= emb::kFewTokens && T * T * ((d + 255) / 256) <= 12 << 20; }
 template <typename T, typename TW>
 int launch_few(emb::RunArgs a, cudaStream_t st) {
   a.slices = (a.d + 255) / 256;
@@ -179,7 +183,7 @@ NormPlan plan_norm(int64_t units, int dt) {
   if (units <= 1536) return {512, 3, 512};
   if (units <= 2048) return {512, 4, 512};
   // a thread's units of fp32 take half the registers: 1024 x 16384 forward and backward 81 us, 118 walked
-  if (dt == FLOP_F32 && units <= 3072) return {1024, 3, 1024};
+  if (dt == FLOP_F32 && units <= 3 * 1024) return {1024, 3, 1024};
   if (dt == FLOP_F32 && units <= 4096) return {1024, 4, 1024};
   return {0, 0, 0};
 }
@@ -357,9 +361,7 @@ int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t
     if (dt == FLOP_BF16) return wgrad_dt == FLOP_BF16 ? go(bf16{}, bf16{}) : go(bf16{}, float{});
     return wgrad_dt == FLOP_BF16 ? go(float{}, bf16{}) : go(float{}, float{});
   };
-  // 256 / 512 / 1024 tokens of 32000 words, 768 columns: 16.5 / 17.0 / 18.7 us in one launch, 25.9 / 27.2 / 28.0 sorted; all tokens one word, 2048 columns: 7.8 / 13.1 / 22.7
-  // against 13.2 / 11.1 / 12.4
-  if (T <= emb::kFewTokens) return typed([&](auto t, auto tw) { return launch_few<decltype(t), decltype(tw)>(a, st); });
+  if (few_tokens(T, d)) return typed([&](auto t, auto tw) { return launch_few<decltype(t), decltype(tw)>(a, st); });
   emb::SortArgs s{};
   s.ids = ids; s.T = T; s.V = (uint32_t)n_rows; s.clear = z;
   s.order[0] = w.order[0]; s.order[1] = w.order[1];

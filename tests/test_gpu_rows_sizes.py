@@ -29,11 +29,11 @@ def test_norm_widths(b, kind, per, units):
     check_norm(b, kind, 3, units * per, "plain")
 
 
-@pytest.mark.parametrize("units", [3072, 4096])
-def test_norm_widths_of_wide_fp32_rows(b, units):
-    for d in (units * 4 - 1, units * 4, units * 4 + 1):
+@pytest.mark.parametrize("width", [12288, 16384])
+def test_norm_widths_of_wide_fp32_rows(b, width):
+    for d in (width - 1, width, width + 1):
         check_norm(b, "f32", 3, d, "pre", 0.2)
-    check_norm(b, "f32", 300, units * 4 - 6, "plain")
+    check_norm(b, "f32", 300, width - 6, "plain")
 
 
 @pytest.mark.parametrize("T", [1, 2, 147, 148, 149, 1184, 2368, 2369, 4737])
@@ -53,7 +53,8 @@ def test_dropout_widths(b, kind, per, units):
 @pytest.mark.parametrize("T,V,d,how", [
     (1023, 60, 72, "zipf"), (1024, 60, 72, "same"), (1024, 90000, 300, "any"), (1000, 5, 264, "runs"), (1025, 60, 72, "zipf"), (1025, 300000, 16, "any"), (2048, 511, 130, "runs"),
     (2049, 512, 130, "zipf"), (16384, 300, 40, "zipf"), (16385, 300, 40, "zipf"), (16385, 300000, 24, "any"), (40000, 262143, 8, "any"), (40000, 262144, 8, "zipf"), (70000, 3, 16, "same"),
-    (300000, 100, 8, "zipf"), (1500, 40, 4104, "zipf")])
+    (300000, 100, 8, "zipf"), (1500, 40, 4104, "zipf"), (2048, 7, 256, "same"), (2048, 900, 768, "zipf"), (2048, 900, 769, "zipf"), (2047, 90000, 24, "any"), (1254, 60, 2048, "runs"),
+    (1255, 60, 2048, "runs")])
 def test_embedding_batches(b, T, V, d, how):
     check_gradient(b, "bf16", "f32", T, V, d, how)
     check_gradient(b, "f32", "bf16", T, V, d, how)

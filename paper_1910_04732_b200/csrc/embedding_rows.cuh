@@ -639,18 +639,19 @@ joints_kernel(const RunArgs a) {
 }
 
 // ---------------------------------------------------------------- few tokens
-// Eight tokens and 256 columns a block, a warp for each token: it looks through all words, lane j keeps which of the j-th and of the (j + 32)-th 32 are its own, and the warp of the
+// Eight tokens and 256 columns a block, a warp for each token: it looks through all words, lane j keeps which of the j-th 32 are its own (of the (j + 32)-th too, WORDS = 2), and the warp of the
 // first token of a word lists the word's tokens and adds up their rows, U in flight; where they are many, the eight warps of the block do, an eighth of the list each, and
 // their sums are added in order.  The blocks behind clear a range of dE's rows each, but for the words that occur, which they mark first.
-constexpr int kFewTokens = 2048, kFewRows = 4096;        // two bits of 32 lanes' words for each token; rows that a block can mark
-template <typename T, typename TW>
+constexpr int kFewTokens = 2048, kFewRows = 4096;        // bits that two words of 32 lanes hold; rows that a block can mark
+template <typename T, typename TW, int WORDS>
 __global__ void __launch_bounds__(256)
 few_kernel(const RunArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   constexpr int U = sizeof(T) == 2 ? 8 : 4, kAlone = 2 * U;
-  __shared__ int32_t ids[kFewTokens];
-  __shared__ uint16_t list[8][kFewTokens];
+  constexpr int kTokens = 1024 * WORDS;
+  __shared__ int32_t ids[kFewTokens];                    // kTokens of them; room for the sums of eight warps
+  __shared__ uint16_t list[8][kTokens];
   __shared__ int2 many[8];                               // a word that all warps add up, and how many tokens it has
   float(*red)[32][8] = reinterpret_cast<float(*)[32][8]>(ids);           // once the words have been looked through
   static_assert(sizeof(ids) >= 8 * 32 * 8 * sizeof(float), "");
@@ -671,17 +672,17 @@ few_kernel(const RunArgs a) {
     return;
   }
 #pragma unroll
-  for (int i = threadIdx.x; i < kFewTokens; i += 256) ids[i] = i < n_tokens ? a.ids[i] : -1;
+  for (int i = threadIdx.x; i < kTokens; i += 256) ids[i] = i < n_tokens ? a.ids[i] : -1;
   __syncthreads();
   const int eight = blockIdx.x / a.slices, t = eight * 8 + warp, k = (((int)blockIdx.x - eight * a.slices) * 32 + lane) * 8, n = a.d - k;
   const int32_t word = t < n_tokens ? ids[t] : -1;
-  uint32_t mine[2] = {0, 0};
+  uint32_t mine[WORDS] = {};
   bool first = word >= 0 && (uint32_t)word < a.V;
   for (int j = 0; first && j * 32 < n_tokens; j += 4) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const uint32_t m = __ballot_sync(0xffffffffu, ids[(j + u) * 32 + lane] == word);
-      if (lane == ((j + u) & 31)) mine[(j + u) >> 5 & 1] = m;
+      if (lane == ((j + u) & 31)) mine[WORDS == 1 ? 0 : (j + u) >> 5 & 1] = m;
       const int at = (j + u) * 32;
       if (at <= t && (at + 32 <= t ? m : m & ((1u << (t - at)) - 1))) first = false;
     }
@@ -689,7 +690,7 @@ few_kernel(const RunArgs a) {
   int count = 0;
   if (first) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < WORDS; ++h) {
       int inc = __popc(mine[h]);
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {

@@ -161,7 +161,10 @@ int launch_few(emb::RunArgs a, cudaStream_t st) {
   a.token_blocks = (int)((a.T + 7) / 8) * a.slices;
   a.clear_rows = (int)std::max<int64_t>(1, std::min<int64_t>(emb::kFewRows, 65536 / std::max<int64_t>(a.clear.row_bytes, 1)));
   const int64_t clear_blocks = (a.clear.rows + a.clear_rows - 1) / a.clear_rows;
-  launch_k(emb::few_kernel<T, TW>, dim3((unsigned)(a.token_blocks + clear_blocks)), dim3(256), (size_t)0, st, a);
+  const dim3 grid((unsigned)(a.token_blocks + clear_blocks));
+  // lists of 2048 tokens in every block: 1000 tokens of 50001 x 410 fp32 25.1 us, lists of 1024 24.4
+  if (a.T <= 1024) launch_k(emb::few_kernel<T, TW, 1>, grid, dim3(256), (size_t)0, st, a);
+  else launch_k(emb::few_kernel<T, TW, 2>, grid, dim3(256), (size_t)0, st, a);
   return launched();
 }
 

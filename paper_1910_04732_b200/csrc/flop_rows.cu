@@ -428,7 +428,7 @@ int flop_layer_norm_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, 
     if (y.span(T, d).meets(v) || (s.given() && s.span(T, d).meets(v))) return FLOP_ERR_INVALID_ARG;
   if (rs.meets(x.span(T, d)) || (r.given() && rs.meets(r.span(T, d))) || rs.meets(Span(weight, 1, d, d, 4)) || rs.meets(Span(bias, 1, d, d, 4))) return FLOP_ERR_INVALID_ARG;
   norm::FwdArgs a{};
-  a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.S = S; a.lds = lds; a.Y = Y; a.ldy = ldy; a.w = weight; a.b = bias; a.stats = (float2*)stats; a.eps = eps;
+  a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.S = S; a.lds = lds; a.Y = Y; a.ldy = ldy; a.w = weight; a.b = bias; a.stats = (float2*)stats; a.eps = eps; a.inv_d = 1. / (double)d;
   a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
   a.vec = x.vec() && y.vec() && (!r.given() || r.vec()) && (!s.given() || s.vec());
   a.wvec = aligned16(weight) && aligned16(bias);

@@ -4,7 +4,16 @@
 //   backward: x^ = (s - mean) rstd, a = dy w;  g = rstd (a - mean(a) - x^ mean(a x^)) + dS;  dR = g, dX = dropout'(g);
 //             dw = sum_t dy x^, db = sum_t dy
 // Sums, means and the deviation are fp32; the variance is the mean of squared differences from the mean (a second look at the row).
+//
+// A row of equal values has differences of exactly 0, so that its result is the bias: its mean has to be the value to the last bit, whatever the width.
+//   bf16 : sums of up to 16384 equal values take 22 bits and are exact, and divided() gives a quotient that is representable as it is
+//   fp32 : sums round, and the mean is a few steps of the value off.  Where the deviation is below 2^-12 of the mean, so that this could be seen, the differences are added up and what
+//          they are off by on average is taken from them and given to the mean: of equal values they are k steps each, k below 64 (a sum of 16384 passes through at most 45 additions), and d k
+//          steps are exact.  Other rows pay a comparison (8192 x 1024 11.2 us; every row corrected 13.9, summed in fp64 13.4).
+//   walked rows are summed in fp64: 2^23 equal values take 47 bits
 #pragma once
+#include <type_traits>
+
 #include "dropout.cuh"
 
 namespace flop {
@@ -18,6 +27,7 @@ struct FwdArgs {
   const float* w; const float* b;   // nullable: ones, zeros
   float2* stats;                    // nullable: (mean, rstd) of each row
   float eps;
+  double inv_d;                     // for sums in fp64
   int64_t T;
   int d, groups, vec, wvec;
   Drop drop;
@@ -70,9 +80,9 @@ __device__ __forceinline__ Raw8<T> summed(const FwdArgs& a, const Raw8<T>& xr, c
   return pack8<T>(x);
 }
 
-// Sum over the block in a fixed order; every thread gets it.  `scratch` holds a float per warp and is free again at the next sum's barrier.
-template <int N>
-__device__ __forceinline__ void block_sum(float (&v)[N], float* scratch) {
+// Sum over the block in a fixed order; every thread gets it.  `scratch` holds a value per warp and is free again at the next sum's barrier.
+template <typename V, int N>
+__device__ __forceinline__ void block_sum(V (&v)[N], V* scratch) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
 #pragma unroll
   for (int i = 0; i < N; ++i)
@@ -86,7 +96,7 @@ __device__ __forceinline__ void block_sum(float (&v)[N], float* scratch) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    v[i] = 0.f;
+    v[i] = 0;
     for (int w = 0; w < warps; ++w) v[i] += scratch[i * 32 + w];
   }
 }
@@ -98,6 +108,7 @@ fwd_walk_kernel(const FwdArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ float scratch[32];
+  __shared__ double total_scratch[32];
   const uint64_t offset = SUM ? drop_offset(a.drop) : 0;
   const int64_t t = blockIdx.x;
   const bool inner = t + 1 < a.T;
@@ -119,15 +130,19 @@ fwd_walk_kernel(const FwdArgs a) {
     unpack8(raw, n, s);
     return n;
   };
+  double total[1] = {0.};
   float sum[1] = {0.f}, s[8];
   for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
     at(g, true, s);
+    if constexpr (sizeof(T) == 2) {                        // eight equal values take 11 bits; two of fp32 as many as one
+      total[0] += (double)(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[0] += s[j];
+      for (int j = 0; j < 8; j += 2) total[0] += (double)(s[j] + s[j + 1]);
+    }
   }
-  block_sum(sum, scratch);
-  const float mean = sum[0] / (float)a.d;
-  sum[0] = 0.f;
+  block_sum(total, total_scratch);
+  const float mean = (float)(total[0] * a.inv_d);
   for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
     const int n = at(g, false, s);
 #pragma unroll
@@ -265,6 +280,11 @@ __device__ __forceinline__ float both(uint64_t v) {
   const float2 u = unpack2(v);
   return u.x + u.y;
 }
+// sum / d: what the product with 1 / d (inv_d, rounded) leaves over is divided too.
+__device__ __forceinline__ float divided(float sum, float d, float inv_d) {
+  const float q = sum * inv_d;
+  return fmaf(fmaf(-q, d, sum), inv_d, q);
+}
 
 // What the forward kernel does with a row: WHOLE is the norm of X, SUMMED that of S = R + dropout(X); ADDED and DROPPED stop at S, with and without R: dropout by itself, which
 // has no use for whole rows, so that a row may be cut into segments of LANES * NG units (blockIdx.y).
@@ -277,11 +297,11 @@ fwd_kernel(const FwdArgs a) {
   constexpr bool SUM = MODE != WHOLE, NORM = kNorm<MODE>, RES = kTensors<MODE> == 2;
   constexpr int ROWS = THREADS / LANES, E = kUnit<T>, H = kPairs<T>, ROW = NG * THREADS, SIZE = kTensors<MODE> * RB * ROW;
   extern __shared__ uint4 ring[];                        // [STAGES][X and R][RB][NG][THREADS]
-  __shared__ float scratch[2][RB][32];
+  __shared__ float scratch[sizeof(T) == 4 ? 4 : 2][RB][32];
   const int l = threadIdx.x % LANES + (NORM ? 0 : blockIdx.y * LANES * NG), r = threadIdx.x / LANES;
   const int last = a.d - (l + (NG - 1) * LANES) * E;     // columns of the last unit
   const int batches = (int)((a.T + ROWS * RB - 1) / (ROWS * RB));
-  const float inv_d = 1.f / (float)a.d;
+  const float d = (float)a.d, inv_d = 1.f / d;
   pdl_wait();
   pdl_launch_dependents();
   const uint64_t offset = SUM ? drop_offset(a.drop) : 0, scale = SUM ? pack2(a.drop.scale, a.drop.scale) : 0;
@@ -309,95 +329,138 @@ fwd_kernel(const FwdArgs a) {
       vector_unit<T>(a.b, k, a.d - k, a.wvec, 0.f, b[i]);
     }
   }
-  int stage = 0;
-  for (int batch = blockIdx.x; batch < batches; batch += gridDim.x) {
-    copies_wait<STAGES - 1>();
-    const uint4* at = ring + stage * SIZE + threadIdx.x;
-    uint64_t s[NORM ? RB : 1][NORM ? NG : 1][H];
-    float sum[RB];
-#pragma unroll
-    for (int q = 0; q < RB; ++q) {
-      const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
-      uint64_t total = 0;
-      uint32_t bits[NG][H];
-      if (SUM && (!RES || a.drop.threshold)) drop_units<T, NG>(a.drop, l & 1, [&](int i) { return offset + (uint64_t)t * a.groups + (uint32_t)((l + i * LANES) / (8 / E)); }, bits);
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        uint64_t(&v)[H] = s[NORM ? q : 0][NORM ? i : 0];
-        unpack_unit<T>(at[q * ROW + i * THREADS], v);
-        if constexpr (SUM) {
-          uint64_t res[H];
-          if (RES && a.R) {
-            unpack_unit<T>(at[(RB + q) * ROW + i * THREADS], res);
-          } else {
-#pragma unroll
-            for (int j = 0; j < H; ++j) res[j] = 0;
-          }
-#pragma unroll
-          for (int j = 0; j < H; ++j) {
-            if (!RES) v[j] = select_pair(bits[i][j], a.drop.threshold, mul2(v[j], scale), 0);
-            else v[j] = a.drop.threshold ? select_pair(bits[i][j], a.drop.threshold, fma2(v[j], scale, res[j]), res[j]) : add2(v[j], res[j]);
-          }
-          const uint4 rounded = pack_unit<T>(v);
-          const int n = !NORM ? last + (NG - 1 - i) * LANES * E : i < NG - 1 ? E : last;
-          if (a.S && t < a.T && n > 0) store_unit((T*)a.S + t * a.lds + (l + i * LANES) * E, rounded, n, a.vec);
-          if (NORM) unpack_unit<T>(rounded, v);
-        }
-        if constexpr (NORM) {
-#pragma unroll
-          for (int j = 0; j < H; ++j) total = add2(total, v[j]);
-        }
-      }
-      sum[q] = both(total);
-    }
-    const int ahead = batch + STAGES * gridDim.x;
-    if (ahead < batches) fetch(ahead, stage);
-    copies_commit();
-    stage = stage + 1 == STAGES ? 0 : stage + 1;
-    if constexpr (NORM) {
-      row_sum<LANES, THREADS>(sum, scratch[0]);
-      float mean[RB];
-#pragma unroll
-      for (int q = 0; q < RB; ++q) {
-        mean[q] = sum[q] * inv_d;
-        const uint64_t minus = pack2(-mean[q], -mean[q]);
-        uint64_t total = 0;
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-#pragma unroll
-          for (int j = 0; j < H; ++j) s[q][i][j] = add2(s[q][i][j], minus);
-          if (i == NG - 1 && last < E) {                   // what lies behind the row's end is no difference
-#pragma unroll
-            for (int j = 0; j < H; ++j) {
-              const float2 u = unpack2(s[q][i][j]);
-              s[q][i][j] = pack2(2 * j < last ? u.x : 0.f, 2 * j + 1 < last ? u.y : 0.f);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < H; ++j) total = fma2(s[q][i][j], s[q][i][j], total);
-        }
-        sum[q] = both(total);
-      }
-      row_sum<LANES, THREADS>(sum, scratch[1]);
+  auto rows = [&](auto known) {                          // dropout: 0 no, 1 yes, 2 as the arguments say
+    constexpr int KNOWN = decltype(known)::value;
+    const bool drops = KNOWN == 2 ? a.drop.threshold != 0 : KNOWN == 1;
+    int stage = 0;
+    for (int batch = blockIdx.x; batch < batches; batch += gridDim.x) {
+      copies_wait<STAGES - 1>();
+      const uint4* at = ring + stage * SIZE + threadIdx.x;
+      uint64_t s[NORM ? RB : 1][NORM ? NG : 1][H];
+      float sum[RB];
 #pragma unroll
       for (int q = 0; q < RB; ++q) {
         const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
-        if (t >= a.T) break;
-        const float rstd = rsqrtf(fmaf(sum[q], inv_d, a.eps));
-        if (a.stats && l == 0) a.stats[t] = make_float2(mean[q], rstd);
-        const uint64_t by = pack2(rstd, rstd);
-        T* Y = (T*)a.Y + t * a.ldy + l * E;
+        uint64_t total = 0;
+        uint32_t bits[NG][H];
+        if (SUM && (!RES || drops)) drop_units<T, NG>(a.drop, l & 1, [&](int i) { return offset + (uint64_t)t * a.groups + (uint32_t)((l + i * LANES) / (8 / E)); }, bits);
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const int n = i < NG - 1 ? E : last;
-          if (n > 0) {
+          uint64_t(&v)[H] = s[NORM ? q : 0][NORM ? i : 0];
+          unpack_unit<T>(at[q * ROW + i * THREADS], v);
+          if constexpr (SUM) {
+            uint64_t res[H];
+            if (RES && a.R) {
+              unpack_unit<T>(at[(RB + q) * ROW + i * THREADS], res);
+            } else {
 #pragma unroll
-            for (int j = 0; j < H; ++j) s[q][i][j] = fma2(mul2(s[q][i][j], by), w[i][j], b[i][j]);
-            store_unit(Y + i * LANES * E, pack_unit<T>(s[q][i]), n, a.vec);
+              for (int j = 0; j < H; ++j) res[j] = 0;
+            }
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+              if (!RES) v[j] = select_pair(bits[i][j], a.drop.threshold, mul2(v[j], scale), 0);
+              else v[j] = drops ? select_pair(bits[i][j], a.drop.threshold, fma2(v[j], scale, res[j]), res[j]) : add2(v[j], res[j]);
+            }
+            const uint4 rounded = pack_unit<T>(v);
+            const int n = !NORM ? last + (NG - 1 - i) * LANES * E : i < NG - 1 ? E : last;
+            if (a.S && t < a.T && n > 0) store_unit((T*)a.S + t * a.lds + (l + i * LANES) * E, rounded, n, a.vec);
+            if (NORM) unpack_unit<T>(rounded, v);
+          }
+          if constexpr (NORM) {
+#pragma unroll
+            for (int j = 0; j < H; ++j) total = add2(total, v[j]);
+          }
+        }
+        sum[q] = both(total);
+      }
+      const int ahead = batch + STAGES * gridDim.x;
+      if (ahead < batches) fetch(ahead, stage);
+      copies_commit();
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      if constexpr (NORM) {
+        row_sum<LANES, THREADS>(sum, scratch[0]);
+        float mean[RB];
+        auto less = [&](int q, float by) {                   // the row's values less `by`; the sum of this thread's squares
+          const uint64_t minus = pack2(-by, -by);
+          uint64_t total = 0;
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+#pragma unroll
+            for (int j = 0; j < H; ++j) s[q][i][j] = add2(s[q][i][j], minus);
+            if (i == NG - 1 && last < E) {                   // what lies behind the row's end is no difference
+#pragma unroll
+              for (int j = 0; j < H; ++j) {
+                const float2 u = unpack2(s[q][i][j]);
+                s[q][i][j] = pack2(2 * j < last ? u.x : 0.f, 2 * j + 1 < last ? u.y : 0.f);
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < H; ++j) total = fma2(s[q][i][j], s[q][i][j], total);
+          }
+          return both(total);
+        };
+#pragma unroll
+        for (int q = 0; q < RB; ++q) {
+          mean[q] = divided(sum[q], d, inv_d);
+          sum[q] = less(q, mean[q]);
+        }
+        row_sum<LANES, THREADS>(sum, scratch[1]);
+        if constexpr (sizeof(T) == 4) {                      // rows whose values are nearly equal; all threads of a row agree on it
+          auto close = [&](int q) { return sum[q] <= mean[q] * mean[q] * (d * 0x1p-24f) && mean[q] != 0.f; };     // also where squares are too small to be held
+          bool any = false;
+#pragma unroll
+          for (int q = 0; q < RB; ++q) any |= close(q);
+          if (LANES < 32) any = __any_sync(0xffffffffu, any);
+          if (any) {
+            float off[RB], square[RB];
+#pragma unroll
+            for (int q = 0; q < RB; ++q) {
+              uint64_t total = 0;
+#pragma unroll
+              for (int i = 0; i < NG; ++i)
+#pragma unroll
+                for (int j = 0; j < H; ++j) total = add2(total, s[q][i][j]);
+              off[q] = both(total);
+            }
+            row_sum<LANES, THREADS>(off, scratch[2]);
+#pragma unroll
+            for (int q = 0; q < RB; ++q) {
+              off[q] = close(q) ? divided(off[q], d, inv_d) : 0.f;       // a row's result does not depend on its neighbours
+              mean[q] += off[q];
+              square[q] = less(q, off[q]);
+            }
+            row_sum<LANES, THREADS>(square, scratch[3]);
+#pragma unroll
+            for (int q = 0; q < RB; ++q) sum[q] = square[q];
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < RB; ++q) {
+          const int64_t t = ((int64_t)batch * RB + q) * ROWS + r;
+          if (t >= a.T) break;
+          const float rstd = rsqrtf(fmaf(sum[q], inv_d, a.eps));
+          if (a.stats && l == 0) a.stats[t] = make_float2(mean[q], rstd);
+          const uint64_t by = pack2(rstd, rstd);
+          T* Y = (T*)a.Y + t * a.ldy + l * E;
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            const int n = i < NG - 1 ? E : last;
+            if (n > 0) {
+#pragma unroll
+              for (int j = 0; j < H; ++j) s[q][i][j] = fma2(mul2(s[q][i][j], by), w[i][j], b[i][j]);
+              store_unit(Y + i * LANES * E, pack_unit<T>(s[q][i]), n, a.vec);
+            }
           }
         }
       }
     }
+  };
+  // Twice for sums of fp32: a condition in the loop keeps the generator's rounds from being spread among the row's other work (9000 x 410 16.6 us, 13.5 now).
+  if constexpr (sizeof(T) == 4 && MODE == SUMMED) {
+    if (a.drop.threshold) rows(std::integral_constant<int, 1>{});
+    else rows(std::integral_constant<int, 0>{});
+  } else {
+    rows(std::integral_constant<int, 2>{});
   }
 }
 

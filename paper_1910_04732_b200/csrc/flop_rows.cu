@@ -79,15 +79,22 @@ int launch_lookup(const emb::LookupArgs& a, int64_t units, cudaStream_t st) {
 struct RunPlan { int lanes, slices, chunk; int64_t chunks; };
 // Chunks so long that there are about 16 warps for an SM, which is what the rings leave room for (with 24 and shorter rings 16384 tokens of 205 words take the same time, a batch
 // of one word 38 us instead of 35); a long batch of narrow rows has no more than 4096, so that a frequent word has not too many parts.
-constexpr int kRunWarps = 16, kRunAhead = 6;
+constexpr int kRunWarps = 16, kRunAhead = 6, kLeastChunk = 16, kMostChunk = 256;
 RunPlan plan_runs(int64_t T, int64_t d) {
   RunPlan p;
   p.lanes = d <= 64 ? 8 : d <= 128 ? 16 : 32;
   p.slices = (int)((d + p.lanes * 8 - 1) / (p.lanes * 8));
-  const int64_t warps = (int64_t)num_sms() * kRunWarps, by_work = (T * p.slices * p.lanes / 32 + warps - 1) / warps, by_parts = T / 4096;
-  p.chunk = (int)round_up(std::min<int64_t>(std::max<int64_t>({16, by_work, by_parts}), 256), 4);
+  const int64_t warps = (int64_t)num_sms() * kRunWarps, by_work = (T * p.slices * p.lanes + 32 * warps - 1) / (32 * warps), by_parts = T / 4096;
+  p.chunk = (int)round_up(std::min<int64_t>(std::max<int64_t>({kLeastChunk, by_work, by_parts}), kMostChunk), 4);
   p.chunks = (T + p.chunk - 1) / p.chunk;
   return p;
+}
+// Room for the parts: the most chunks of any batch of up to T tokens, so that a workspace for a batch serves the smaller ones (their chunks are shorter, and there may be more of
+// them).  Chunks that are not of the greatest length are at least the work of a warp long.
+int64_t most_chunks(int64_t T, int64_t d) {
+  const RunPlan p = plan_runs(T, d);
+  const int64_t warps = (int64_t)num_sms() * kRunWarps, share = (int64_t)p.slices * p.lanes;
+  return std::min<int64_t>((T + kLeastChunk - 1) / kLeastChunk, std::max<int64_t>((warps * 32 + share - 1) / share, (T + kMostChunk - 1) / kMostChunk));
 }
 struct EmbWs { uint2* order[2]; uint32_t* counts; float* part; int64_t part_ld; size_t bytes; };
 EmbWs plan_emb_ws(Arena& ar, int64_t T, int64_t d) {
@@ -96,7 +103,7 @@ EmbWs plan_emb_ws(Arena& ar, int64_t T, int64_t d) {
   for (auto& o : w.order) o = (uint2*)ar.take((size_t)(T + emb::kBehind) * sizeof(uint2));
   w.counts = (uint32_t*)ar.take((size_t)emb::kSortBlocks * (1u << emb::kMaxDigitBits) * 4);
   w.part_ld = round_up(d, 8);
-  w.part = (float*)ar.take((size_t)plan_runs(T, d).chunks * 2 * w.part_ld * 4);
+  w.part = (float*)ar.take((size_t)most_chunks(T, d) * 2 * w.part_ld * 4);
   w.bytes = ar.used;
   return w;
 }
@@ -222,13 +229,22 @@ int64_t norm_parts(int64_t T, int64_t d, int dt) {
   const int64_t slabs = std::max<int64_t>((groups_of(d) + 31) / 32, 1);
   return std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, std::max<int64_t>(1, (int64_t)num_sms() * 4 / slabs)));
 }
+// Room for the parts: the most of any batch of up to T rows (equal shares may leave a larger batch fewer blocks than a smaller one), so that a workspace for a batch serves the
+// smaller ones.
+int64_t most_parts(int64_t T, int64_t d, int dt) {
+  const NormPlan p = plan_norm(units_of(d, dt), dt);
+  if (!p.lanes) return norm_parts(T, d, dt);
+  const NormShape s = bwd_shape(p.lanes, p.ng, dt);
+  const int64_t rows = (int64_t)(bwd_threads(p.lanes, p.ng) / p.lanes) * s.rb;
+  return std::min<int64_t>((T + rows - 1) / rows, (int64_t)num_sms() * s.blocks);
+}
 struct NormWs { float* part; int64_t part_ld, n_part; size_t bytes; };
 NormWs plan_norm_ws(Arena& ar, int64_t T, int64_t d, int dt) {
   NormWs w{};
   if (T == 0 || d == 0) return w;
   w.part_ld = round_up(d, 8);
   w.n_part = norm_parts(T, d, dt);
-  w.part = (float*)ar.take((size_t)w.n_part * 2 * w.part_ld * 4);
+  w.part = (float*)ar.take((size_t)most_parts(T, d, dt) * 2 * w.part_ld * 4);
   w.bytes = ar.used;
   return w;
 }

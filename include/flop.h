@@ -510,6 +510,7 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
  *   _bwd   dE[v] (= | += with accumulate) scale * sum over {t: ids[t] = v} of dY[t], in type wgrad_dt.  Without accumulate every row of
  *          dE[n_rows, d] is written (zeros for words that do not occur), with it only the rows of words that do.
  *          Sums are fp32, in an order that depends on T, d and the device alone: results are reproducible.
+ *          With accumulate the scaled sum is rounded and then added; an fp32 table's values, and sums, below 2^-126 may count as zero there.
  *          dE may not overlap dY or ids; lddy below 2^31.  ws: flop_workspace_bytes(FLOP_OP_EMBEDDING_SORTED_BWD, T, d, 0, n_rows, dt). */
 int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde, int64_t n_rows, float scale, void* Y,
                        int64_t ldy, int64_t d, int dt, void* stream);

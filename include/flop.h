@@ -502,6 +502,7 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
  * dt is the type of every matrix of a call; bf16 matrices follow the header's rules on alignment, fp32 ones may start anywhere and have any
  * leading dimension (rows that start on 16 bytes are faster).  Columns of an output from d on are left untouched.
  * At most 2^31 - 1 rows, 2^23 columns (FLOP_ERR_UNSUPPORTED beyond).
+ * Matrices of one pitch may lie side by side in the rows of a buffer: that is no overlap.
  * A workspace sized for T rows serves every smaller T of the same call.
  *
  * Embedding, dense (the counterpart of flop_gated_embedding_* for a table that is not factorised): ids[T] (int32, DEVICE) are rows of

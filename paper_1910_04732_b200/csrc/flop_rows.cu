@@ -24,12 +24,22 @@ struct RowsArg {
   bool placed() const { return dt != FLOP_BF16 || bf16_ok(p, ld); }                         // the library's rule for bf16
   bool vec() const { return aligned16(p) && (ld * (int64_t)elt(dt)) % 16 == 0; }            // rows start on 16 bytes
   Span span(int64_t T, int64_t d) const { return Span(p, T, d, ld, elt(dt)); }
+  // Whether this matrix, of T rows, and another one of To rows share a byte.  Rows of the same pitch may lie side by side: then neither's columns reach the other's, to the right or,
+  // in the next row, to the left.
+  bool meets(const RowsArg& o, int64_t T, int64_t To, int64_t d) const {
+    if (!span(T, d).meets(o.span(To, d))) return false;
+    const uint64_t pitch = (uint64_t)ld * elt(dt), mine = (uint64_t)d * elt(dt), theirs = (uint64_t)d * elt(o.dt);
+    if (pitch != (uint64_t)o.ld * elt(o.dt)) return true;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    const uint64_t right = a <= b ? (b - a) % pitch : (pitch - (a - b) % pitch) % pitch;      // from a row's start to that of the other's next one
+    return right < mine || pitch - right < theirs;
+  }
 };
 // Every row is read before it is written, element by element by the same thread, so an output may be an input; half of it may not.
 bool in_place_or_apart(const RowsArg& out, const RowsArg& in, int64_t T, int64_t d) {
-  return !out.given() || !in.given() || (out.p == in.p && out.ld == in.ld && out.dt == in.dt) || !out.span(T, d).meets(in.span(T, d));
+  return !out.given() || !in.given() || (out.p == in.p && out.ld == in.ld && out.dt == in.dt) || !out.meets(in, T, T, d);
 }
-bool apart(const RowsArg& a, const RowsArg& b, int64_t T, int64_t d) { return !a.given() || !b.given() || !a.span(T, d).meets(b.span(T, d)); }
+bool apart(const RowsArg& a, const RowsArg& b, int64_t T, int64_t d) { return !a.given() || !b.given() || !a.meets(b, T, T, d); }
 
 int64_t groups_of(int64_t d) { return (d + 7) / 8; }
 int64_t units_of(int64_t d, int dt) { return (d * (int64_t)elt(dt) + 15) / 16; }
@@ -348,7 +358,7 @@ int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde
   const RowsArg e{E, lde, dt}, y{Y, ldy, dt};
   if (!ids || !y.given() || !y.fits(d) || (n_rows > 0 && (!e.given() || !e.fits(d)))) return FLOP_ERR_INVALID_ARG;
   if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || !y.placed() || (n_rows > 0 && !e.placed())) return FLOP_ERR_UNSUPPORTED;
-  if (e.span(n_rows, d).meets(y.span(T, d)) || Span(ids, 1, T, T, 4).meets(y.span(T, d))) return FLOP_ERR_INVALID_ARG;
+  if (e.meets(y, n_rows, T, d) || Span(ids, 1, T, T, 4).meets(y.span(T, d))) return FLOP_ERR_INVALID_ARG;
   emb::LookupArgs a{};
   a.ids = ids; a.T = T; a.E = E; a.lde = lde; a.V = n_rows; a.Y = Y; a.ldy = ldy; a.scale = scale; a.d = (int)d;
   a.vec = y.vec() && (n_rows == 0 || e.vec());
@@ -363,7 +373,7 @@ int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t
   if (!de.given() || !de.fits(d) || (T > 0 && (!ids || !dy.given() || !dy.fits(d)))) return FLOP_ERR_INVALID_ARG;
   if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || lddy > INT32_MAX || !de.placed() || (T > 0 && !dy.placed())) return FLOP_ERR_UNSUPPORTED;
   const Span out = de.span(n_rows, d);
-  if (T > 0 && (out.meets(dy.span(T, d)) || out.meets(Span(ids, 1, T, T, 4)))) return FLOP_ERR_INVALID_ARG;
+  if (T > 0 && (de.meets(dy, n_rows, T, d) || out.meets(Span(ids, 1, T, T, 4)))) return FLOP_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   Arena ar{(unsigned char*)ws, ws_bytes, 0};
   const EmbWs w = plan_emb_ws(ar, T, d);

@@ -499,8 +499,9 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
                               void* stream);
 
 /* Operators on token rows, in front of and between the factorised matrices of a model in training (no counterpart in the paper).
- * dt is the type of every matrix of a call; bf16 matrices follow the header's rules on alignment, fp32 ones may start anywhere and have any
- * leading dimension (rows that start on 16 bytes are faster).  Columns of an output from d on are left untouched.
+ * dt is the type of every matrix of a call; bf16 matrices follow the header's rules on alignment, fp32 ones may start anywhere (on a multiple of
+ * 4 bytes, like ids and vectors; offset_dev: 8, FLOP_ERR_UNSUPPORTED otherwise) and have any leading dimension (rows that start on 16 bytes
+ * are faster).  Columns of an output from d on are left untouched.
  * At most 2^31 - 1 rows, 2^23 columns (FLOP_ERR_UNSUPPORTED beyond).
  * Matrices of one pitch may lie side by side in the rows of a buffer: that is no overlap.
  * A workspace sized for T rows serves every smaller T of the same call.

@@ -16,12 +16,16 @@ namespace {
 
 constexpr int64_t kMaxCols = 1 << 23;      // a launch has at most 65535 segments of a row, of 256 columns or more
 
+// Kernels read and write whole values: an address between them would fault.
+bool on_values(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }         // fp32, int32
+bool on_pairs(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0; }          // the generator's counter, (mean, rstd)
+
 // A matrix that an operator reads or writes: where it lies, and whether the kernels can take it.
 struct RowsArg {
   const void* p; int64_t ld; int dt;
   bool given() const { return p != nullptr; }
   bool fits(int64_t d) const { return ld >= d; }
-  bool placed() const { return dt != FLOP_BF16 || bf16_ok(p, ld); }                         // the library's rule for bf16
+  bool placed() const { return dt == FLOP_BF16 ? bf16_ok(p, ld) : on_values(p); }           // the library's rule for bf16; whole values
   bool vec() const { return aligned16(p) && (ld * (int64_t)elt(dt)) % 16 == 0; }            // rows start on 16 bytes
   Span span(int64_t T, int64_t d) const { return Span(p, T, d, ld, elt(dt)); }
   // Whether this matrix, of T rows, and another one of To rows share a byte.  Rows of the same pitch may lie side by side: then neither's columns reach the other's, to the right or,
@@ -357,7 +361,7 @@ int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde
   if (T == 0 || d == 0) return FLOP_OK;
   const RowsArg e{E, lde, dt}, y{Y, ldy, dt};
   if (!ids || !y.given() || !y.fits(d) || (n_rows > 0 && (!e.given() || !e.fits(d)))) return FLOP_ERR_INVALID_ARG;
-  if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || !y.placed() || (n_rows > 0 && !e.placed())) return FLOP_ERR_UNSUPPORTED;
+  if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || !y.placed() || (n_rows > 0 && !e.placed()) || !on_values(ids)) return FLOP_ERR_UNSUPPORTED;
   if (e.meets(y, n_rows, T, d) || Span(ids, 1, T, T, 4).meets(y.span(T, d))) return FLOP_ERR_INVALID_ARG;
   emb::LookupArgs a{};
   a.ids = ids; a.T = T; a.E = E; a.lde = lde; a.V = n_rows; a.Y = Y; a.ldy = ldy; a.scale = scale; a.d = (int)d;
@@ -371,7 +375,7 @@ int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t
   if (n_rows == 0 || d == 0 || (T == 0 && accumulate)) return FLOP_OK;
   const RowsArg dy{dY, lddy, dt}, de{dE, ldde, wgrad_dt};
   if (!de.given() || !de.fits(d) || (T > 0 && (!ids || !dy.given() || !dy.fits(d)))) return FLOP_ERR_INVALID_ARG;
-  if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || lddy > INT32_MAX || !de.placed() || (T > 0 && !dy.placed())) return FLOP_ERR_UNSUPPORTED;
+  if (T > INT32_MAX || n_rows > INT32_MAX || d > kMaxCols || lddy > INT32_MAX || !de.placed() || (T > 0 && (!dy.placed() || !on_values(ids)))) return FLOP_ERR_UNSUPPORTED;
   const Span out = de.span(n_rows, d);
   if (T > 0 && (de.meets(dy, n_rows, T, d) || out.meets(Span(ids, 1, T, T, 4)))) return FLOP_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
@@ -417,7 +421,7 @@ static int dropout_impl(const void* X, int64_t ldx, const void* R, int64_t ldr, 
   if (T == 0 || d == 0) return FLOP_OK;
   const RowsArg x{X, ldx, dt}, r{R, ldr, dt}, y{Y, ldy, dt};
   if (!x.given() || !x.fits(d) || !y.given() || !y.fits(d) || (r.given() && !r.fits(d))) return FLOP_ERR_INVALID_ARG;
-  if (T > INT32_MAX || d > kMaxCols || !x.placed() || !y.placed() || (r.given() && !r.placed())) return FLOP_ERR_UNSUPPORTED;
+  if (T > INT32_MAX || d > kMaxCols || !x.placed() || !y.placed() || (r.given() && !r.placed()) || !on_pairs(offset_dev)) return FLOP_ERR_UNSUPPORTED;
   if (!in_place_or_apart(y, x, T, d) || !in_place_or_apart(y, r, T, d)) return FLOP_ERR_INVALID_ARG;
   norm::FwdArgs a{};
   a.X = X; a.ldx = ldx; a.R = R; a.ldr = ldr; a.S = Y; a.lds = ldy; a.T = T; a.d = (int)d; a.groups = (int)groups_of(d);
@@ -445,7 +449,7 @@ int flop_layer_norm_fwd(const void* X, int64_t ldx, const void* R, int64_t ldr, 
   const RowsArg x{X, ldx, dt}, r{R, ldr, dt}, s{S, lds, dt}, y{Y, ldy, dt};
   if (!x.given() || !x.fits(d) || !y.given() || !y.fits(d) || (r.given() && !r.fits(d)) || (s.given() && !s.fits(d))) return FLOP_ERR_INVALID_ARG;
   if (T > INT32_MAX || d > kMaxCols || !x.placed() || !y.placed() || (r.given() && !r.placed()) || (s.given() && !s.placed()) ||
-      (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+      !on_pairs(stats) || !on_pairs(offset_dev) || !on_values(weight) || !on_values(bias))
     return FLOP_ERR_UNSUPPORTED;
   if (!in_place_or_apart(s, x, T, d) || !in_place_or_apart(s, r, T, d) || !in_place_or_apart(y, x, T, d) || !in_place_or_apart(y, r, T, d) || !apart(s, y, T, d))
     return FLOP_ERR_INVALID_ARG;
@@ -471,7 +475,7 @@ int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds
   if (T < 0 || d < 0 || !valid_dt(dt) || !valid_p(p)) return FLOP_ERR_INVALID_ARG;
   if (d == 0) return FLOP_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  if (d > kMaxCols || T > INT32_MAX) return FLOP_ERR_UNSUPPORTED;
+  if (d > kMaxCols || T > INT32_MAX || !on_values(dweight) || !on_values(dbias)) return FLOP_ERR_UNSUPPORTED;
   if (T == 0) {                          // sums over no rows
     if (accumulate || (!dweight && !dbias)) return FLOP_OK;
     launch_k(norm::bwd_finish_kernel, dim3((unsigned)((d + 31) / 32), 2), dim3(32 * norm::kFinishWarps), (size_t)0, st, (const float*)nullptr, (int64_t)0, 0, (int)d, dweight, dbias, 0);
@@ -481,7 +485,7 @@ int flop_layer_norm_bwd(const void* dY, int64_t lddy, const void* S, int64_t lds
   if (!dy.given() || !dy.fits(d) || !s.given() || !s.fits(d) || !stats || (ds.given() && !ds.fits(d)) || (dx.given() && !dx.fits(d)) || (dr.given() && !dr.fits(d)))
     return FLOP_ERR_INVALID_ARG;
   if (!dy.placed() || !s.placed() || (ds.given() && !ds.placed()) || (dx.given() && !dx.placed()) || (dr.given() && !dr.placed()) ||
-      (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+      !on_pairs(stats) || !on_pairs(offset_dev) || !on_values(weight))
     return FLOP_ERR_UNSUPPORTED;
   for (const RowsArg* out : {&dx, &dr})
     for (const RowsArg* in : {&dy, &s, &ds})

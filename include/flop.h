@@ -525,6 +525,7 @@ int flop_embedding_bwd(const void* dY, int64_t lddy, const int32_t* ids, int64_t
  *                    (offset + *offset_dev + t ceil(d / 8) + g as 64 bits, 1, 0)
  *     threshold = min(floor(65536 p + 1/2), 65535),  keep = h >= threshold,  s = 65536 / (65536 - threshold)
  *   _fwd   Y = R + keep * X * s (R nullable: 0)        _bwd   dX = keep * dY * s  (the gradient of R is dY itself)
+ * Products and sums are rounded to fp32 one by one, then to dt.
  * p in [0, 1) is used in units of 2^-16; s is that of the probability used, so the expectation of Y is R + X.  A call uses up
  * T ceil(d / 8) counters.  flop_gate_sample draws from other counters (third word 0), so that both may share a seed.  What is
  * dropped counts as 0, whatever it holds (infinities and NaN too).  Y may be X or R (same ld), dX may be dY; no other overlap. */

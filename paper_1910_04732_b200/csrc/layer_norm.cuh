@@ -1,5 +1,5 @@
 // Layer norm of token rows, forward and backward, with the residual sum and the dropout in front of it in the same pass.
-//   forward : s = R + dropout(X), rounded to the rows' type (that is what S holds and what the blocks behind read, so it is also
+//   forward : s = R + dropout(X), the product and the sum in fp32, rounded to the rows' type (that is what S holds and what the blocks behind read, so it is also
 //             what is normalised: the result is that of the separate calls);  y = (s - mean) rstd w + b
 //   backward: x^ = (s - mean) rstd, a = dy w;  g = rstd (a - mean(a) - x^ mean(a x^)) + dS;  dR = g, dX = dropout'(g);
 //             dw = sum_t dy x^, db = sum_t dy
@@ -72,7 +72,7 @@ __device__ __forceinline__ Raw8<T> summed(const FwdArgs& a, const Raw8<T>& xr, c
   if (a.drop.threshold) {
     const uint4 bits = drop_bits(a.drop, ctr);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = drop_keeps(bits, j, a.drop.threshold) ? fmaf(x[j], a.drop.scale, r[j]) : r[j];
+    for (int j = 0; j < 8; ++j) x[j] = __fadd_rn(drop_keeps(bits, j, a.drop.threshold) ? __fmul_rn(x[j], a.drop.scale) : 0.f, r[j]);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] += r[j];
@@ -358,8 +358,8 @@ fwd_kernel(const FwdArgs a) {
             }
 #pragma unroll
             for (int j = 0; j < H; ++j) {
-              if (!RES) v[j] = select_pair(bits[i][j], a.drop.threshold, mul2(v[j], scale), 0);
-              else v[j] = drops ? select_pair(bits[i][j], a.drop.threshold, fma2(v[j], scale, res[j]), res[j]) : add2(v[j], res[j]);
+              if (!RES || drops) v[j] = select_pair(bits[i][j], a.drop.threshold, mul2(v[j], scale), 0);
+              if (RES) v[j] = add2(v[j], res[j]);
             }
             const uint4 rounded = pack_unit<T>(v);
             const int n = !NORM ? last + (NG - 1 - i) * LANES * E : i < NG - 1 ? E : last;

@@ -132,7 +132,9 @@ int flop_gemm_stamps_accumulate(const unsigned long long* stamps_dev, int capaci
                                 void* stream);
 
 /* Bytes of scratch the given call needs (HOST out pointer).  For FLOP_OP_L0
- * pass the total number of gates as T and the number of segments as r. */
+ * pass the total number of gates as T and the number of segments as r.
+ * FLOP_OP_BWD in bf16: that of this T.  Its products are split by size, and a smaller
+ * batch may need more than a larger one. */
 int flop_workspace_bytes(int op, int64_t T, int64_t d_in, int64_t d_out, int64_t r, int dt,
                          size_t* out_bytes);
 
@@ -511,7 +513,8 @@ int flop_distill_topk_fwd_bwd(const void* S, int64_t lds, int64_t T, int64_t V, 
  *   _fwd   Y[t] = scale E[ids[t]]; zeros for padding.  Y may not overlap E or ids.
  *   _bwd   dE[v] (= | += with accumulate) scale * sum over {t: ids[t] = v} of dY[t], in type wgrad_dt.  Without accumulate every row of
  *          dE[n_rows, d] is written (zeros for words that do not occur), with it only the rows of words that do.
- *          Sums are fp32, in an order that depends on T, d and the device alone: results are reproducible.
+ *          Sums are fp32.  The same call gives the same bits on a device; how a word's terms are grouped depends on the sizes, the types, the
+ *          alignment and the other tokens' words.
  *          With accumulate the scaled sum is rounded and then added; an fp32 table's values, and sums, below 2^-126 may count as zero there.
  *          dE may not overlap dY or ids; lddy below 2^31.  ws: flop_workspace_bytes(FLOP_OP_EMBEDDING_SORTED_BWD, T, d, 0, n_rows, dt). */
 int flop_embedding_fwd(const int32_t* ids, int64_t T, const void* E, int64_t lde, int64_t n_rows, float scale, void* Y,
@@ -545,7 +548,7 @@ int flop_dropout_bwd(const void* dY, int64_t lddy, float p, uint64_t seed, uint6
  *              x = (S - mean) rstd,  a = dY weight,  g = rstd (a - mean(a) - x mean(a x)) + dS
  *              dR = g,  dX = keep * g * s (p, seed, offset as in the forward call; p = 0: g),
  *              dweight (= | += with accumulate) sum_t dY x,  dbias likewise sum_t dY      (f32[d])
- *          Any output may be NULL.  Sums over rows are fp32, in an order that depends on T, d and the device alone.
+ *          Any output may be NULL.  Sums over rows are fp32, in an order that depends on T, d, dt and the device alone.
  *          ws: flop_workspace_bytes(FLOP_OP_LAYER_NORM_BWD, T, d, 0, 0, dt); not needed where dweight and dbias are NULL.
  * Outputs may take the place of inputs (same ld): S and Y that of X or R, dX and dR that of dY, S or dS.  S and Y, and dX and dR, are
  * apart; there is no other overlap. */

@@ -1,8 +1,9 @@
 // Embedding lookup with a scale, Y[t] = scale E[ids[t]], and the table's gradient, dE[v] = scale sum over {t: ids[t] = v} of dY[t].
 // Words outside the table are padding: a row of zeros, no gradient.
 //
-// The gradient sorts the tokens by word (stably: a word's tokens stay in the order of the batch) and adds up runs of equal words.  Every
-// sum is taken in fp32 in an order that depends on the sizes only, and every row is written once, by one thread for each column.
+// The gradient sorts the tokens by word (stably: a word's tokens stay in the order of the batch) and adds up runs of equal words.  Sums are
+// fp32; how a word's tokens are grouped depends on where its run meets the borders of chunks, or on how many there are (few_kernel), so that the same call
+// gives the same bits.  Every row is written once, by one thread for each column.
 //   sort_kernel   : one thread-block cluster sorts (word, token) pairs, least significant digit first; the blocks behind it clear dE
 //                   meanwhile, because most rows of a large table stay empty.  Long batches are sorted by two launches a digit (sort_count_kernel,
 //                   sort_move_kernel) on as many blocks as they fill

@@ -92,7 +92,8 @@ int launch_lookup(const emb::LookupArgs& a, int64_t units, cudaStream_t st) {
 
 struct RunPlan { int lanes, slices, chunk; int64_t chunks; };
 // Chunks so long that there are about 16 warps for an SM, which is what the rings leave room for (with 24 and shorter rings 16384 tokens of 205 words take the same time, a batch
-// of one word 38 us instead of 35); a long batch of narrow rows has no more than 4096, so that a frequent word has not too many parts.
+// of one word 38 us instead of 35).  A long batch of narrow rows has longer ones, up to 256 tokens, so that a frequent word has not too many parts: 4219 of 135000 tokens of 16 columns, 16384
+// of 4 Mi.
 constexpr int kRunWarps = 16, kRunAhead = 6, kLeastChunk = 16, kMostChunk = 256;
 RunPlan plan_runs(int64_t T, int64_t d) {
   RunPlan p;
@@ -174,7 +175,7 @@ int launch_runs(const emb::RunArgs& a, int lanes, cudaStream_t st) {
 
 // One launch, in which every token looks through all words for every 256 columns (at most 12 Mi looks), against a sort and two more launches.  us in one launch / sorted: 32000 words, 768 columns, 256
 // tokens 16.6 / 25.9, 1024 19.9 / 28.0, 1500 23.0 / 28.5, 2048 26.8 / 29.1; 205 words, 2048 columns, 1024 tokens 12.5 / 15.1, 1500 17.6 / 14.2; 50000 words, 4096 columns, 1024
-// tokens 77.6 / 71, 1500 94 / 72.  A batch of one word is the worst for it: 512 tokens, 2048 columns 13.1 / 11.1, 1024 22.5 / 12.4.
+// tokens 77.6 / 71, 1500 94 / 72.  A batch of one word is the worst for it, and the rule does not see it: 512 tokens, 2048 columns 13.1 / 11.1, 1024 22.5 / 12.4.
 bool few_tokens(int64_t T, int64_t d) { return T <= emb::kFewTokens && T * T * ((d + 255) / 256) <= 12 << 20; }
 template <typename T, typename TW>
 int launch_few(emb::RunArgs a, cudaStream_t st) {
@@ -222,8 +223,9 @@ constexpr NormShape fwd_shape(int ng, int threads, int tensors, int per_sm = 512
   const int rb = between(1, 4 / (ng * tensors), 4), blocks = between(1, per_sm / threads, 16);
   return {rb, blocks, between(1, kRing / (tensors * rb * ng * threads * 16 * blocks), 4)};
 }
-// One block on an SM, so that there are few parts of the column sums to add up: 512 threads, or, where a thread's three units take more than 128
-// registers, 384 (4096 x 768 bf16 15.0 us, 16.7 with 512 threads that spill).
+// One block on an SM, so that there are few parts of the column sums to add up: 512 threads, or, because a thread's three units of bf16 take more than 128
+// registers, 384 (4096 x 768 bf16 15.0 us, 16.7 with 512 threads that spill; 32 lanes still spill 8 bytes).  It goes by the units, not by the type: three of fp32 take 118.  Four units of
+// bf16 (12289 to 16384 columns) keep 512 threads, and spill 196 bytes a thread here and 120 in the forward pass with sums; so do four of fp32 on 1024 threads (64 and 128).
 constexpr int bwd_threads(int lanes, int ng) { return lanes > 512 ? lanes : ng < 3 || lanes == 512 ? 512 : 384 / lanes > 0 ? 384 / lanes * lanes : lanes; }
 // Two rows at once for every barrier among the warps that share one (16384 x 2048 bf16: 43.0 us, 44.5 one by one); fp32 rows are twice the bytes.
 constexpr NormShape bwd_shape(int lanes, int ng, int dt) {

@@ -396,17 +396,12 @@ __device__ __forceinline__ void write_columns(const RunArgs& a, uint32_t word, i
   const bool whole = a.vec_out && n >= E;
   if constexpr (sizeof(TW) == 4) {
     // This thread alone writes here: the memory adds, and nothing waits for the old values (16384 fp32 rows of 1024 columns, 40000 words: 31.5 us; read, added and written 59.8).  It
-    // takes subnormal values for zero.  Rows that do not start on 16 bytes are read and written (value by value the memory takes longer: 16384 bf16 rows of 1024 columns 90 us, 56).
-    if (a.accumulate && a.vec_out) {
-      if (whole) {
+    // takes subnormal values for zero.  What is no whole piece is read and written (by the memory, value by value: bf16 rows that start anywhere 90 us, 56 this way; and
+    // few_kernel has 68 registers instead of 56 with a path for the ends of rows).
+    if (a.accumulate && whole) {
 #pragma unroll
-        for (int j = 0; j < E; j += 4)
-          atomicAdd(reinterpret_cast<float4*>(p + j), make_float4(a.scale * v[j], a.scale * v[j + 1], a.scale * v[j + 2], a.scale * v[j + 3]));
-      } else {
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-          if (j < n) atomicAdd(p + j, a.scale * v[j]);
-      }
+      for (int j = 0; j < E; j += 4)
+        atomicAdd(reinterpret_cast<float4*>(p + j), make_float4(a.scale * v[j], a.scale * v[j + 1], a.scale * v[j + 2], a.scale * v[j + 3]));
       return;
     }
   }
